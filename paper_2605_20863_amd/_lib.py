@@ -1,7 +1,7 @@
-"""ctypes binding of the C interface in include/pda.h.
+"""ctypes binding of the C interface in include/pda.h and include/pda_ops.h.
 
-Argument marshalling only: every step of the decode attention, KV append and
-prefill runs in the HIP library ``libpda.so``. Importing this module fails loudly when the
+Argument marshalling only: every step of the decode attention, KV append,
+prefill and the operators around them runs in the HIP library ``libpda.so``. Importing this module fails loudly when the
 library has not been built; there is no fallback.
 
 torch is used for device memory and streams: tensors provide device pointers
@@ -18,6 +18,7 @@ _PKG = os.path.dirname(os.path.abspath(__file__))
 # PDA_LIBRARY may point at another build of the same library (same C interface)
 LIB_PATH = os.environ.get("PDA_LIBRARY") or os.path.join(_PKG, "libpda.so")
 HEADER_PATH = os.path.join(os.path.dirname(_PKG), "include", "pda.h")
+OPS_HEADER_PATH = os.path.join(os.path.dirname(_PKG), "include", "pda_ops.h")
 
 if not os.path.exists(LIB_PATH):
     raise ImportError(
@@ -42,6 +43,8 @@ VARIANT_AUTO, VARIANT_VECTOR, VARIANT_MFMA = 0, 1, 2
 _VARIANTS = {"auto": VARIANT_AUTO, "vector": VARIANT_VECTOR, "mfma": VARIANT_MFMA}
 STATUS_LEN_CLAMPED, STATUS_BAD_BLOCK, STATUS_PREFIX_SHORTENED, STATUS_BAD_OFFSETS = 1, 2, 4, 8
 STATUS_HALF_RANGE = 16
+STATUS_BAD_POSITION, STATUS_BAD_TARGET = 32, 64
+POLICY_STATS = ("loss", "policy", "kl", "entropy", "clipped", "ratio", "old_kl", "weight")
 NOALLOC_SCRATCH_BYTES = 32 << 20   # PDA_NOALLOC_SCRATCH_BYTES
 
 
@@ -112,6 +115,63 @@ class PrefillProblem(ctypes.Structure):
     ]
 
 
+class RopeProblem(ctypes.Structure):
+    _fields_ = [
+        ("num_tokens", ctypes.c_int32),
+        ("num_q_heads", ctypes.c_int32),
+        ("num_kv_heads", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32),
+        ("rotary_dim", ctypes.c_int32),
+        ("max_positions", ctypes.c_int32),
+        ("interleaved", ctypes.c_int32),
+        ("dtype", ctypes.c_int32),
+        ("out_dtype", ctypes.c_int32),
+        ("weight_dtype", ctypes.c_int32),
+        ("eps", ctypes.c_float),
+        ("q_stride", ctypes.c_int64),
+        ("k_stride", ctypes.c_int64),
+        ("v_stride", ctypes.c_int64),
+        ("q_out_stride", ctypes.c_int64),
+        ("k_out_stride", ctypes.c_int64),
+        ("grad_q_stride", ctypes.c_int64),
+        ("grad_k_stride", ctypes.c_int64),
+    ]
+
+
+class Cache(ctypes.Structure):
+    _fields_ = [
+        ("num_seqs", ctypes.c_int32),
+        ("block_size", ctypes.c_int32),
+        ("max_blocks_per_seq", ctypes.c_int32),
+        ("max_seq_len", ctypes.c_int32),
+        ("num_blocks", ctypes.c_int64),
+        ("kv_dtype", ctypes.c_int32),
+    ]
+
+
+class LogitsProblem(ctypes.Structure):
+    _fields_ = [
+        ("num_tokens", ctypes.c_int32),
+        ("vocab", ctypes.c_int32),
+        ("row_stride", ctypes.c_int64),
+        ("dtype", ctypes.c_int32),
+        ("targets_int64", ctypes.c_int32),
+        ("temperature", ctypes.c_float),
+    ]
+
+
+class PolicyOptions(ctypes.Structure):
+    _fields_ = [
+        ("clip_low", ctypes.c_float),
+        ("clip_high", ctypes.c_float),
+        ("dual_clip", ctypes.c_float),
+        ("kl_coef", ctypes.c_float),
+        ("entropy_coef", ctypes.c_float),
+        ("grad_scale", ctypes.c_float),
+        ("dlogits_stride", ctypes.c_int64),
+    ]
+
+
 _vp = ctypes.c_void_p
 _lib.pda_paged_decode_attention.argtypes = [_vp, _vp, _vp, _vp, _vp, _vp, _vp, ctypes.c_float,
                                             ctypes.POINTER(Problem), ctypes.POINTER(Options), _vp]
@@ -141,6 +201,18 @@ _lib.pda_last_error.argtypes = []
 _lib.pda_last_error.restype = ctypes.c_char_p
 _lib.pda_version.argtypes = []
 _lib.pda_version.restype = ctypes.c_int
+# include/pda_ops.h. PDA_LIBRARY may name a build of the host code behind pda.h
+# alone; a call of one of these then fails for want of its symbol.
+_rope, _logits = ctypes.POINTER(RopeProblem), ctypes.POINTER(LogitsProblem)
+for _name, _args in (
+        ("pdaops_paged_qk_norm_rope_append", [_vp] * 14 + [_rope, ctypes.POINTER(Cache), _vp]),
+        ("pdaops_qk_norm_rope", [_vp] * 8 + [_rope, _vp]),
+        ("pdaops_qk_norm_rope_backward", [_vp] * 12 + [_rope, _vp]),
+        ("pdaops_token_logprobs", [_vp] * 4 + [_logits, _vp]),
+        ("pdaops_policy_loss", [_vp] * 10 + [_logits, ctypes.POINTER(PolicyOptions), _vp])):
+    if hasattr(_lib, _name):
+        getattr(_lib, _name).argtypes = _args
+        getattr(_lib, _name).restype = ctypes.c_int
 
 
 class PdaError(RuntimeError):
@@ -161,6 +233,11 @@ def header_symbols():
     """Names of the functions include/pda.h declares."""
     text = open(HEADER_PATH).read()
     return sorted(set(re.findall(r"^\s*(?:const\s+)?\w+\*?\s+\*?(pda_\w+)\s*\(", text, re.M)))
+
+
+def ops_header_symbols():
+    """Names of the functions include/pda_ops.h declares."""
+    return sorted(set(re.findall(r"^int (pdaops_\w+)\s*\(", open(OPS_HEADER_PATH).read(), re.M)))
 
 
 def _check(rc):
@@ -497,6 +574,231 @@ def paged_prefill_attention(q, q_offsets, k_cache, v_cache, block_table, seq_len
             v_cache.data_ptr(), block_table.data_ptr(), seq_lens.data_ptr(),
             kv_scales.data_ptr() if kv_scales is not None else None, out.data_ptr(), float(softmax_scale), prob)
     return out
+
+
+# ------------------------------------------------------------------ around attention
+
+def _on_device(index, tensors, contiguous=()):
+    """Every given tensor on HIP device ``index``; those named in ``contiguous`` contiguous."""
+    for name, t in tensors.items():
+        if t is None:
+            continue
+        if not t.is_cuda or t.get_device() != index:
+            raise ValueError(f"{name} must be on HIP device {index}")
+        if name in contiguous and not t.is_contiguous():
+            raise ValueError(f"{name} must be contiguous")
+
+
+def _device_index(t, name):
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be on a HIP device")
+    return t.get_device()
+
+
+def _heads(t, name, shape=None, dtype=None):
+    """Elements between the tokens of t [T, H, D], whose heads must be contiguous."""
+    s = t.shape
+    if len(s) != 3 or (shape is not None and s != shape):
+        raise ValueError(f"{name} must be {'[tokens, heads, head_dim]' if shape is None else tuple(shape)}, got {tuple(s)}")
+    if dtype is not None and t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    step, head, one = t.stride()
+    if (one != 1 and s[2] > 1) or (head != s[2] and s[1] > 1):
+        raise ValueError(f"{name}: a token's heads must be contiguous")
+    if s[0] <= 1:
+        return 0
+    if step < s[1] * s[2]:
+        raise ValueError(f"{name}: tokens must not overlap (an expanded tensor needs .contiguous())")
+    return step
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _rope_problem(q, k, q_weight, k_weight, cos_sin, positions, q_out, out_dtype, eps, interleaved):
+    (T, hq, d), hkv = q.shape, k.shape[1]
+    if k.shape[0] != T or k.shape[2] != d:
+        raise ValueError(f"k {tuple(k.shape)} must have q's tokens and head_dim {tuple(q.shape)}")
+    if cos_sin.dim() != 2 or cos_sin.dtype != _FLOAT32:
+        raise ValueError("cos_sin must be float32 [max_positions, rotary_dim]")
+    if positions is not None and (positions.shape != (T,) or positions.dtype != _INT32):
+        raise ValueError("positions must be int32 [tokens]")
+    if (q_weight is None) != (k_weight is None):
+        raise ValueError("q_weight and k_weight are given both or neither")
+    w = F32
+    if q_weight is not None:
+        if q_weight.shape != (d,) or k_weight.shape != (d,) or q_weight.dtype != k_weight.dtype:
+            raise ValueError("q_weight and k_weight must be [head_dim] of one dtype")
+        w = _dtype_code(q_weight, "q_weight")
+    return RopeProblem(T, hq, hkv, d, cos_sin.shape[1], cos_sin.shape[0], int(interleaved), _dtype_code(q, "q"),
+                       out_dtype, w, eps)
+
+
+def paged_qk_norm_rope_append(q, k, v, q_weight, k_weight, cos_sin, q_offsets, k_cache, v_cache, kv_scales,
+                              block_table, seq_lens, q_out, eps=1e-6, interleaved=False, positions=None,
+                              max_seq_len=0, stream=None):
+    """Enqueue the norm and rotation of new tokens' queries and keys and the write
+    of their keys and values into the paged cache, in one launch.
+
+    q [T, Hq, D], k and v [T, Hkv, D] (float32 or bfloat16; views of a packed
+    projection need no copy); rows q_offsets[b] .. q_offsets[b + 1] - 1 (int32 [B +
+    1], or None: T / B tokens each) are the last tokens of sequence b, whose length
+    with them is seq_lens[b]. q_weight, k_weight [D], or both None: rotation alone.
+    cos_sin [max_positions, rotary_dim] float32 holds each position's cosines, then
+    its sines; ``positions`` [T] int32 names rows of it other than the tokens' places.
+    The rotated queries go to q_out [T, Hq, D]; cache layouts and fp8 scales as for
+    paged_kv_append.
+    """
+    index = _device_index(q, "q")
+    _on_device(index, {"q": q, "k": k, "v": v, "q_weight": q_weight, "k_weight": k_weight, "cos_sin": cos_sin,
+                       "q_offsets": q_offsets, "k_cache": k_cache, "v_cache": v_cache, "kv_scales": kv_scales,
+                       "block_table": block_table, "seq_lens": seq_lens, "q_out": q_out, "positions": positions},
+               _APPEND_CONTIGUOUS)
+    qs, ks = _heads(q, "q"), _heads(k, "k", None, q.dtype)
+    pr = _rope_problem(q, k, q_weight, k_weight, cos_sin, positions, q_out, _dtype_code(q_out, "q_out"), eps, interleaved)
+    pr.q_stride, pr.k_stride = qs, ks
+    pr.v_stride, pr.q_out_stride = _heads(v, "v", k.shape, q.dtype), _heads(q_out, "q_out", q.shape)
+    shape, bts = k_cache.shape, block_table.shape
+    if len(shape) != 4 or shape[1] != k.shape[1] or shape[3] != k.shape[2] or v_cache.shape != (shape[0], shape[1], shape[3], shape[2]):
+        raise ValueError("shapes: k_cache [NB, Hkv, 16, D], v_cache [NB, Hkv, D, 16]")
+    if len(bts) != 2 or seq_lens.shape != bts[:1]:
+        raise ValueError("block_table must be [num_seqs, max_blocks_per_seq] and seq_lens [num_seqs]")
+    if q_offsets is not None and (q_offsets.shape != (bts[0] + 1,) or q_offsets.dtype != _INT32):
+        raise ValueError("q_offsets must be int32 [num_seqs + 1]")
+    if block_table.dtype != _INT32 or seq_lens.dtype != _INT32:
+        raise TypeError("block_table and seq_lens must be int32")
+    kv_dt = _dtype_code(k_cache, "k_cache")
+    if _dtype_code(v_cache, "v_cache") != kv_dt:
+        raise TypeError("k_cache and v_cache dtypes differ")
+    if kv_dt == FP8_E4M3 and (kv_scales is None or kv_scales.shape != (2, shape[0], shape[1]) or kv_scales.dtype != _FLOAT32):
+        raise ValueError("an fp8 cache needs float32 kv_scales [2, num_blocks, num_kv_heads]")
+    cache = Cache(bts[0], shape[2], bts[1], int(max_seq_len), shape[0], kv_dt)
+    _launch(_lib.pdaops_paged_qk_norm_rope_append, index, stream, q.data_ptr(), k.data_ptr(), v.data_ptr(), _ptr(q_weight),
+            _ptr(k_weight), cos_sin.data_ptr(), _ptr(positions), _ptr(q_offsets), q_out.data_ptr(), k_cache.data_ptr(),
+            v_cache.data_ptr(), _ptr(kv_scales), block_table.data_ptr(), seq_lens.data_ptr(), pr, cache)
+    return q_out
+
+
+_APPEND_CONTIGUOUS = frozenset(("q_weight", "k_weight", "cos_sin", "q_offsets", "k_cache", "v_cache", "kv_scales",
+                                "block_table", "seq_lens", "positions"))
+
+
+def qk_norm_rope(q, k, q_weight, k_weight, cos_sin, positions, q_out, k_out, eps=1e-6, interleaved=False, stream=None):
+    """Enqueue the norm and rotation of q [T, Hq, D] and k [T, Hkv, D] (as for
+    paged_qk_norm_rope_append) at ``positions`` [T] int32 into q_out and k_out."""
+    index = _device_index(q, "q")
+    _on_device(index, {"q": q, "k": k, "q_weight": q_weight, "k_weight": k_weight, "cos_sin": cos_sin,
+                       "positions": positions, "q_out": q_out, "k_out": k_out}, _APPEND_CONTIGUOUS)
+    qs, ks = _heads(q, "q"), _heads(k, "k", None, q.dtype)
+    pr = _rope_problem(q, k, q_weight, k_weight, cos_sin, positions, q_out, _dtype_code(q_out, "q_out"), eps, interleaved)
+    pr.q_stride, pr.k_stride = qs, ks
+    pr.q_out_stride, pr.k_out_stride = _heads(q_out, "q_out", q.shape), _heads(k_out, "k_out", k.shape, q_out.dtype)
+    _launch(_lib.pdaops_qk_norm_rope, index, stream, q.data_ptr(), k.data_ptr(), _ptr(q_weight), _ptr(k_weight),
+            cos_sin.data_ptr(), positions.data_ptr(), q_out.data_ptr(), k_out.data_ptr(), pr)
+    return q_out, k_out
+
+
+def qk_norm_rope_backward(q, k, q_weight, k_weight, cos_sin, positions, grad_q_out, grad_k_out, grad_q, grad_k,
+                          grad_q_weight=None, grad_k_weight=None, eps=1e-6, interleaved=False, stream=None):
+    """Enqueue the gradient of qk_norm_rope: grad_q, grad_k (q's dtype) from
+    grad_q_out, grad_k_out, and with weights grad_q_weight, grad_k_weight [D]
+    float32, which are written, not added to."""
+    index = _device_index(q, "q")
+    _on_device(index, {"q": q, "k": k, "q_weight": q_weight, "k_weight": k_weight, "cos_sin": cos_sin,
+                       "positions": positions, "grad_q_out": grad_q_out, "grad_k_out": grad_k_out, "grad_q": grad_q,
+                       "grad_k": grad_k, "grad_q_weight": grad_q_weight, "grad_k_weight": grad_k_weight},
+               _BACKWARD_CONTIGUOUS)
+    qs, ks = _heads(q, "q"), _heads(k, "k", None, q.dtype)
+    pr = _rope_problem(q, k, q_weight, k_weight, cos_sin, positions, grad_q, _dtype_code(q, "q"), eps, interleaved)
+    pr.q_stride, pr.k_stride = qs, ks
+    pr.q_out_stride = _heads(grad_q_out, "grad_q_out", q.shape, q.dtype)
+    pr.k_out_stride = _heads(grad_k_out, "grad_k_out", k.shape, q.dtype)
+    pr.grad_q_stride = _heads(grad_q, "grad_q", q.shape, q.dtype)
+    pr.grad_k_stride = _heads(grad_k, "grad_k", k.shape, q.dtype)
+    for name, t in (("grad_q_weight", grad_q_weight), ("grad_k_weight", grad_k_weight)):
+        if q_weight is not None and (t is None or t.shape != (q.shape[2],) or t.dtype != _FLOAT32):
+            raise ValueError(f"{name} must be float32 [head_dim]")
+    _launch(_lib.pdaops_qk_norm_rope_backward, index, stream, q.data_ptr(), k.data_ptr(), _ptr(q_weight), _ptr(k_weight),
+            cos_sin.data_ptr(), positions.data_ptr(), grad_q_out.data_ptr(), grad_k_out.data_ptr(), grad_q.data_ptr(),
+            grad_k.data_ptr(), _ptr(grad_q_weight), _ptr(grad_k_weight), pr)
+    return grad_q, grad_k
+
+
+_BACKWARD_CONTIGUOUS = frozenset(("q_weight", "k_weight", "cos_sin", "positions", "grad_q_weight", "grad_k_weight"))
+
+
+def _logits_problem(logits, targets, temperature):
+    if logits.dim() != 2 or (logits.shape[1] > 1 and logits.stride(1) != 1):
+        raise ValueError("logits must be [tokens, vocab] with contiguous rows")
+    T, V = logits.shape
+    if targets.shape != (T,) or targets.dtype not in _TARGETS:
+        raise ValueError("targets must be int64 or int32 [tokens]")
+    return LogitsProblem(T, V, _row_step(logits, "logits"), _dtype_code(logits, "logits"), _TARGETS[targets.dtype],
+                         temperature)
+
+
+def _row_step(t, name):
+    if t.shape[0] <= 1:
+        return 0
+    if t.stride(0) < t.shape[1]:
+        raise ValueError(f"{name}: rows must not overlap (an expanded tensor needs .contiguous())")
+    return t.stride(0)
+
+
+if _torch_rt is not None:
+    _TARGETS = {_torch_rt.int64: 1, _torch_rt.int32: 0}
+
+
+def _rows(tensors, T):
+    for name, t in tensors:
+        if t is not None and (t.shape != (T,) or t.dtype != _FLOAT32 or not t.is_contiguous()):
+            raise ValueError(f"{name} must be contiguous float32 [tokens]")
+
+
+def token_logprobs(logits, targets, logprobs, entropy=None, temperature=1.0, stream=None):
+    """Enqueue the log-probabilities of ``targets`` (int64 or int32 [T]; negative:
+    a row that takes no part) under logits [T, V] / temperature, and the rows'
+    entropies, into float32 [T] tensors. Rows of logits may be apart."""
+    index = _device_index(logits, "logits")
+    _on_device(index, {"targets": targets, "logprobs": logprobs, "entropy": entropy}, ("targets",))
+    pr = _logits_problem(logits, targets, temperature)
+    _rows((("logprobs", logprobs), ("entropy", entropy)), pr.num_tokens)
+    _launch(_lib.pdaops_token_logprobs, index, stream, logits.data_ptr(), targets.data_ptr(), logprobs.data_ptr(),
+            _ptr(entropy), pr)
+    return logprobs
+
+
+def policy_loss(logits, targets, old_logprobs, advantages, weights, stats, dlogits=None, logprobs=None, entropy=None,
+                ref_logprobs=None, clip_low=0.2, clip_high=0.2, dual_clip=0.0, kl_coef=0.0, entropy_coef=0.0,
+                temperature=1.0, grad_scale=1.0, stream=None):
+    """Enqueue the clipped policy loss with its KL and entropy terms and its
+    gradient at the logits.
+
+    old_logprobs, advantages, weights (and ref_logprobs) are float32 [T]; ``stats``
+    float32 [8] gets the weighted sums named in POLICY_STATS, the loss first;
+    ``dlogits`` [T, V] of the logits' dtype (may be ``logits``; None: the loss alone)
+    grad_scale times its gradient; ``logprobs`` and ``entropy`` the rows' values.
+    """
+    index = _device_index(logits, "logits")
+    _on_device(index, {"targets": targets, "old_logprobs": old_logprobs, "advantages": advantages, "weights": weights,
+                       "stats": stats, "dlogits": dlogits, "logprobs": logprobs, "entropy": entropy,
+                       "ref_logprobs": ref_logprobs}, ("targets", "stats"))
+    pr = _logits_problem(logits, targets, temperature)
+    _rows((("old_logprobs", old_logprobs), ("advantages", advantages), ("weights", weights), ("logprobs", logprobs),
+           ("entropy", entropy), ("ref_logprobs", ref_logprobs)), pr.num_tokens)
+    if stats.shape != (8,) or stats.dtype != _FLOAT32:
+        raise ValueError("stats must be float32 [8]")
+    step = 0
+    if dlogits is not None:
+        if dlogits.shape != logits.shape or dlogits.dtype != logits.dtype or (pr.vocab > 1 and dlogits.stride(1) != 1):
+            raise ValueError("dlogits must have the logits' shape and dtype, with contiguous rows")
+        step = _row_step(dlogits, "dlogits")
+    op = PolicyOptions(clip_low, clip_high, dual_clip, kl_coef, entropy_coef, grad_scale, step)
+    _launch(_lib.pdaops_policy_loss, index, stream, logits.data_ptr(), targets.data_ptr(), old_logprobs.data_ptr(),
+            _ptr(ref_logprobs), advantages.data_ptr(), weights.data_ptr(), stats.data_ptr(), _ptr(dlogits), _ptr(logprobs),
+            _ptr(entropy), pr, op)
+    return stats
 
 
 def read_device_status(stream=None, device=None) -> int:

@@ -1,0 +1,53 @@
+// Element types and wave helpers of the operators around attention
+// (pda_rope.hip, pda_policy.hip).
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace pda {
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
+// By value: a bit cast of a vector's element in place reads the vector's first.
+__device__ __forceinline__ float as_f32(uint32_t u) { return __builtin_bit_cast(float, u); }
+__device__ __forceinline__ uint32_t as_u32(float f) { return __builtin_bit_cast(uint32_t, f); }
+
+// Two floats as bf16 bits in one word (round to nearest even, one instruction).
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  const f32x2 x = {lo, hi};
+  const bf16x2 y = __builtin_convertvector(x, bf16x2);
+  return __builtin_bit_cast(uint32_t, y);
+}
+__device__ __forceinline__ uint16_t to_bf16(float x) { return (uint16_t)pack_bf16(x, x); }
+
+// Value of the lane that DPP control `ctrl` names (all lanes active).
+template <int ctrl>
+__device__ __forceinline__ float dpp(float x) {
+  return as_f32((uint32_t)__builtin_amdgcn_update_dpp(0, (int)as_u32(x), ctrl, 0xF, 0xF, true));
+}
+constexpr int kDppXor1 = 0xB1, kDppXor2 = 0x4E;  // quad_perm [1,0,3,2], [2,3,0,1]
+constexpr int kDppHalfMirror = 0x141, kDppMirror = 0x140;
+constexpr int kDppRor8 = 0x128;  // lane i of a row of 16 takes lane (i + 8) % 16's value
+
+// Sum over the aligned group of N = 8 or 16 lanes, in every lane of it.
+template <int N>
+__device__ __forceinline__ float group_sum(float x) {
+  x += dpp<kDppXor1>(x);
+  x += dpp<kDppXor2>(x);
+  x += dpp<kDppHalfMirror>(x);
+  if constexpr (N == 16) x += dpp<kDppMirror>(x);
+  return x;
+}
+
+__device__ __forceinline__ float wave_max_f(float x) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) x = fmaxf(x, __shfl_xor(x, o, 64));
+  return x;
+}
+
+}  // namespace pda

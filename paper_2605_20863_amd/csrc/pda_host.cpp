@@ -4,6 +4,7 @@
 // prefill.
 
 #include "pda.h"
+#include "pda_host.h"
 #include "pda_internal.h"
 
 #include <hip/hip_runtime.h>
@@ -370,6 +371,40 @@ int ensure_workspace(Workspace* ws, int64_t bytes, hipStream_t s) {
 }
 
 }  // namespace
+
+namespace pda {
+
+int host_fail(int code, const char* fmt, ...) {
+  char buf[512];
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(buf, sizeof buf, fmt, ap);
+  va_end(ap);
+  g_error = buf;
+  return code;
+}
+
+int host_fail_hip(hipError_t e, const char* what) { return fail_hip(e, what); }
+
+void host_clear_error() { g_error.clear(); }
+
+int hold_workspace(hipStream_t s, int64_t bytes, HeldWorkspace* out) {
+  int dev = 0;
+  hipError_t e = hipGetDevice(&dev);
+  if (e != hipSuccess) return fail_hip(e, "hipGetDevice");
+  const DeviceInfo* di = nullptr;
+  int rc;
+  if ((rc = device_info(dev, &di)) != PDA_OK) return rc;
+  if (!di->ok) return fail(PDA_EUNSUPPORTED, "device %d is %s; this library is built for gfx950", dev, di->arch.c_str());
+  Workspace* ws = workspace_for(dev, s);
+  out->lock = std::unique_lock<std::mutex>(ws->mu);
+  if ((rc = ensure_workspace(ws, bytes, s)) != PDA_OK) return rc;
+  out->base = static_cast<char*>(ws->ptr);
+  out->cus = di->cus;
+  return PDA_OK;
+}
+
+}  // namespace pda
 
 extern "C" {
 

@@ -1,0 +1,485 @@
+// HIP kernels for the log-probabilities of given tokens and the clipped policy
+// loss with its gradient at the logits, on MI355X (gfx950).
+//
+// For a row of logits l [V], z = l / temperature, target y:
+//     lse = log sum exp z,  log p = z - lse,  lp = log p_y,  H = -sum p log p
+// and with the rollout's lp0, a reference policy's lpr, advantage A, weight w,
+// d = clamp(lp - lp0, +-20), ratio = e^d, u = clamp(lpr - lp, +-20):
+//     policy = max(-A ratio, -A clip(ratio, 1 - low, 1 + high)), for A < 0 at most -A dual
+//     kl = e^u - 1 - u,   loss = sum over rows of w (policy + kl_coef kl - ent_coef H)
+//     dloss / dl_v = w / temperature ((1[v = y] - p_v) g + ent_coef p_v (log p_v + H)),
+//     g = dpolicy / dlp + kl_coef (1 - e^u), a part being 0 where its clamp or clip holds.
+//
+// Everything about a row follows from its largest logit m, s = sum e^x and
+// u = sum e^x (l - m), x = (l - m) / temperature: lp = x_y - log s,
+// H = log s - u / (temperature s). Parts of a row are merged by rescaling to the
+// larger m; s and u are float32. Logits are subtracted before they are scaled, so
+// that a row of the type's lowest values is an even distribution.
+
+#include "pda_elem.h"
+#include "pda_ops_internal.h"
+
+namespace pda {
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLowest = -3.402823466e38f;
+constexpr float kFar = -1e25f;  // bound on differences in products with a zero: its exponential is 0
+constexpr float kClamp = 20.f;  // bound on log ratios
+constexpr int kPartThreads = 256;
+constexpr int kUnroll = 8;      // 16-byte loads of a thread in flight
+
+// A row's address has the alignment of its elements only.
+typedef u32x4 __attribute__((aligned(2))) u32x4_any;
+
+template <typename T>
+constexpr int kPer = 16 / (int)sizeof(T);  // elements of a vector
+
+// -inf in every element
+template <typename T>
+__device__ __forceinline__ u32x4 nothing() {
+  const uint32_t w = sizeof(T) == 2 ? 0xFF80FF80u : 0xFF800000u;
+  return u32x4{w, w, w, w};
+}
+
+template <typename T>
+__device__ __forceinline__ float element(const u32x4& v, int i) {
+  if constexpr (sizeof(T) == 2) {
+    const uint32_t w = v[i / 2];
+    return as_f32(i & 1 ? w & 0xFFFF0000u : w << 16);
+  } else {
+    const uint32_t w = v[i];
+    return as_f32(w);
+  }
+}
+
+template <typename T>
+__device__ __forceinline__ float load1(const T* p) {
+  if constexpr (sizeof(T) == 2) return as_f32((uint32_t)*p << 16);
+  else return *p;
+}
+
+// Vector i of a row of V elements (-inf past its end).
+template <typename T>
+__device__ __forceinline__ u32x4 load_vec(const T* row, int i, int V) {
+  const int at = i * kPer<T>;
+  if (at + kPer<T> <= V) return *reinterpret_cast<const u32x4_any*>(row + at);
+  u32x4 v = nothing<T>();
+  if (at < V) {
+#pragma unroll
+    for (int e = 0; e < kPer<T>; ++e) {
+      if (at + e >= V) continue;
+      if constexpr (sizeof(T) == 2) {
+        const uint32_t x = row[at + e];
+        v[e / 2] = e & 1 ? (v[e / 2] & 0xFFFFu) | x << 16 : (v[e / 2] & 0xFFFF0000u) | x;
+      } else {
+        v[e] = as_u32(row[at + e]);
+      }
+    }
+  }
+  return v;
+}
+
+template <typename T>
+__device__ __forceinline__ void store_vec(T* row, int i, int V, const float (&y)[kPer<T>]) {
+  const int at = i * kPer<T>;
+  u32x4 v;
+  if constexpr (sizeof(T) == 2) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = pack_bf16(y[2 * e], y[2 * e + 1]);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = as_u32(y[e]);
+  }
+  if (at + kPer<T> <= V) {
+    *reinterpret_cast<u32x4_any*>(row + at) = v;
+  } else {
+#pragma unroll
+    for (int e = 0; e < kPer<T>; ++e) {
+      if (at + e >= V) continue;
+      if constexpr (sizeof(T) == 2) row[at + e] = (T)(v[e / 2] >> (16 * (e & 1)));
+      else row[at + e] = y[e];
+    }
+  }
+}
+
+template <typename T>
+__device__ __forceinline__ void store1(T* p, float y) {
+  if constexpr (sizeof(T) == 2) *p = to_bf16(y);
+  else *p = y;
+}
+
+struct Soft {
+  float m, s, u;
+};
+__device__ __forceinline__ Soft none() { return Soft{kLowest, 0.f, 0.f}; }
+
+// x's sums as of the larger maximum m.
+__device__ __forceinline__ Soft rebase(const Soft& x, float m, float c) {
+  const float d = fmaxf(x.m - m, kFar), f = __builtin_amdgcn_exp2f(d * c);
+  return Soft{m, x.s * f, f * fmaf(x.s, d, x.u)};
+}
+__device__ __forceinline__ Soft merge(const Soft& a, const Soft& b, float c) {
+  const float m = fmaxf(a.m, b.m);
+  const Soft x = rebase(a, m, c), y = rebase(b, m, c);
+  return Soft{m, x.s + y.s, x.u + y.u};
+}
+
+// Makes the compiler unpack a vector's elements again after this point, rather
+// than keep them all in registers of their own (twice the vector's for bf16).
+__device__ __forceinline__ void again(u32x4& v) { asm volatile("" : "+v"(v)); }
+
+// Adds the N vectors' elements to x.
+template <typename T, int N>
+__device__ __forceinline__ void add(Soft& x, u32x4 (&v)[N], float c) {
+  float m = x.m;
+#pragma unroll
+  for (int n = 0; n < N; ++n)
+#pragma unroll
+    for (int e = 0; e < kPer<T>; ++e) m = fmaxf(m, element<T>(v[n], e));
+  x = rebase(x, m, c);
+#pragma unroll
+  for (int n = 0; n < N; ++n) again(v[n]);
+#pragma unroll
+  for (int n = 0; n < N; ++n)
+#pragma unroll
+    for (int e = 0; e < kPer<T>; ++e) {
+      const float d = element<T>(v[n], e) - m, p = __builtin_amdgcn_exp2f(d * c);
+      x.s += p;
+      x.u = fmaf(p, fmaxf(d, kFar), x.u);
+    }
+}
+
+__device__ __forceinline__ Soft wave_merge(Soft x, float c) {
+#pragma unroll
+  for (int o = 1; o < 64; o *= 2)
+    x = merge(x, Soft{__shfl_xor(x.m, o, 64), __shfl_xor(x.s, o, 64), __shfl_xor(x.u, o, 64)}, c);
+  return x;
+}
+
+// Over the workgroup, in every thread (and a barrier for all of them).
+template <int NT>
+__device__ __forceinline__ Soft group_merge(Soft x, float c) {
+  __shared__ Soft parts[NT / 64];
+  x = wave_merge(x, c);
+  if constexpr (NT == 64) return x;
+  if ((threadIdx.x & 63) == 0) parts[threadIdx.x >> 6] = x;
+  __syncthreads();
+  x = parts[0];
+#pragma unroll
+  for (int w = 1; w < NT / 64; ++w) x = merge(x, parts[w], c);
+  return x;
+}
+
+// Row t's target, or -1 for a row that takes no part.
+__device__ __forceinline__ int target_of(const LogitsArgs& a, int t) {
+  const int64_t y = a.targets64 ? static_cast<const int64_t*>(a.targets)[t] : static_cast<const int32_t*>(a.targets)[t];
+  if (y >= a.V) {
+    if (threadIdx.x == 0) atomicOr(a.status, kStatusBadTarget);
+    return -1;
+  }
+  return y < 0 ? -1 : (int)y;
+}
+
+struct RowStats {
+  float lp, ent, log_s;
+};
+// From a row's sums and its target's logit.
+__device__ __forceinline__ RowStats row_stats(const LogitsArgs& a, const Soft& x, float ly) {
+  RowStats r;
+  if (x.s == 0.f) {  // every logit is -inf: no distribution
+    r.lp = -__builtin_huge_valf();
+    r.ent = r.log_s = 0.f;
+    return r;
+  }
+  r.log_s = logf(x.s);
+  r.lp = (ly - x.m) * a.inv_temp - r.log_s;
+  r.ent = r.log_s - x.u / x.s * a.inv_temp;
+  return r;
+}
+
+// A row's loss terms (times its weight) and the loss's derivative by lp.
+__device__ __forceinline__ float policy_terms(const LogitsArgs& a, int t, const RowStats& r, float w, float (&out)[kTerms]) {
+  const float A = a.adv[t], x = r.lp - a.old_logp[t];
+  const float d = fminf(fmaxf(x, -kClamp), kClamp), ratio = expf(d);
+  const float plain = -A * ratio, cut = -A * fminf(fmaxf(ratio, 1.f - a.clip_low), 1.f + a.clip_high);
+  bool held = cut > plain;
+  float policy = held ? cut : plain;
+  if (a.dual > 0.f && A < 0.f && policy > -A * a.dual) {
+    policy = -A * a.dual;
+    held = true;
+  }
+  float g = held || !(fabsf(x) <= kClamp) ? 0.f : plain, kl = 0.f;
+  if (a.ref_logp) {
+    const float y = a.ref_logp[t] - r.lp, u = fminf(fmaxf(y, -kClamp), kClamp), em = expm1f(u);
+    kl = em - u;
+    if (fabsf(y) <= kClamp) g -= a.kl * em;
+  }
+  const float v[kTerms] = {policy + a.kl * kl - a.ent_coef * r.ent, policy, kl, r.ent, held ? 1.f : 0.f, ratio,
+                           expm1f(-d) + d, 1.f};
+#pragma unroll
+  for (int i = 0; i < kTerms; ++i) out[i] = w != 0.f ? w * v[i] : 0.f;
+  return g;
+}
+
+__device__ __forceinline__ void write_terms(const LogitsArgs& a, int t, const float (&v)[kTerms]) {
+  f32x4* p = reinterpret_cast<f32x4*>(a.terms + (int64_t)t * kTerms);
+  p[0] = f32x4{v[0], v[1], v[2], v[3]};
+  p[1] = f32x4{v[4], v[5], v[6], v[7]};
+}
+
+// dl_v = p_v (base + slope x), x = l_v - m, p_v = exp2(x c - log2 s); + at_y for the target.
+struct Grad {
+  float m, c, log2_s, base, slope, at_y;
+  bool zero;
+};
+__device__ __forceinline__ Grad row_grad(const LogitsArgs& a, const Soft& x, const RowStats& r, float g, float w, float c) {
+#pragma clang fp contract(off)  // the products rounded: a target of probability 1 has gradient 0
+  const float k = w * a.grad_scale * a.inv_temp;
+  Grad d;
+  d.zero = k == 0.f || x.s == 0.f;
+  d.m = x.m;
+  d.c = c;
+  d.log2_s = r.log_s * kLog2e;
+  d.base = k * (a.ent_coef * (r.ent - r.log_s) - g);
+  d.slope = k * a.ent_coef * a.inv_temp;
+  d.at_y = k * g;
+  return d;
+}
+__device__ __forceinline__ float grad_of(const Grad& d, float l) {
+  const float x = l - d.m;
+  return __builtin_amdgcn_exp2f(fmaf(x, d.c, -d.log2_s)) * fmaf(d.slope, fmaxf(x, kFar), d.base);
+}
+
+// ------------------------------------------------------------- parts of rows
+
+// Sums of vectors first .. end - 1 of a row, by the workgroup's threads.
+template <typename T>
+__device__ __forceinline__ Soft sum_vectors(const T* row, int first, int end, int V, float c) {
+  Soft x = none();
+  for (int i = first + (int)threadIdx.x; i < end; i += kPartThreads * kUnroll) {
+    u32x4 v[kUnroll];
+#pragma unroll
+    for (int n = 0; n < kUnroll; ++n) {
+      const int at = i + n * kPartThreads;
+      v[n] = at < end ? load_vec(row, at, V) : nothing<T>();
+    }
+    add<T>(x, v, c);
+  }
+  return x;
+}
+
+// Workgroup (row, part). A whole row's log-probability and entropy are written;
+// of a part, or for policy_part_kernel, the sums.
+template <typename T>
+__global__ __launch_bounds__(kPartThreads) void sums_kernel(LogitsArgs a) {
+  const int t = (int)(blockIdx.x / (uint32_t)a.splits), p = (int)(blockIdx.x - (uint32_t)t * a.splits);
+  const int y = target_of(a, t);
+  const bool whole = a.splits == 1 && !a.terms;
+  if (y < 0) {
+    if (whole && threadIdx.x == 0) {
+      a.logp[t] = 0.f;
+      if (a.ent) a.ent[t] = 0.f;
+    }
+    return;
+  }
+  const T* row = static_cast<const T*>(a.logits) + (int64_t)t * a.stride;
+  const int vectors = (a.V + kPer<T> - 1) / kPer<T>, first = p * a.chunk, end = min(first + a.chunk, vectors);
+  const float c = a.inv_temp * kLog2e, ly = load1(row + y);
+  const Soft x = group_merge<kPartThreads>(sum_vectors(row, first, end, a.V, c), c);
+  if (threadIdx.x) return;
+  if (!whole) {
+    a.part[(int64_t)t * a.splits + p] = float4{x.m, x.s, x.u, ly};
+    return;
+  }
+  const RowStats r = row_stats(a, x, ly);
+  a.logp[t] = r.lp;
+  if (a.ent) a.ent[t] = r.ent;
+}
+
+// A row's parts merged, in every lane of a wave; ly: its target's logit.
+__device__ __forceinline__ Soft merge_parts(const LogitsArgs& a, int t, float c, float& ly) {
+  const int l = (int)(threadIdx.x & 63);
+  const float4 q = a.part[(int64_t)t * a.splits + min(l, a.splits - 1)];
+  ly = q.w;
+  return wave_merge(l < a.splits ? Soft{q.x, q.y, q.z} : none(), c);
+}
+
+// A wave per row.
+__global__ __launch_bounds__(kPartThreads) void finish_kernel(LogitsArgs a) {
+  const int t = (int)(blockIdx.x * (kPartThreads / 64) + (threadIdx.x >> 6));
+  if (t >= a.T) return;
+  const int64_t y = a.targets64 ? static_cast<const int64_t*>(a.targets)[t] : static_cast<const int32_t*>(a.targets)[t];
+  RowStats r = {0.f, 0.f, 0.f};
+  if (y >= 0 && y < a.V) {
+    float ly;
+    const Soft x = merge_parts(a, t, a.inv_temp * kLog2e, ly);
+    r = row_stats(a, x, ly);
+  }
+  if ((threadIdx.x & 63) == 0) {
+    a.logp[t] = r.lp;
+    if (a.ent) a.ent[t] = r.ent;
+  }
+}
+
+template <typename T>
+__device__ __forceinline__ void zero_vectors(T* out, int first, int end, int V) {
+  const float z[kPer<T>] = {};
+  for (int i = first + (int)threadIdx.x; i < end; i += (int)blockDim.x) store_vec(out, i, V, z);
+}
+
+// What thread 0 of a row writes beside the gradient.
+__device__ __forceinline__ void write_row(const LogitsArgs& a, int t, const RowStats& r, const float (&terms)[kTerms]) {
+  if (a.logp) a.logp[t] = r.lp;
+  if (a.ent) a.ent[t] = r.ent;
+  write_terms(a, t, terms);
+}
+
+// Workgroup (row, part), after sums_kernel: the loss's terms and the gradient.
+template <typename T>
+__global__ __launch_bounds__(kPartThreads) void policy_part_kernel(LogitsArgs a) {
+  const int t = (int)(blockIdx.x / (uint32_t)a.splits), p = (int)(blockIdx.x - (uint32_t)t * a.splits);
+  const int y = target_of(a, t);
+  const int vectors = (a.V + kPer<T> - 1) / kPer<T>, first = p * a.chunk, end = min(first + a.chunk, vectors);
+  T* out = static_cast<T*>(a.dlogits) + (int64_t)t * a.d_stride;
+  float terms[kTerms] = {};
+  if (y < 0) {
+    if (p == 0 && threadIdx.x == 0) write_row(a, t, RowStats{0.f, 0.f, 0.f}, terms);
+    if (a.dlogits) zero_vectors(out, first, end, a.V);
+    return;
+  }
+  const T* row = static_cast<const T*>(a.logits) + (int64_t)t * a.stride;
+  const float c = a.inv_temp * kLog2e, w = a.weight[t];
+  float ly;
+  const Soft x = merge_parts(a, t, c, ly);
+  const RowStats r = row_stats(a, x, ly);
+  const float g = policy_terms(a, t, r, w, terms);
+  if (p == 0 && threadIdx.x == 0) write_row(a, t, r, terms);
+  if (!a.dlogits) return;
+  const Grad d = row_grad(a, x, r, g, w, c);
+  if (d.zero) {
+    zero_vectors(out, first, end, a.V);
+    return;
+  }
+  for (int i = first + (int)threadIdx.x; i < end; i += kPartThreads) {
+    const u32x4 v = load_vec(row, i, a.V);
+    float o[kPer<T>];
+#pragma unroll
+    for (int e = 0; e < kPer<T>; ++e) o[e] = grad_of(d, element<T>(v, e));
+    store_vec(out, i, a.V, o);
+    if (i == y / kPer<T>) store1(out + y, grad_of(d, ly) + d.at_y);
+  }
+}
+
+// ------------------------------------------------------------- rows in registers
+
+// Workgroup per row, whose vectors stay in its threads' registers between the
+// sums and the gradient: one read and one write of the row.
+template <typename T, int NT, int N>
+__global__ __launch_bounds__(NT) void policy_row_kernel(LogitsArgs a) {
+  const int t = (int)blockIdx.x, y = target_of(a, t);
+  const int vectors = (a.V + kPer<T> - 1) / kPer<T>;
+  T* out = static_cast<T*>(a.dlogits) + (int64_t)t * a.d_stride;
+  float terms[kTerms] = {};
+  if (y < 0) {
+    if (threadIdx.x == 0) write_row(a, t, RowStats{0.f, 0.f, 0.f}, terms);
+    if (a.dlogits) zero_vectors(out, 0, vectors, a.V);
+    return;
+  }
+  const T* row = static_cast<const T*>(a.logits) + (int64_t)t * a.stride;
+  const float c = a.inv_temp * kLog2e, ly = load1(row + y), w = a.weight[t];
+  u32x4 v[N];
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    const int i = (int)threadIdx.x + n * NT;
+    v[n] = i < vectors ? load_vec(row, i, a.V) : nothing<T>();
+  }
+  Soft x = none();
+  add<T>(x, v, c);
+  x = group_merge<NT>(x, c);
+  const RowStats r = row_stats(a, x, ly);
+  const float g = policy_terms(a, t, r, w, terms);
+  if (threadIdx.x == 0) write_row(a, t, r, terms);
+  if (!a.dlogits) return;
+  const Grad d = row_grad(a, x, r, g, w, c);
+  if (d.zero) {
+    zero_vectors(out, 0, vectors, a.V);
+    return;
+  }
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    const int i = (int)threadIdx.x + n * NT;
+    if (i >= vectors) break;
+    again(v[n]);
+    float o[kPer<T>];
+#pragma unroll
+    for (int e = 0; e < kPer<T>; ++e) o[e] = grad_of(d, element<T>(v[n], e));
+    store_vec(out, i, a.V, o);
+    if (i == y / kPer<T>) store1(out + y, grad_of(d, ly) + d.at_y);
+  }
+}
+
+// The rows' terms summed in a fixed order, in float64.
+__global__ __launch_bounds__(1024) void stats_kernel(LogitsArgs a) {
+  __shared__ double sums[1024 / kTerms][kTerms];
+  const int k = (int)threadIdx.x % kTerms, r = (int)threadIdx.x / kTerms;
+  double x = 0.;
+  for (int t = r; t < a.T; t += 1024 / kTerms) x += (double)a.terms[(int64_t)t * kTerms + k];
+  sums[r][k] = x;
+  __syncthreads();
+  for (int n = 1024 / kTerms / 2; n > 0; n /= 2) {
+    if (r < n) sums[r][k] += sums[r + n][k];
+    __syncthreads();
+  }
+  if (r == 0) a.stats[k] = (float)sums[0][k];
+}
+
+hipError_t launch(const void* kernel, int64_t wgs, int threads, const LogitsArgs& a, hipStream_t s) {
+  LogitsArgs args = a;
+  void* params[] = {&args};
+  return hipLaunchKernel(kernel, dim3((unsigned)wgs), dim3((unsigned)threads), params, 0, s);
+}
+
+template <typename T>
+hipError_t logprobs_for(const LogitsArgs& a, hipStream_t s) {
+  hipError_t e = launch(reinterpret_cast<const void*>(&sums_kernel<T>), (int64_t)a.T * a.splits, kPartThreads, a, s);
+  if (e != hipSuccess || a.splits == 1) return e;
+  constexpr int rows = kPartThreads / 64;
+  return launch(reinterpret_cast<const void*>(&finish_kernel), (a.T + rows - 1) / rows, kPartThreads, a, s);
+}
+
+template <typename T, int NT, int N>
+hipError_t rows_for(const LogitsArgs& a, hipStream_t s) {
+  return launch(reinterpret_cast<const void*>(&policy_row_kernel<T, NT, N>), a.T, NT, a, s);
+}
+
+template <typename T>
+hipError_t policy_for(const LogitsArgs& a, hipStream_t s) {
+  hipError_t e = hipSuccess;
+  if (a.splits) {
+    const int64_t wgs = (int64_t)a.T * a.splits;
+    e = launch(reinterpret_cast<const void*>(&sums_kernel<T>), wgs, kPartThreads, a, s);
+    if (e == hipSuccess) e = launch(reinterpret_cast<const void*>(&policy_part_kernel<T>), wgs, kPartThreads, a, s);
+  } else if (a.T) {
+    const int v = (a.V + kPer<T> - 1) / kPer<T>;
+    e = v <= 256 * 4 ? rows_for<T, 256, 4>(a, s)
+        : v <= 256 * 8 ? rows_for<T, 256, 8>(a, s)
+        : v <= 256 * 16 ? rows_for<T, 256, 16>(a, s)
+        : v <= 512 * 16 ? rows_for<T, 512, 16>(a, s)
+        : v <= 1024 * 16 ? rows_for<T, 1024, 16>(a, s) : rows_for<T, kRowThreads, kRowVectors>(a, s);
+  }
+  if (e != hipSuccess) return e;
+  return launch(reinterpret_cast<const void*>(&stats_kernel), 1, 1024, a, s);
+}
+
+}  // namespace
+
+hipError_t launch_token_logprobs(const LogitsArgs& a, hipStream_t s) {
+  return a.bf16 ? logprobs_for<uint16_t>(a, s) : logprobs_for<float>(a, s);
+}
+
+hipError_t launch_policy_loss(const LogitsArgs& a, hipStream_t s) {
+  return a.bf16 ? policy_for<uint16_t>(a, s) : policy_for<float>(a, s);
+}
+
+}  // namespace pda
