@@ -577,32 +577,50 @@ def paged_prefill_attention(q, q_offsets, k_cache, v_cache, block_table, seq_len
 
 
 # ------------------------------------------------------------------ around attention
+#
+# As above, a call's checks are one pass that only says whether something is
+# wrong; _refuse and _heads then work out what.
 
-def _on_device(index, tensors, contiguous=()):
-    """Every given tensor on HIP device ``index``; those named in ``contiguous`` contiguous."""
-    for name, t in tensors.items():
-        if t is None:
-            continue
-        if not t.is_cuda or t.get_device() != index:
+if _torch_rt is not None:
+    _FLOATS = {_torch_rt.float32: F32, _torch_rt.bfloat16: BF16}
+    _TARGETS = {_torch_rt.int64: 1, _torch_rt.int32: 0}
+
+
+def _refuse(index, strided, packed):
+    """Raise what keeps the tensors of a call from being on HIP device ``index``, or ``packed`` ones contiguous."""
+    if index < 0:
+        raise ValueError(f"{next(iter(strided))} must be on a HIP device")
+    for name, t in {**strided, **packed}.items():
+        if t is not None and t.get_device() != index:
             raise ValueError(f"{name} must be on HIP device {index}")
-        if name in contiguous and not t.is_contiguous():
+    for name, t in packed.items():
+        if t is not None and not t.is_contiguous():
             raise ValueError(f"{name} must be contiguous")
 
 
-def _device_index(t, name):
-    if not t.is_cuda:
-        raise ValueError(f"{name} must be on a HIP device")
-    return t.get_device()
+def _apart(index, strided, packed):
+    """Whether some tensor is off HIP device ``index``, or one of ``packed`` not contiguous (None passes)."""
+    if index < 0:
+        return True
+    for t in strided:
+        if t is not None and t.get_device() != index:
+            return True
+    for t in packed:
+        if t is not None and (t.get_device() != index or not t.is_contiguous()):
+            return True
+    return False
 
 
 def _heads(t, name, shape=None, dtype=None):
-    """Elements between the tokens of t [T, H, D], whose heads must be contiguous."""
+    """Elements between the tokens of t [T, H, D], whose heads must be contiguous (0: one token)."""
     s = t.shape
     if len(s) != 3 or (shape is not None and s != shape):
         raise ValueError(f"{name} must be {'[tokens, heads, head_dim]' if shape is None else tuple(shape)}, got {tuple(s)}")
-    if dtype is not None and t.dtype != dtype:
+    if dtype is not None and t.dtype is not dtype:
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
     step, head, one = t.stride()
+    if one == 1 and head == s[2] and step >= s[1] * head and s[0] > 1:
+        return step
     if (one != 1 and s[2] > 1) or (head != s[2] and s[1] > 1):
         raise ValueError(f"{name}: a token's heads must be contiguous")
     if s[0] <= 1:
@@ -616,23 +634,33 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
-def _rope_problem(q, k, q_weight, k_weight, cos_sin, positions, q_out, out_dtype, eps, interleaved):
-    (T, hq, d), hkv = q.shape, k.shape[1]
-    if k.shape[0] != T or k.shape[2] != d:
+def _float_code(t, name):
+    code = _FLOATS.get(t.dtype)
+    if code is None:
+        raise TypeError(f"{name} must be float32 or bfloat16, got {t.dtype}")
+    return code
+
+
+def _rope_problem(q, k, q_weight, k_weight, cos_sin, positions, out_code, eps, interleaved, q_stride, k_stride, v_stride,
+                  q_out_stride, k_out_stride, grad_q_stride=0, grad_k_stride=0):
+    T, hq, d = q.shape
+    Tk, hkv, dk = k.shape
+    if Tk != T or dk != d:
         raise ValueError(f"k {tuple(k.shape)} must have q's tokens and head_dim {tuple(q.shape)}")
-    if cos_sin.dim() != 2 or cos_sin.dtype != _FLOAT32:
+    if cos_sin.dtype is not _FLOAT32 or cos_sin.dim() != 2:
         raise ValueError("cos_sin must be float32 [max_positions, rotary_dim]")
-    if positions is not None and (positions.shape != (T,) or positions.dtype != _INT32):
+    P, rot = cos_sin.shape
+    if positions is not None and (positions.dtype is not _INT32 or positions.shape != (T,)):
         raise ValueError("positions must be int32 [tokens]")
-    if (q_weight is None) != (k_weight is None):
-        raise ValueError("q_weight and k_weight are given both or neither")
     w = F32
     if q_weight is not None:
-        if q_weight.shape != (d,) or k_weight.shape != (d,) or q_weight.dtype != k_weight.dtype:
-            raise ValueError("q_weight and k_weight must be [head_dim] of one dtype")
-        w = _dtype_code(q_weight, "q_weight")
-    return RopeProblem(T, hq, hkv, d, cos_sin.shape[1], cos_sin.shape[0], int(interleaved), _dtype_code(q, "q"),
-                       out_dtype, w, eps)
+        if k_weight is None or q_weight.shape != (d,) or k_weight.shape != (d,) or q_weight.dtype is not k_weight.dtype:
+            raise ValueError("q_weight and k_weight must both be [head_dim], of one dtype, or both None")
+        w = _float_code(q_weight, "q_weight")
+    elif k_weight is not None:
+        raise ValueError("q_weight and k_weight must both be given, or both None")
+    return RopeProblem(T, hq, hkv, d, rot, P, 1 if interleaved else 0, _float_code(q, "q"), out_code, w, eps, q_stride,
+                       k_stride, v_stride, q_out_stride, k_out_stride, grad_q_stride, grad_k_stride)
 
 
 def paged_qk_norm_rope_append(q, k, v, q_weight, k_weight, cos_sin, q_offsets, k_cache, v_cache, kv_scales,
@@ -650,50 +678,49 @@ def paged_qk_norm_rope_append(q, k, v, q_weight, k_weight, cos_sin, q_offsets, k
     The rotated queries go to q_out [T, Hq, D]; cache layouts and fp8 scales as for
     paged_kv_append.
     """
-    index = _device_index(q, "q")
-    _on_device(index, {"q": q, "k": k, "v": v, "q_weight": q_weight, "k_weight": k_weight, "cos_sin": cos_sin,
-                       "q_offsets": q_offsets, "k_cache": k_cache, "v_cache": v_cache, "kv_scales": kv_scales,
-                       "block_table": block_table, "seq_lens": seq_lens, "q_out": q_out, "positions": positions},
-               _APPEND_CONTIGUOUS)
-    qs, ks = _heads(q, "q"), _heads(k, "k", None, q.dtype)
-    pr = _rope_problem(q, k, q_weight, k_weight, cos_sin, positions, q_out, _dtype_code(q_out, "q_out"), eps, interleaved)
-    pr.q_stride, pr.k_stride = qs, ks
-    pr.v_stride, pr.q_out_stride = _heads(v, "v", k.shape, q.dtype), _heads(q_out, "q_out", q.shape)
+    index = q.get_device()
+    if _apart(index, (q, k, v, q_out), (cos_sin, k_cache, v_cache, block_table, seq_lens, q_weight, k_weight, q_offsets,
+                                        kv_scales, positions)):
+        _refuse(index, {"q": q, "k": k, "v": v, "q_out": q_out},
+                {"cos_sin": cos_sin, "k_cache": k_cache, "v_cache": v_cache, "block_table": block_table,
+                 "seq_lens": seq_lens, "q_weight": q_weight, "k_weight": k_weight, "q_offsets": q_offsets,
+                 "kv_scales": kv_scales, "positions": positions})
+    dt, ks = q.dtype, k.shape
+    qs = _heads(q, "q")
+    pr = _rope_problem(q, k, q_weight, k_weight, cos_sin, positions, _float_code(q_out, "q_out"), eps, interleaved, qs,
+                       _heads(k, "k", None, dt), _heads(v, "v", ks, dt), _heads(q_out, "q_out", q.shape), 0)
     shape, bts = k_cache.shape, block_table.shape
-    if len(shape) != 4 or shape[1] != k.shape[1] or shape[3] != k.shape[2] or v_cache.shape != (shape[0], shape[1], shape[3], shape[2]):
+    if len(shape) != 4 or shape[1] != ks[1] or shape[3] != ks[2] or v_cache.shape != (shape[0], shape[1], shape[3], shape[2]):
         raise ValueError("shapes: k_cache [NB, Hkv, 16, D], v_cache [NB, Hkv, D, 16]")
     if len(bts) != 2 or seq_lens.shape != bts[:1]:
         raise ValueError("block_table must be [num_seqs, max_blocks_per_seq] and seq_lens [num_seqs]")
-    if q_offsets is not None and (q_offsets.shape != (bts[0] + 1,) or q_offsets.dtype != _INT32):
-        raise ValueError("q_offsets must be int32 [num_seqs + 1]")
-    if block_table.dtype != _INT32 or seq_lens.dtype != _INT32:
+    if block_table.dtype is not _INT32 or seq_lens.dtype is not _INT32:
         raise TypeError("block_table and seq_lens must be int32")
+    if q_offsets is not None and (q_offsets.shape != (bts[0] + 1,) or q_offsets.dtype is not _INT32):
+        raise ValueError("q_offsets must be int32 [num_seqs + 1]")
     kv_dt = _dtype_code(k_cache, "k_cache")
     if _dtype_code(v_cache, "v_cache") != kv_dt:
         raise TypeError("k_cache and v_cache dtypes differ")
-    if kv_dt == FP8_E4M3 and (kv_scales is None or kv_scales.shape != (2, shape[0], shape[1]) or kv_scales.dtype != _FLOAT32):
+    if kv_dt == FP8_E4M3 and (kv_scales is None or kv_scales.shape != (2, shape[0], shape[1]) or kv_scales.dtype is not _FLOAT32):
         raise ValueError("an fp8 cache needs float32 kv_scales [2, num_blocks, num_kv_heads]")
-    cache = Cache(bts[0], shape[2], bts[1], int(max_seq_len), shape[0], kv_dt)
     _launch(_lib.pdaops_paged_qk_norm_rope_append, index, stream, q.data_ptr(), k.data_ptr(), v.data_ptr(), _ptr(q_weight),
             _ptr(k_weight), cos_sin.data_ptr(), _ptr(positions), _ptr(q_offsets), q_out.data_ptr(), k_cache.data_ptr(),
-            v_cache.data_ptr(), _ptr(kv_scales), block_table.data_ptr(), seq_lens.data_ptr(), pr, cache)
+            v_cache.data_ptr(), _ptr(kv_scales), block_table.data_ptr(), seq_lens.data_ptr(), pr,
+            Cache(bts[0], shape[2], bts[1], max_seq_len, shape[0], kv_dt))
     return q_out
-
-
-_APPEND_CONTIGUOUS = frozenset(("q_weight", "k_weight", "cos_sin", "q_offsets", "k_cache", "v_cache", "kv_scales",
-                                "block_table", "seq_lens", "positions"))
 
 
 def qk_norm_rope(q, k, q_weight, k_weight, cos_sin, positions, q_out, k_out, eps=1e-6, interleaved=False, stream=None):
     """Enqueue the norm and rotation of q [T, Hq, D] and k [T, Hkv, D] (as for
     paged_qk_norm_rope_append) at ``positions`` [T] int32 into q_out and k_out."""
-    index = _device_index(q, "q")
-    _on_device(index, {"q": q, "k": k, "q_weight": q_weight, "k_weight": k_weight, "cos_sin": cos_sin,
-                       "positions": positions, "q_out": q_out, "k_out": k_out}, _APPEND_CONTIGUOUS)
-    qs, ks = _heads(q, "q"), _heads(k, "k", None, q.dtype)
-    pr = _rope_problem(q, k, q_weight, k_weight, cos_sin, positions, q_out, _dtype_code(q_out, "q_out"), eps, interleaved)
-    pr.q_stride, pr.k_stride = qs, ks
-    pr.q_out_stride, pr.k_out_stride = _heads(q_out, "q_out", q.shape), _heads(k_out, "k_out", k.shape, q_out.dtype)
+    index = q.get_device()
+    if _apart(index, (q, k, q_out, k_out), (cos_sin, positions, q_weight, k_weight)):
+        _refuse(index, {"q": q, "k": k, "q_out": q_out, "k_out": k_out},
+                {"cos_sin": cos_sin, "positions": positions, "q_weight": q_weight, "k_weight": k_weight})
+    qs = _heads(q, "q")
+    pr = _rope_problem(q, k, q_weight, k_weight, cos_sin, positions, _float_code(q_out, "q_out"), eps, interleaved, qs,
+                       _heads(k, "k", None, q.dtype), 0, _heads(q_out, "q_out", q.shape),
+                       _heads(k_out, "k_out", k.shape, q_out.dtype))
     _launch(_lib.pdaops_qk_norm_rope, index, stream, q.data_ptr(), k.data_ptr(), _ptr(q_weight), _ptr(k_weight),
             cos_sin.data_ptr(), positions.data_ptr(), q_out.data_ptr(), k_out.data_ptr(), pr)
     return q_out, k_out
@@ -704,66 +731,67 @@ def qk_norm_rope_backward(q, k, q_weight, k_weight, cos_sin, positions, grad_q_o
     """Enqueue the gradient of qk_norm_rope: grad_q, grad_k (q's dtype) from
     grad_q_out, grad_k_out, and with weights grad_q_weight, grad_k_weight [D]
     float32, which are written, not added to."""
-    index = _device_index(q, "q")
-    _on_device(index, {"q": q, "k": k, "q_weight": q_weight, "k_weight": k_weight, "cos_sin": cos_sin,
-                       "positions": positions, "grad_q_out": grad_q_out, "grad_k_out": grad_k_out, "grad_q": grad_q,
-                       "grad_k": grad_k, "grad_q_weight": grad_q_weight, "grad_k_weight": grad_k_weight},
-               _BACKWARD_CONTIGUOUS)
-    qs, ks = _heads(q, "q"), _heads(k, "k", None, q.dtype)
-    pr = _rope_problem(q, k, q_weight, k_weight, cos_sin, positions, grad_q, _dtype_code(q, "q"), eps, interleaved)
-    pr.q_stride, pr.k_stride = qs, ks
-    pr.q_out_stride = _heads(grad_q_out, "grad_q_out", q.shape, q.dtype)
-    pr.k_out_stride = _heads(grad_k_out, "grad_k_out", k.shape, q.dtype)
-    pr.grad_q_stride = _heads(grad_q, "grad_q", q.shape, q.dtype)
-    pr.grad_k_stride = _heads(grad_k, "grad_k", k.shape, q.dtype)
-    for name, t in (("grad_q_weight", grad_q_weight), ("grad_k_weight", grad_k_weight)):
-        if q_weight is not None and (t is None or t.shape != (q.shape[2],) or t.dtype != _FLOAT32):
-            raise ValueError(f"{name} must be float32 [head_dim]")
+    index = q.get_device()
+    if _apart(index, (q, k, grad_q_out, grad_k_out, grad_q, grad_k),
+              (cos_sin, positions, q_weight, k_weight, grad_q_weight, grad_k_weight)):
+        _refuse(index, {"q": q, "k": k, "grad_q_out": grad_q_out, "grad_k_out": grad_k_out, "grad_q": grad_q,
+                        "grad_k": grad_k},
+                {"cos_sin": cos_sin, "positions": positions, "q_weight": q_weight, "k_weight": k_weight,
+                 "grad_q_weight": grad_q_weight, "grad_k_weight": grad_k_weight})
+    dt, qs, ks = q.dtype, q.shape, k.shape
+    code, step = _float_code(q, "q"), _heads(q, "q")
+    pr = _rope_problem(q, k, q_weight, k_weight, cos_sin, positions, code, eps, interleaved, step, _heads(k, "k", None, dt), 0,
+                       _heads(grad_q_out, "grad_q_out", qs, dt), _heads(grad_k_out, "grad_k_out", ks, dt),
+                       _heads(grad_q, "grad_q", qs, dt), _heads(grad_k, "grad_k", ks, dt))
+    if q_weight is not None:
+        for name, t in (("grad_q_weight", grad_q_weight), ("grad_k_weight", grad_k_weight)):
+            if t is None or t.dtype is not _FLOAT32 or t.shape != q_weight.shape:
+                raise ValueError(f"{name} must be float32 [head_dim]")
     _launch(_lib.pdaops_qk_norm_rope_backward, index, stream, q.data_ptr(), k.data_ptr(), _ptr(q_weight), _ptr(k_weight),
             cos_sin.data_ptr(), positions.data_ptr(), grad_q_out.data_ptr(), grad_k_out.data_ptr(), grad_q.data_ptr(),
             grad_k.data_ptr(), _ptr(grad_q_weight), _ptr(grad_k_weight), pr)
     return grad_q, grad_k
 
 
-_BACKWARD_CONTIGUOUS = frozenset(("q_weight", "k_weight", "cos_sin", "positions", "grad_q_weight", "grad_k_weight"))
+def _row_step(t, name):
+    """Elements between the rows of t [T, V], whose words must be contiguous (0: one row)."""
+    if t.dim() != 2:
+        raise ValueError(f"{name} must be [tokens, vocab]")
+    T, V = t.shape
+    step, one = t.stride()
+    if one != 1 and V > 1:
+        raise ValueError(f"{name}: rows must be contiguous")
+    if T <= 1:
+        return 0
+    if step < V:
+        raise ValueError(f"{name}: rows must not overlap (an expanded tensor needs .contiguous())")
+    return step
 
 
 def _logits_problem(logits, targets, temperature):
-    if logits.dim() != 2 or (logits.shape[1] > 1 and logits.stride(1) != 1):
-        raise ValueError("logits must be [tokens, vocab] with contiguous rows")
+    step = _row_step(logits, "logits")
     T, V = logits.shape
-    if targets.shape != (T,) or targets.dtype not in _TARGETS:
+    kind = _TARGETS.get(targets.dtype)
+    if kind is None or targets.shape != (T,):
         raise ValueError("targets must be int64 or int32 [tokens]")
-    return LogitsProblem(T, V, _row_step(logits, "logits"), _dtype_code(logits, "logits"), _TARGETS[targets.dtype],
-                         temperature)
+    return LogitsProblem(T, V, step, _float_code(logits, "logits"), kind, temperature)
 
 
-def _row_step(t, name):
-    if t.shape[0] <= 1:
-        return 0
-    if t.stride(0) < t.shape[1]:
-        raise ValueError(f"{name}: rows must not overlap (an expanded tensor needs .contiguous())")
-    return t.stride(0)
-
-
-if _torch_rt is not None:
-    _TARGETS = {_torch_rt.int64: 1, _torch_rt.int32: 0}
-
-
-def _rows(tensors, T):
-    for name, t in tensors:
-        if t is not None and (t.shape != (T,) or t.dtype != _FLOAT32 or not t.is_contiguous()):
-            raise ValueError(f"{name} must be contiguous float32 [tokens]")
+def _rows(T, tensors):
+    for t in tensors:
+        if t is not None and (t.dtype is not _FLOAT32 or t.shape != (T,)):
+            raise ValueError("log-probabilities, entropies, advantages and weights must be float32 [tokens]")
 
 
 def token_logprobs(logits, targets, logprobs, entropy=None, temperature=1.0, stream=None):
     """Enqueue the log-probabilities of ``targets`` (int64 or int32 [T]; negative:
     a row that takes no part) under logits [T, V] / temperature, and the rows'
     entropies, into float32 [T] tensors. Rows of logits may be apart."""
-    index = _device_index(logits, "logits")
-    _on_device(index, {"targets": targets, "logprobs": logprobs, "entropy": entropy}, ("targets",))
+    index = logits.get_device()
+    if _apart(index, (logits,), (targets, logprobs, entropy)):
+        _refuse(index, {"logits": logits}, {"targets": targets, "logprobs": logprobs, "entropy": entropy})
     pr = _logits_problem(logits, targets, temperature)
-    _rows((("logprobs", logprobs), ("entropy", entropy)), pr.num_tokens)
+    _rows(pr.num_tokens, (logprobs, entropy))
     _launch(_lib.pdaops_token_logprobs, index, stream, logits.data_ptr(), targets.data_ptr(), logprobs.data_ptr(),
             _ptr(entropy), pr)
     return logprobs
@@ -780,24 +808,24 @@ def policy_loss(logits, targets, old_logprobs, advantages, weights, stats, dlogi
     ``dlogits`` [T, V] of the logits' dtype (may be ``logits``; None: the loss alone)
     grad_scale times its gradient; ``logprobs`` and ``entropy`` the rows' values.
     """
-    index = _device_index(logits, "logits")
-    _on_device(index, {"targets": targets, "old_logprobs": old_logprobs, "advantages": advantages, "weights": weights,
-                       "stats": stats, "dlogits": dlogits, "logprobs": logprobs, "entropy": entropy,
-                       "ref_logprobs": ref_logprobs}, ("targets", "stats"))
+    index = logits.get_device()
+    if _apart(index, (logits, dlogits), (targets, old_logprobs, advantages, weights, stats, logprobs, entropy, ref_logprobs)):
+        _refuse(index, {"logits": logits, "dlogits": dlogits},
+                {"targets": targets, "old_logprobs": old_logprobs, "advantages": advantages, "weights": weights,
+                 "stats": stats, "logprobs": logprobs, "entropy": entropy, "ref_logprobs": ref_logprobs})
     pr = _logits_problem(logits, targets, temperature)
-    _rows((("old_logprobs", old_logprobs), ("advantages", advantages), ("weights", weights), ("logprobs", logprobs),
-           ("entropy", entropy), ("ref_logprobs", ref_logprobs)), pr.num_tokens)
-    if stats.shape != (8,) or stats.dtype != _FLOAT32:
+    _rows(pr.num_tokens, (old_logprobs, advantages, weights, logprobs, entropy, ref_logprobs))
+    if stats.shape != (8,) or stats.dtype is not _FLOAT32:
         raise ValueError("stats must be float32 [8]")
     step = 0
     if dlogits is not None:
-        if dlogits.shape != logits.shape or dlogits.dtype != logits.dtype or (pr.vocab > 1 and dlogits.stride(1) != 1):
-            raise ValueError("dlogits must have the logits' shape and dtype, with contiguous rows")
+        if dlogits.shape != logits.shape or dlogits.dtype is not logits.dtype:
+            raise ValueError("dlogits must have the logits' shape and dtype")
         step = _row_step(dlogits, "dlogits")
-    op = PolicyOptions(clip_low, clip_high, dual_clip, kl_coef, entropy_coef, grad_scale, step)
     _launch(_lib.pdaops_policy_loss, index, stream, logits.data_ptr(), targets.data_ptr(), old_logprobs.data_ptr(),
             _ptr(ref_logprobs), advantages.data_ptr(), weights.data_ptr(), stats.data_ptr(), _ptr(dlogits), _ptr(logprobs),
-            _ptr(entropy), pr, op)
+            _ptr(entropy), pr,
+            PolicyOptions(clip_low, clip_high, dual_clip, kl_coef, entropy_coef, grad_scale, step))
     return stats
 
 

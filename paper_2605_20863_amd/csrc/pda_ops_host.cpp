@@ -251,7 +251,8 @@ int check_logits(const pdaops_logits_problem* pr, pda::LogitsArgs* a) {
   return PDA_OK;
 }
 
-int vectors_of(const pda::LogitsArgs& a) { return a.bf16 ? (a.V + 7) / 8 : (a.V + 3) / 4; }
+// Whole 16-byte vectors of a row.
+int vectors_of(const pda::LogitsArgs& a) { return a.bf16 ? a.V / 8 : a.V / 4; }
 
 // Parts per row: enough workgroups for the compute units, of at least 512 vectors
 // (two for each thread) each.
@@ -263,7 +264,9 @@ void split_rows(pda::LogitsArgs* a) {
   if (s > pda::kMaxSplits) s = pda::kMaxSplits;
   if (s < 1) s = 1;
   a->chunk = (int32_t)((v + s - 1) / s);
+  if (a->chunk < 1) a->chunk = 1;
   a->splits = (int32_t)((v + a->chunk - 1) / a->chunk);
+  if (a->splits < 1) a->splits = 1;
 }
 
 int logprobs_run(const void* logits, const void* targets, float* logprobs, float* entropy,

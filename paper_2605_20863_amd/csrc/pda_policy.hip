@@ -27,7 +27,6 @@ constexpr float kLowest = -3.402823466e38f;
 constexpr float kFar = -1e25f;  // bound on differences in products with a zero: its exponential is 0
 constexpr float kClamp = 20.f;  // bound on log ratios
 constexpr int kPartThreads = 256;
-constexpr int kUnroll = 8;      // 16-byte loads of a thread in flight
 
 // A row's address has the alignment of its elements only.
 typedef u32x4 __attribute__((aligned(2))) u32x4_any;
@@ -59,30 +58,14 @@ __device__ __forceinline__ float load1(const T* p) {
   else return *p;
 }
 
-// Vector i of a row of V elements (-inf past its end).
+// Vector i of a row: elements i * kPer .. all of them in the row.
 template <typename T>
-__device__ __forceinline__ u32x4 load_vec(const T* row, int i, int V) {
-  const int at = i * kPer<T>;
-  if (at + kPer<T> <= V) return *reinterpret_cast<const u32x4_any*>(row + at);
-  u32x4 v = nothing<T>();
-  if (at < V) {
-#pragma unroll
-    for (int e = 0; e < kPer<T>; ++e) {
-      if (at + e >= V) continue;
-      if constexpr (sizeof(T) == 2) {
-        const uint32_t x = row[at + e];
-        v[e / 2] = e & 1 ? (v[e / 2] & 0xFFFFu) | x << 16 : (v[e / 2] & 0xFFFF0000u) | x;
-      } else {
-        v[e] = as_u32(row[at + e]);
-      }
-    }
-  }
-  return v;
+__device__ __forceinline__ u32x4 load_vec(const T* row, int i) {
+  return *reinterpret_cast<const u32x4_any*>(row + (int64_t)i * kPer<T>);
 }
 
 template <typename T>
-__device__ __forceinline__ void store_vec(T* row, int i, int V, const float (&y)[kPer<T>]) {
-  const int at = i * kPer<T>;
+__device__ __forceinline__ void store_vec(T* row, int i, const float (&y)[kPer<T>]) {
   u32x4 v;
   if constexpr (sizeof(T) == 2) {
 #pragma unroll
@@ -91,16 +74,7 @@ __device__ __forceinline__ void store_vec(T* row, int i, int V, const float (&y)
 #pragma unroll
     for (int e = 0; e < 4; ++e) v[e] = as_u32(y[e]);
   }
-  if (at + kPer<T> <= V) {
-    *reinterpret_cast<u32x4_any*>(row + at) = v;
-  } else {
-#pragma unroll
-    for (int e = 0; e < kPer<T>; ++e) {
-      if (at + e >= V) continue;
-      if constexpr (sizeof(T) == 2) row[at + e] = (T)(v[e / 2] >> (16 * (e & 1)));
-      else row[at + e] = y[e];
-    }
-  }
+  *reinterpret_cast<u32x4_any*>(row + (int64_t)i * kPer<T>) = v;
 }
 
 template <typename T>
@@ -150,9 +124,27 @@ __device__ __forceinline__ void add(Soft& x, u32x4 (&v)[N], float c) {
     }
 }
 
-__device__ __forceinline__ Soft wave_merge(Soft x, float c) {
+// Adds one element.
+__device__ __forceinline__ void add1(Soft& x, float l, float c) {
+  const float m = fmaxf(x.m, l);
+  x = rebase(x, m, c);
+  const float d = l - m, p = __builtin_amdgcn_exp2f(d * c);
+  x.s += p;
+  x.u = fmaf(p, fmaxf(d, kFar), x.u);
+}
+
+// The element past a row's whole vectors that is thread `threadIdx.x`'s, -1 if none is.
+template <typename T>
+__device__ __forceinline__ int tail_of(int V) {
+  const int at = V / kPer<T> * kPer<T> + (int)threadIdx.x;
+  return (int)threadIdx.x < kPer<T> && at < V ? at : -1;
+}
+
+// Over the aligned group of N lanes, in each of them.
+template <int N>
+__device__ __forceinline__ Soft lanes_merge(Soft x, float c) {
 #pragma unroll
-  for (int o = 1; o < 64; o *= 2)
+  for (int o = 1; o < N; o *= 2)
     x = merge(x, Soft{__shfl_xor(x.m, o, 64), __shfl_xor(x.s, o, 64), __shfl_xor(x.u, o, 64)}, c);
   return x;
 }
@@ -160,15 +152,12 @@ __device__ __forceinline__ Soft wave_merge(Soft x, float c) {
 // Over the workgroup, in every thread (and a barrier for all of them).
 template <int NT>
 __device__ __forceinline__ Soft group_merge(Soft x, float c) {
-  __shared__ Soft parts[NT / 64];
-  x = wave_merge(x, c);
-  if constexpr (NT == 64) return x;
+  constexpr int W = NT / 64;
+  __shared__ Soft parts[W];
+  x = lanes_merge<64>(x, c);
   if ((threadIdx.x & 63) == 0) parts[threadIdx.x >> 6] = x;
   __syncthreads();
-  x = parts[0];
-#pragma unroll
-  for (int w = 1; w < NT / 64; ++w) x = merge(x, parts[w], c);
-  return x;
+  return lanes_merge<W>(parts[threadIdx.x % W], c);
 }
 
 // Row t's target, or -1 for a row that takes no part.
@@ -253,17 +242,20 @@ __device__ __forceinline__ float grad_of(const Grad& d, float l) {
 
 // ------------------------------------------------------------- parts of rows
 
-// Sums of vectors first .. end - 1 of a row, by the workgroup's threads.
-template <typename T>
-__device__ __forceinline__ Soft sum_vectors(const T* row, int first, int end, int V, float c) {
+// Sums of vectors first .. end - 1 of a row, by the workgroup's threads; U
+// vectors of a thread at a time.
+template <typename T, int U>
+__device__ __forceinline__ Soft sum_vectors(const T* row, int first, int end, float c) {
   Soft x = none();
-  for (int i = first + (int)threadIdx.x; i < end; i += kPartThreads * kUnroll) {
-    u32x4 v[kUnroll];
+  int i = first + (int)threadIdx.x;
+  for (; i + (U - 1) * kPartThreads < end; i += kPartThreads * U) {
+    u32x4 v[U];
 #pragma unroll
-    for (int n = 0; n < kUnroll; ++n) {
-      const int at = i + n * kPartThreads;
-      v[n] = at < end ? load_vec(row, at, V) : nothing<T>();
-    }
+    for (int n = 0; n < U; ++n) v[n] = load_vec(row, i + n * kPartThreads);
+    add<T>(x, v, c);
+  }
+  for (; i < end; i += kPartThreads) {
+    u32x4 v[1] = {load_vec(row, i)};
     add<T>(x, v, c);
   }
   return x;
@@ -271,7 +263,7 @@ __device__ __forceinline__ Soft sum_vectors(const T* row, int first, int end, in
 
 // Workgroup (row, part). A whole row's log-probability and entropy are written;
 // of a part, or for policy_part_kernel, the sums.
-template <typename T>
+template <typename T, int U>
 __global__ __launch_bounds__(kPartThreads) void sums_kernel(LogitsArgs a) {
   const int t = (int)(blockIdx.x / (uint32_t)a.splits), p = (int)(blockIdx.x - (uint32_t)t * a.splits);
   const int y = target_of(a, t);
@@ -284,9 +276,11 @@ __global__ __launch_bounds__(kPartThreads) void sums_kernel(LogitsArgs a) {
     return;
   }
   const T* row = static_cast<const T*>(a.logits) + (int64_t)t * a.stride;
-  const int vectors = (a.V + kPer<T> - 1) / kPer<T>, first = p * a.chunk, end = min(first + a.chunk, vectors);
+  const int first = p * a.chunk, end = min(first + a.chunk, a.V / kPer<T>), tail = tail_of<T>(a.V);
   const float c = a.inv_temp * kLog2e, ly = load1(row + y);
-  const Soft x = group_merge<kPartThreads>(sum_vectors(row, first, end, a.V, c), c);
+  Soft x = sum_vectors<T, U>(row, first, end, c);
+  if (p == a.splits - 1 && tail >= 0) add1(x, load1(row + tail), c);
+  x = group_merge<kPartThreads>(x, c);
   if (threadIdx.x) return;
   if (!whole) {
     a.part[(int64_t)t * a.splits + p] = float4{x.m, x.s, x.u, ly};
@@ -302,7 +296,7 @@ __device__ __forceinline__ Soft merge_parts(const LogitsArgs& a, int t, float c,
   const int l = (int)(threadIdx.x & 63);
   const float4 q = a.part[(int64_t)t * a.splits + min(l, a.splits - 1)];
   ly = q.w;
-  return wave_merge(l < a.splits ? Soft{q.x, q.y, q.z} : none(), c);
+  return lanes_merge<64>(l < a.splits ? Soft{q.x, q.y, q.z} : none(), c);
 }
 
 // A wave per row.
@@ -322,10 +316,19 @@ __global__ __launch_bounds__(kPartThreads) void finish_kernel(LogitsArgs a) {
   }
 }
 
+// Zeros in vectors first .. end - 1, and past a row's last one.
 template <typename T>
 __device__ __forceinline__ void zero_vectors(T* out, int first, int end, int V) {
   const float z[kPer<T>] = {};
-  for (int i = first + (int)threadIdx.x; i < end; i += (int)blockDim.x) store_vec(out, i, V, z);
+  for (int i = first + (int)threadIdx.x; i < end; i += (int)blockDim.x) store_vec(out, i, z);
+  const int tail = tail_of<T>(V);
+  if (end == V / kPer<T> && tail >= 0) store1(out + tail, 0.f);
+}
+
+// The target's gradient, by the thread that wrote the others around it.
+template <typename T>
+__device__ __forceinline__ void store_target(T* out, int y, float ly, const Grad& d) {
+  store1(out + y, grad_of(d, ly) + d.at_y);
 }
 
 // What thread 0 of a row writes beside the gradient.
@@ -340,7 +343,7 @@ template <typename T>
 __global__ __launch_bounds__(kPartThreads) void policy_part_kernel(LogitsArgs a) {
   const int t = (int)(blockIdx.x / (uint32_t)a.splits), p = (int)(blockIdx.x - (uint32_t)t * a.splits);
   const int y = target_of(a, t);
-  const int vectors = (a.V + kPer<T> - 1) / kPer<T>, first = p * a.chunk, end = min(first + a.chunk, vectors);
+  const int first = p * a.chunk, end = min(first + a.chunk, a.V / kPer<T>);
   T* out = static_cast<T*>(a.dlogits) + (int64_t)t * a.d_stride;
   float terms[kTerms] = {};
   if (y < 0) {
@@ -362,12 +365,17 @@ __global__ __launch_bounds__(kPartThreads) void policy_part_kernel(LogitsArgs a)
     return;
   }
   for (int i = first + (int)threadIdx.x; i < end; i += kPartThreads) {
-    const u32x4 v = load_vec(row, i, a.V);
+    const u32x4 v = load_vec(row, i);
     float o[kPer<T>];
 #pragma unroll
     for (int e = 0; e < kPer<T>; ++e) o[e] = grad_of(d, element<T>(v, e));
-    store_vec(out, i, a.V, o);
-    if (i == y / kPer<T>) store1(out + y, grad_of(d, ly) + d.at_y);
+    store_vec(out, i, o);
+    if (i == y / kPer<T>) store_target(out, y, ly, d);
+  }
+  const int tail = tail_of<T>(a.V);
+  if (p == a.splits - 1 && tail >= 0) {
+    store1(out + tail, grad_of(d, load1(row + tail)));
+    if (tail == y) store_target(out, y, ly, d);
   }
 }
 
@@ -377,8 +385,7 @@ __global__ __launch_bounds__(kPartThreads) void policy_part_kernel(LogitsArgs a)
 // sums and the gradient: one read and one write of the row.
 template <typename T, int NT, int N>
 __global__ __launch_bounds__(NT) void policy_row_kernel(LogitsArgs a) {
-  const int t = (int)blockIdx.x, y = target_of(a, t);
-  const int vectors = (a.V + kPer<T> - 1) / kPer<T>;
+  const int t = (int)blockIdx.x, y = target_of(a, t), vectors = a.V / kPer<T>;
   T* out = static_cast<T*>(a.dlogits) + (int64_t)t * a.d_stride;
   float terms[kTerms] = {};
   if (y < 0) {
@@ -387,15 +394,18 @@ __global__ __launch_bounds__(NT) void policy_row_kernel(LogitsArgs a) {
     return;
   }
   const T* row = static_cast<const T*>(a.logits) + (int64_t)t * a.stride;
+  const int tail = tail_of<T>(a.V);
   const float c = a.inv_temp * kLog2e, ly = load1(row + y), w = a.weight[t];
   u32x4 v[N];
 #pragma unroll
   for (int n = 0; n < N; ++n) {
     const int i = (int)threadIdx.x + n * NT;
-    v[n] = i < vectors ? load_vec(row, i, a.V) : nothing<T>();
+    v[n] = i < vectors ? load_vec(row, i) : nothing<T>();
   }
+  const float lt = tail >= 0 ? load1(row + tail) : -__builtin_huge_valf();
   Soft x = none();
   add<T>(x, v, c);
+  add1(x, lt, c);
   x = group_merge<NT>(x, c);
   const RowStats r = row_stats(a, x, ly);
   const float g = policy_terms(a, t, r, w, terms);
@@ -414,8 +424,12 @@ __global__ __launch_bounds__(NT) void policy_row_kernel(LogitsArgs a) {
     float o[kPer<T>];
 #pragma unroll
     for (int e = 0; e < kPer<T>; ++e) o[e] = grad_of(d, element<T>(v[n], e));
-    store_vec(out, i, a.V, o);
-    if (i == y / kPer<T>) store1(out + y, grad_of(d, ly) + d.at_y);
+    store_vec(out, i, o);
+    if (i == y / kPer<T>) store_target(out, y, ly, d);
+  }
+  if (tail >= 0) {
+    store1(out + tail, grad_of(d, lt));
+    if (tail == y) store_target(out, y, ly, d);
   }
 }
 
@@ -424,7 +438,16 @@ __global__ __launch_bounds__(1024) void stats_kernel(LogitsArgs a) {
   __shared__ double sums[1024 / kTerms][kTerms];
   const int k = (int)threadIdx.x % kTerms, r = (int)threadIdx.x / kTerms;
   double x = 0.;
-  for (int t = r; t < a.T; t += 1024 / kTerms) x += (double)a.terms[(int64_t)t * kTerms + k];
+  int t = r;
+  constexpr int step = 1024 / kTerms, U = 8;  // eight rows' terms of a thread in flight
+  for (; t + (U - 1) * step < a.T; t += U * step) {
+    float v[U];
+#pragma unroll
+    for (int i = 0; i < U; ++i) v[i] = a.terms[(int64_t)(t + i * step) * kTerms + k];
+#pragma unroll
+    for (int i = 0; i < U; ++i) x += (double)v[i];
+  }
+  for (; t < a.T; t += step) x += (double)a.terms[(int64_t)t * kTerms + k];
   sums[r][k] = x;
   __syncthreads();
   for (int n = 1024 / kTerms / 2; n > 0; n /= 2) {
@@ -440,9 +463,17 @@ hipError_t launch(const void* kernel, int64_t wgs, int threads, const LogitsArgs
   return hipLaunchKernel(kernel, dim3((unsigned)wgs), dim3((unsigned)threads), params, 0, s);
 }
 
+// Eight 16-byte loads of a thread in flight; four where a part has no more for it.
+template <typename T>
+hipError_t sums_for(const LogitsArgs& a, hipStream_t s) {
+  const void* k = a.chunk < 8 * kPartThreads ? reinterpret_cast<const void*>(&sums_kernel<T, 4>)
+                                             : reinterpret_cast<const void*>(&sums_kernel<T, 8>);
+  return launch(k, (int64_t)a.T * a.splits, kPartThreads, a, s);
+}
+
 template <typename T>
 hipError_t logprobs_for(const LogitsArgs& a, hipStream_t s) {
-  hipError_t e = launch(reinterpret_cast<const void*>(&sums_kernel<T>), (int64_t)a.T * a.splits, kPartThreads, a, s);
+  hipError_t e = sums_for<T>(a, s);
   if (e != hipSuccess || a.splits == 1) return e;
   constexpr int rows = kPartThreads / 64;
   return launch(reinterpret_cast<const void*>(&finish_kernel), (a.T + rows - 1) / rows, kPartThreads, a, s);
@@ -458,10 +489,10 @@ hipError_t policy_for(const LogitsArgs& a, hipStream_t s) {
   hipError_t e = hipSuccess;
   if (a.splits) {
     const int64_t wgs = (int64_t)a.T * a.splits;
-    e = launch(reinterpret_cast<const void*>(&sums_kernel<T>), wgs, kPartThreads, a, s);
+    e = sums_for<T>(a, s);
     if (e == hipSuccess) e = launch(reinterpret_cast<const void*>(&policy_part_kernel<T>), wgs, kPartThreads, a, s);
   } else if (a.T) {
-    const int v = (a.V + kPer<T> - 1) / kPer<T>;
+    const int v = a.V / kPer<T>;
     e = v <= 256 * 4 ? rows_for<T, 256, 4>(a, s)
         : v <= 256 * 8 ? rows_for<T, 256, 8>(a, s)
         : v <= 256 * 16 ? rows_for<T, 256, 16>(a, s)

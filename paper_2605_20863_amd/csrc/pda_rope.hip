@@ -274,11 +274,24 @@ __device__ __forceinline__ uint32_t enc4(const float (&z)[4]) {
   const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
   return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], lo, true);
 }
-__device__ __forceinline__ uint32_t reencode4(uint32_t w, float old, float s) {
-  const float z[4] = {__fdiv_rn(__builtin_amdgcn_cvt_f32_fp8((int)w, 0) * old, s),
-                      __fdiv_rn(__builtin_amdgcn_cvt_f32_fp8((int)w, 1) * old, s),
-                      __fdiv_rn(__builtin_amdgcn_cvt_f32_fp8((int)w, 2) * old, s),
-                      __fdiv_rn(__builtin_amdgcn_cvt_f32_fp8((int)w, 3) * old, s)};
+// Correctly rounded x / s for many x: with y the rounded reciprocal, q = x y and
+// the exact remainder r = x - q s, the quotient is q + r y rounded once
+// (Markstein). Where the remainder could leave float32's range the division is
+// made as such.
+struct Div {
+  float s, y;
+  bool plain;
+};
+__device__ __forceinline__ Div make_div(float s) { return Div{s, 1.f / s, s < 0x1p-90f || s > 0x1p90f}; }
+__device__ __forceinline__ float quotient(float x, const Div& d) {
+  if (d.plain) return __fdiv_rn(x, d.s);
+  const float q = x * d.y, r = fmaf(-q, d.s, x);
+  return r == 0.f ? q : fmaf(r, d.y, q);  // q as it is keeps the sign of a zero
+}
+__device__ __forceinline__ uint32_t reencode4(uint32_t w, float old, const Div& d) {
+  const float z[4] = {
+      quotient(__builtin_amdgcn_cvt_f32_fp8((int)w, 0) * old, d), quotient(__builtin_amdgcn_cvt_f32_fp8((int)w, 1) * old, d),
+      quotient(__builtin_amdgcn_cvt_f32_fp8((int)w, 2) * old, d), quotient(__builtin_amdgcn_cvt_f32_fp8((int)w, 3) * old, d)};
   return enc4(z);
 }
 // bytes first .. end - 1 of a 16-byte piece from y, the others from x
@@ -343,10 +356,15 @@ __device__ __forceinline__ void kv_tile(const RopeArgs& a, uint32_t item, uint32
   const void* in = is_v ? a.v : a.k;
   const int64_t in_stride = is_v ? a.v_stride : a.k_stride;
   // K: rows of neighbouring slots; V: a lane gets both slots of a pair
+  // whether the wave's rows of iteration `it` hold a new slot
+  auto any = [&](int it) {
+    return is_v ? 2 * RPI * (it >> 1) < e && 2 * RPI * ((it >> 1) + 1) > o : RPI * it < e && RPI * (it + 1) > o;
+  };
   auto slot_of = [&](int it) { return is_v ? 2 * (r + RPI * (it >> 1)) + (it & 1) : RPI * it + r; };
   Raw<T> raw[IT];
 #pragma unroll
   for (int it = 0; it < IT; ++it) {
+    if (!any(it)) continue;
     const int s = min(max(slot_of(it), o), e - 1);
     raw[it] = load8<T>(in, (t0 + s) * in_stride + (int64_t)h * D + d0);
   }
@@ -366,7 +384,7 @@ __device__ __forceinline__ void kv_tile(const RopeArgs& a, uint32_t item, uint32
     if (a.wq) load_weight<D>(a.wk, a.w_bf16, w);
 #pragma unroll
     for (int it = 0; it < IT; ++it) {
-      if (RPI * it >= e || RPI * (it + 1) <= o) continue;
+      if (!any(it)) continue;
       const int s = min(max(slot_of(it), o), e - 1);
       const int pos = clamp_position(a, a.positions ? a.positions[t0 + s] : 16 * blk + s);
       norm_turn<D>(a, tn, load_angles<D>(a, tn, pos), w, y[it]);
@@ -378,6 +396,7 @@ __device__ __forceinline__ void kv_tile(const RopeArgs& a, uint32_t item, uint32
     float m = 0.f;
 #pragma unroll
     for (int it = 0; it < IT; ++it) {
+      if (!any(it)) continue;
       const int s = slot_of(it);
 #pragma unroll
       for (int i = 0; i < 8; ++i) m = s >= o && s < e ? fmaxf(m, fabsf(y[it][i])) : m;
@@ -385,6 +404,7 @@ __device__ __forceinline__ void kv_tile(const RopeArgs& a, uint32_t item, uint32
     raised = raise_scale(o, old, wave_max_f(m), scale);
     if (lane_id() == 0) *sp = scale;
   }
+  const Div div = make_div(scale);
   if (!is_v) {
 #pragma unroll
     for (int it = 0; it < IT; ++it) {
@@ -394,7 +414,7 @@ __device__ __forceinline__ void kv_tile(const RopeArgs& a, uint32_t item, uint32
       if constexpr (KV == KvType::FP8) {
         float z[2][4];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) z[i / 4][i % 4] = __fdiv_rn(y[it][i], scale);
+        for (int i = 0; i < 8; ++i) z[i / 4][i % 4] = quotient(y[it][i], div);
         *reinterpret_cast<u32x2*>(static_cast<uint8_t*>(a.k_cache) + at) = u32x2{enc4(z[0]), enc4(z[1])};
       } else {
         store8(a.k_cache, at, KV == KvType::BF16, y[it]);
@@ -406,7 +426,7 @@ __device__ __forceinline__ void kv_tile(const RopeArgs& a, uint32_t item, uint32
         const u32x4 x = pt[i];
         u32x4 n;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) n[w] = reencode4(x[w], old, scale);
+        for (int w = 0; w < 4; ++w) n[w] = reencode4(x[w], old, div);
         pt[i] = n;
       }
     }
@@ -417,6 +437,7 @@ __device__ __forceinline__ void kv_tile(const RopeArgs& a, uint32_t item, uint32
   auto dim_at = [&](int d) { return d * DW + (d >> 3) * 4; };
 #pragma unroll
   for (int it = 0; it < IT; it += 2) {
+    if (!any(it)) continue;
     const int s = slot_of(it);  // an even one
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -427,7 +448,7 @@ __device__ __forceinline__ void kv_tile(const RopeArgs& a, uint32_t item, uint32
       } else if constexpr (KV == KvType::BF16) {
         q[s / 2] = pack_bf16(y[it][i], y[it + 1][i]);
       } else {
-        const float z[4] = {__fdiv_rn(y[it][i], scale), __fdiv_rn(y[it + 1][i], scale), 0.f, 0.f};
+        const float z[4] = {quotient(y[it][i], div), quotient(y[it + 1][i], div), 0.f, 0.f};
         reinterpret_cast<uint16_t*>(q)[s / 2] = (uint16_t)enc4(z);
       }
     }
@@ -456,7 +477,7 @@ __device__ __forceinline__ void kv_tile(const RopeArgs& a, uint32_t item, uint32
         if (raised) {
           u32x4 n;
 #pragma unroll
-          for (int w = 0; w < 4; ++w) n[w] = reencode4(was[w], old, scale);
+          for (int w = 0; w < 4; ++w) n[w] = reencode4(was[w], old, div);
           was = merge16(was, n, 0, o);
         }
         *q = merge16(was, x, o, e);
@@ -603,19 +624,31 @@ __global__ __launch_bounds__(64 * kWaves) void rope_backward_kernel(RopeArgs a) 
   }
 }
 
-// Sums the workgroups' parts in a fixed order: workgroup (16 dims of q's or k's
-// weights), 16 threads of it per 16 dims.
-constexpr int kSumRows = 16;
+// Sums the workgroups' parts in a fixed order: a workgroup per 16 dims of q's or
+// k's weights, a row of parts for each 16 of its threads, four loads of a thread
+// in flight.
+constexpr int kSumRows = 64;
 __global__ __launch_bounds__(16 * kSumRows) void rope_weight_grad_kernel(RopeArgs a) {
   __shared__ double sums[kSumRows][16];
   const int i = (int)threadIdx.x % 16, r = (int)threadIdx.x / 16, at = (int)blockIdx.x * 16 + i;
+  const float* part = a.dw_part + at;
+  const int64_t row = 2 * a.D;
   double x = 0.;
-  for (int g = r; g < a.wgs; g += kSumRows) x += (double)a.dw_part[(int64_t)g * 2 * a.D + at];
+  int g = r;
+  for (; g + 3 * kSumRows < a.wgs; g += 4 * kSumRows) {
+    float v[4];
+#pragma unroll
+    for (int n = 0; n < 4; ++n) v[n] = part[(g + n * kSumRows) * row];
+    x += ((double)v[0] + (double)v[1]) + ((double)v[2] + (double)v[3]);
+  }
+  for (; g < a.wgs; g += kSumRows) x += (double)part[g * row];
   sums[r][i] = x;
   __syncthreads();
-  if (r) return;
-  for (int k = 1; k < kSumRows; ++k) x += sums[k][i];
-  (at < a.D ? a.dwq : a.dwk)[at % a.D] = (float)x;
+  for (int n = kSumRows / 2; n > 0; n /= 2) {
+    if (r < n) sums[r][i] += sums[r + n][i];
+    __syncthreads();
+  }
+  if (r == 0) (at < a.D ? a.dwq : a.dwk)[at % a.D] = (float)sums[0][i];
 }
 
 // ------------------------------------------------------------- launches
