@@ -44,6 +44,16 @@ __device__ __forceinline__ float group_sum(float x) {
   return x;
 }
 
+// Their largest.
+template <int N>
+__device__ __forceinline__ float group_max(float x) {
+  x = fmaxf(x, dpp<kDppXor1>(x));
+  x = fmaxf(x, dpp<kDppXor2>(x));
+  x = fmaxf(x, dpp<kDppHalfMirror>(x));
+  if constexpr (N == 16) x = fmaxf(x, dpp<kDppMirror>(x));
+  return x;
+}
+
 __device__ __forceinline__ float wave_max_f(float x) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) x = fmaxf(x, __shfl_xor(x, o, 64));

@@ -23,6 +23,7 @@ namespace pda {
 namespace {
 
 constexpr int kWaves = 4;  // waves per workgroup
+constexpr int kManyRows = 8, kFewRows = 2;  // rows of a lane group that a wave takes
 constexpr float kE4M3Max = 448.f;
 constexpr float kMinScale = 0x1p-126f;
 
@@ -46,9 +47,15 @@ template <>
 struct Raw<float> {
   u32x4 a, b;
 };
-template <typename T>
+// STREAM: past the caches, for calls whose tensors are larger than they are (see
+// `few`).
+template <bool STREAM, typename T>
 __device__ __forceinline__ Raw<T> load8(const void* base, int64_t at) {
-  return *reinterpret_cast<const Raw<T>*>(static_cast<const T*>(base) + at);
+  const u32x4* p = reinterpret_cast<const u32x4*>(static_cast<const T*>(base) + at);
+  Raw<T> r;
+  r.a = STREAM ? __builtin_nontemporal_load(p) : *p;
+  if constexpr (sizeof(T) == 4) r.b = STREAM ? __builtin_nontemporal_load(p + 1) : p[1];
+  return r;
 }
 __device__ __forceinline__ void unpack(const Raw<uint16_t>& r, float (&x)[8]) {
 #pragma unroll
@@ -66,16 +73,24 @@ __device__ __forceinline__ void unpack(const Raw<float>& r, float (&x)[8]) {
     x[4 + i] = as_f32(w);
   }
 }
+template <bool STREAM>
+__device__ __forceinline__ void put16(void* p, u32x4 v) {
+  if constexpr (STREAM) __builtin_nontemporal_store(v, static_cast<u32x4*>(p));
+  else *static_cast<u32x4*>(p) = v;
+}
+template <bool STREAM>
 __device__ __forceinline__ void store8(void* base, int64_t at, bool bf16, const float (&y)[8]) {
+  u32x4 o[2];
   if (bf16) {
-    u32x4 o;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) o[i] = pack_bf16(y[2 * i], y[2 * i + 1]);
-    *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(base) + at) = o;
+    for (int i = 0; i < 4; ++i) o[0][i] = pack_bf16(y[2 * i], y[2 * i + 1]);
+    put16<STREAM>(static_cast<uint16_t*>(base) + at, o[0]);
   } else {
-    f32x4* p = reinterpret_cast<f32x4*>(static_cast<float*>(base) + at);
-    p[0] = f32x4{y[0], y[1], y[2], y[3]};
-    p[1] = f32x4{y[4], y[5], y[6], y[7]};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) o[i / 4][i % 4] = as_u32(y[i]);
+    float* p = static_cast<float*>(base) + at;
+    put16<STREAM>(p, o[0]);
+    put16<STREAM>(p + 4, o[1]);
   }
 }
 
@@ -174,8 +189,8 @@ __device__ __forceinline__ float inv_rms(const float (&x)[8], float eps) {
 template <int D>
 __device__ __forceinline__ void load_weight(const void* w, bool bf16, float (&o)[8]) {
   const int d0 = 8 * (lane_id() % Row<D>::LPR);
-  if (bf16) unpack(load8<uint16_t>(w, d0), o);
-  else unpack(load8<float>(w, d0), o);
+  if (bf16) unpack(load8<false, uint16_t>(w, d0), o);
+  else unpack(load8<false, float>(w, d0), o);
 }
 
 // Norm (with weights) and rotation of the wave's rows.
@@ -230,7 +245,7 @@ __device__ __forceinline__ Seq sequence(const RopeArgs& a, int b) {
 }
 
 // The rows [row0, rows_end) of token t, heads of q, then (KROWS) of k.
-template <typename T, int D, int NI, bool KROWS, typename P>
+template <typename T, int D, int NI, bool KROWS, bool STREAM, typename P>
 __device__ __forceinline__ void token_rows(const RopeArgs& a, int t, int row0, int rows_end, P position) {
   constexpr int RPI = Row<D>::RPI, LPR = Row<D>::LPR;
   const int r = lane_id() / LPR, d0 = 8 * (lane_id() % LPR);
@@ -240,7 +255,7 @@ __device__ __forceinline__ void token_rows(const RopeArgs& a, int t, int row0, i
     if (row0 + it * RPI >= rows_end) break;
     const int h = min(row0 + it * RPI + r, rows_end - 1);
     const bool k = KROWS && h >= a.Hq;
-    raw[it] = load8<T>(k ? a.k : a.q, (k ? t * a.k_stride + (int64_t)(h - a.Hq) * D : t * a.q_stride + (int64_t)h * D) + d0);
+    raw[it] = load8<STREAM, T>(k ? a.k : a.q, (k ? t * a.k_stride + (int64_t)(h - a.Hq) * D : t * a.q_stride + (int64_t)h * D) + d0);
   }
   float wq[8] = {}, wk[8] = {};
   if (a.wq) load_weight<D>(a.wq, a.w_bf16, wq);
@@ -260,7 +275,7 @@ __device__ __forceinline__ void token_rows(const RopeArgs& a, int t, int row0, i
     for (int i = 0; i < 8; ++i) w[i] = k ? wk[i] : wq[i];
     norm_turn<D>(a, tn, g, w, x);
     if (h < rows_end)
-      store8(k ? a.k_out : a.q_out, (k ? t * a.ko_stride + (int64_t)(h - a.Hq) * D : t * a.qo_stride + (int64_t)h * D) + d0,
+      store8<STREAM>(k ? a.k_out : a.q_out, (k ? t * a.ko_stride + (int64_t)(h - a.Hq) * D : t * a.qo_stride + (int64_t)h * D) + d0,
              a.out_bf16, x);
   }
 }
@@ -325,7 +340,7 @@ constexpr int tile_dwords() {
 }
 
 // One wave: K or V of one KV head in one cache tile, new slots o .. e - 1.
-template <typename T, KvType KV, int D>
+template <typename T, KvType KV, int D, bool STREAM>
 __device__ __forceinline__ void kv_tile(const RopeArgs& a, uint32_t item, uint32_t* lds) {
   constexpr int LPR = Row<D>::LPR, RPI = Row<D>::RPI, IT = 16 / RPI;
   const bool is_v = item & 1;
@@ -366,7 +381,7 @@ __device__ __forceinline__ void kv_tile(const RopeArgs& a, uint32_t item, uint32
   for (int it = 0; it < IT; ++it) {
     if (!any(it)) continue;
     const int s = min(max(slot_of(it), o), e - 1);
-    raw[it] = load8<T>(in, (t0 + s) * in_stride + (int64_t)h * D + d0);
+    raw[it] = load8<STREAM, T>(in, (t0 + s) * in_stride + (int64_t)h * D + d0);
   }
   if ((unsigned)p >= (uint64_t)a.num_blocks) {
     if (lane_id() == 0) atomicOr(a.status, kStatusBadBlock);
@@ -417,7 +432,7 @@ __device__ __forceinline__ void kv_tile(const RopeArgs& a, uint32_t item, uint32
         for (int i = 0; i < 8; ++i) z[i / 4][i % 4] = quotient(y[it][i], div);
         *reinterpret_cast<u32x2*>(static_cast<uint8_t*>(a.k_cache) + at) = u32x2{enc4(z[0]), enc4(z[1])};
       } else {
-        store8(a.k_cache, at, KV == KvType::BF16, y[it]);
+        store8<STREAM>(a.k_cache, at, KV == KvType::BF16, y[it]);
       }
     }
     if (KV == KvType::FP8 && raised) {
@@ -466,7 +481,7 @@ __device__ __forceinline__ void kv_tile(const RopeArgs& a, uint32_t item, uint32
     if constexpr (KV == KvType::FP8) {
       u32x4* q = reinterpret_cast<u32x4*>(vt + 16 * pc);
       if (o == 0 && e == 16) {
-        *q = x;
+        put16<STREAM>(q, x);
       } else if (e - o == 1 && !(raised && o > 0)) {
         uint32_t word = x[0];
 #pragma unroll
@@ -484,7 +499,7 @@ __device__ __forceinline__ void kv_tile(const RopeArgs& a, uint32_t item, uint32
       }
     } else {
       if (first <= 0 && end >= PER) {
-        *reinterpret_cast<u32x4*>(vt + 16 * pc) = x;
+        put16<STREAM>(vt + 16 * pc, x);
       } else {
 #pragma unroll
         for (int s = 0; s < PER; ++s) {
@@ -497,11 +512,122 @@ __device__ __forceinline__ void kv_tile(const RopeArgs& a, uint32_t item, uint32
   }
 }
 
+// One new token per sequence (a decode step): a wave's lane groups each take one
+// KV head's K or V row of a token, so that a step's waves are all on the chip at
+// once; V's elements go straight to their columns. Against a wave per (head, K or V) by
+// kv_tile: 14.4 us for 512 sequences, 64 / 8 heads, fp8; see rope_token_kernel.
+template <typename T, KvType KV, int D>
+__device__ __forceinline__ void kv_token(const RopeArgs& a, uint32_t item) {
+  constexpr int LPR = Row<D>::LPR, RPI = Row<D>::RPI;
+  const bool is_v = item & 1;
+  const int per = (a.Hkv + RPI - 1) / RPI, pair = (int)(item >> 1), b = pair / per, hc = pair - b * per;
+  const int j = lane_id() % LPR, d0 = 8 * j, h = hc * RPI + lane_id() / LPR;
+  const bool live = h < a.Hkv;
+  const int hh = live ? h : a.Hkv - 1;
+  const Raw<T> raw = load8<false, T>(is_v ? a.v : a.k, b * (is_v ? a.v_stride : a.k_stride) + (int64_t)hh * D + d0);
+  const int full = a.seq_lens[b], len = full < 0 ? 0 : full > a.len_cap ? a.len_cap : full;
+  if (len != full && hc == 0 && !is_v && lane_id() == 0) atomicOr(a.status, kStatusLenClamped);
+  const int pos = len - 1;
+  if (pos < 0) return;
+  const int p = a.block_table[(int64_t)b * a.max_blocks + pos / 16], o = pos % 16;
+  float y[8], w[8] = {};
+  Angles g;
+  const Turn tn = make_turn<D>(a);
+  if (!is_v) {
+    if (a.wq) load_weight<D>(a.wk, a.w_bf16, w);
+    g = load_angles<D>(a, tn, clamp_position(a, a.positions ? a.positions[b] : pos));
+  }
+  if ((unsigned)p >= (uint64_t)a.num_blocks) {
+    if (lane_id() == 0) atomicOr(a.status, kStatusBadBlock);
+    return;
+  }
+  const int64_t ct = (int64_t)p * a.Hkv + hh;
+  float* sp = KV == KvType::FP8 ? a.kv_scales + (is_v ? a.num_blocks * a.Hkv : 0) + ct : nullptr;
+  const float old = KV == KvType::FP8 && o > 0 ? *sp : 0.f;
+  unpack(raw, y);
+  if (!is_v) norm_turn<D>(a, tn, g, w, y);
+  if constexpr (KV != KvType::FP8) {
+    if (!live) return;
+    const int64_t tile = ct * 16 * D;
+    if (!is_v) {
+      store8<false>(a.k_cache, tile + (int64_t)o * D + d0, KV == KvType::BF16, y);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int64_t at = tile + (d0 + i) * 16 + o;
+        if constexpr (KV == KvType::F32) static_cast<float*>(a.v_cache)[at] = y[i];
+        else static_cast<uint16_t*>(a.v_cache)[at] = to_bf16(y[i]);
+      }
+    }
+  } else {
+    float m = 0.f, scale;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = fmaxf(m, fabsf(y[i]));
+    const bool raised = raise_scale(o, old, group_max<LPR>(m), scale);
+    if (!live) return;
+    if (j == 0) *sp = scale;
+    const Div div = make_div(scale);
+    float z[2][4];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) z[i / 4][i % 4] = quotient(y[i], div);
+    const u32x2 codes = {enc4(z[0]), enc4(z[1])};
+    uint8_t* tile = static_cast<uint8_t*>(is_v ? a.v_cache : a.k_cache) + ct * 16 * D;
+    if (!is_v) {
+      *reinterpret_cast<u32x2*>(tile + o * D + d0) = codes;
+      if (raised) {
+        for (int i = j; i < o * D / 16; i += LPR) {
+          u32x4* q = reinterpret_cast<u32x4*>(tile) + i;
+          u32x4 x = *q;
+#pragma unroll
+          for (int n = 0; n < 4; ++n) x[n] = reencode4(x[n], old, div);
+          *q = x;
+        }
+      }
+    } else if (!raised || o == 0) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const uint32_t word = codes[i / 4];
+        tile[(d0 + i) * 16 + o] = (uint8_t)(word >> (8 * (i % 4)));
+      }
+    } else {
+      u32x4* q = reinterpret_cast<u32x4*>(tile) + d0;  // a lane's dims, 16 slots each
+      u32x4 x[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = q[i];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const uint32_t word = codes[i / 4], code = (word >> (8 * (i % 4)) & 0xFFu) * 0x01010101u;
+        u32x4 n;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) n[k] = reencode4(x[i][k], old, div);
+        q[i] = merge16(merge16(x[i], n, 0, o), u32x4{code, code, code, code}, o, o + 1);
+      }
+    }
+  }
+}
+
 // One wave: every sequence's offsets.
 __device__ __forceinline__ void check_offsets(const RopeArgs& a) {
   bool ok = true;
   for (int b = lane_id(); b < a.B; b += 64) ok &= sequence(a, b).ok;
   if (!ok) atomicOr(a.status, kStatusBadOffsets);
+}
+
+template <typename T, KvType KV, int D>
+__global__ __launch_bounds__(64 * kWaves) void rope_token_kernel(RopeArgs a) {
+  const uint32_t per = ((uint32_t)a.Hkv + Row<D>::RPI - 1) / Row<D>::RPI, kv_waves = 2u * (uint32_t)a.B * per;
+  const uint32_t kv_wgs = (kv_waves + kWaves - 1) / kWaves;
+  if (blockIdx.x < kv_wgs) {
+    const uint32_t w = blockIdx.x * kWaves + wave_id();
+    if (w < kv_waves) kv_token<T, KV, D>(a, w);
+    return;
+  }
+  const uint32_t w = (blockIdx.x - kv_wgs) * kWaves + wave_id();
+  if (w >= (uint32_t)a.T * (uint32_t)a.chunks) return;
+  const int t = (int)(w / (uint32_t)a.chunks), c = (int)(w - (uint32_t)t * a.chunks);
+  token_rows<T, D, kFewRows, false, false>(a, t, c * a.rows, min(c * a.rows + a.rows, a.Hq), [&]() {
+    return clamp_position(a, a.positions ? a.positions[t] : max(min(a.seq_lens[t], a.len_cap) - 1, 0));
+  });
 }
 
 // Workgroups of KV waves first (their chains are the longer ones), the offsets'
@@ -512,7 +638,7 @@ __global__ __launch_bounds__(64 * kWaves) void rope_append_kernel(RopeArgs a) {
   const uint32_t kv_waves = 2u * (uint32_t)a.tiles * (uint32_t)a.Hkv, kv_wgs = kv_waves / kWaves + 1;
   if (blockIdx.x < kv_wgs) {
     const uint32_t w = blockIdx.x * kWaves + wave_id();
-    if (w < kv_waves) kv_tile<T, KV, D>(a, w, lds[wave_id()]);
+    if (w < kv_waves) kv_tile<T, KV, D, (NI > kFewRows)>(a, w, lds[wave_id()]);
     else if (w == kv_waves && a.q_offsets) check_offsets(a);
     return;
   }
@@ -520,7 +646,7 @@ __global__ __launch_bounds__(64 * kWaves) void rope_append_kernel(RopeArgs a) {
   if (w >= (uint32_t)a.T * (uint32_t)a.chunks) return;
   const int t = (int)(w / (uint32_t)a.chunks), c = (int)(w - (uint32_t)t * a.chunks);
   const int row0 = c * a.rows, end = min(row0 + a.rows, a.Hq);
-  token_rows<T, D, NI, false>(a, t, row0, end, [&]() {
+  token_rows<T, D, NI, false, (NI > kFewRows)>(a, t, row0, end, [&]() {
     int b = a.n ? t / a.n : 0;
     if (a.q_offsets) b = __builtin_amdgcn_readfirstlane(wave_search(a.B, t, [&](int i) { return a.q_offsets[i]; }));
     const Seq s = sequence(a, b);
@@ -537,12 +663,12 @@ __global__ __launch_bounds__(64 * kWaves) void rope_kernel(RopeArgs a) {
   if (w >= (uint32_t)a.T * (uint32_t)a.chunks) return;
   const int t = (int)(w / (uint32_t)a.chunks), c = (int)(w - (uint32_t)t * a.chunks);
   const int row0 = c * a.rows, end = min(row0 + a.rows, a.Hq + a.Hkv);
-  token_rows<T, D, NI, true>(a, t, row0, end, [&]() { return clamp_position(a, a.positions[t]); });
+  token_rows<T, D, NI, true, (NI > kFewRows)>(a, t, row0, end, [&]() { return clamp_position(a, a.positions[t]); });
 }
 
 // Gradient. Every wave takes (token, chunk of rows) pairs in turn and keeps its
 // rows' part of the weights' gradients; a workgroup's go to dw_part.
-template <typename T, int D, int NI>
+template <typename T, int D, int NI, bool STREAM>
 __global__ __launch_bounds__(64 * kWaves) void rope_backward_kernel(RopeArgs a) {
   constexpr int RPI = Row<D>::RPI, LPR = Row<D>::LPR;
   __shared__ float sums[kWaves][2][D];
@@ -566,8 +692,8 @@ __global__ __launch_bounds__(64 * kWaves) void rope_backward_kernel(RopeArgs a) 
       const int h = min(row0 + it * RPI + r, end - 1);
       const bool k = h >= a.Hq;
       const int64_t head = (int64_t)(k ? h - a.Hq : h) * D + d0;
-      rg[it] = load8<T>(k ? a.gk : a.gq, t * (k ? a.gk_stride : a.gq_stride) + head);
-      if (norm) rx[it] = load8<T>(k ? a.k : a.q, t * (k ? a.k_stride : a.q_stride) + head);
+      rg[it] = load8<false, T>(k ? a.gk : a.gq, t * (k ? a.gk_stride : a.gq_stride) + head);
+      if (norm) rx[it] = load8<false, T>(k ? a.k : a.q, t * (k ? a.k_stride : a.q_stride) + head);
     }
     const Angles g = load_angles<D>(a, tn, clamp_position(a, a.positions[t]));
 #pragma unroll
@@ -598,7 +724,7 @@ __global__ __launch_bounds__(64 * kWaves) void rope_backward_kernel(RopeArgs a) 
       }
       if (live) {
         const int64_t head = (int64_t)(k ? h - a.Hq : h) * D + d0;
-        store8(k ? a.dk : a.dq, t * (k ? a.dk_stride : a.dq_stride) + head, a.out_bf16, y);
+        store8<STREAM>(k ? a.dk : a.dq, t * (k ? a.dk_stride : a.dq_stride) + head, a.out_bf16, y);
       }
     }
   }
@@ -653,8 +779,6 @@ __global__ __launch_bounds__(16 * kSumRows) void rope_weight_grad_kernel(RopeArg
 
 // ------------------------------------------------------------- launches
 
-constexpr int kManyRows = 8, kFewRows = 2;  // rows of a lane group that a wave takes
-
 template <typename K>
 hipError_t launch(K kernel, int64_t wgs, const RopeArgs& a, hipStream_t s) {
   if (wgs <= 0) return hipSuccess;
@@ -675,6 +799,12 @@ bool few(const RopeArgs& a, int heads) { return (int64_t)a.T * heads < 65536; }
 
 template <typename T, KvType KV, int D>
 hipError_t append_for(RopeArgs a, hipStream_t s) {
+  if (a.n == 1) {
+    cut(a, a.Hq, kFewRows);
+    constexpr int rpi = Row<D>::RPI;
+    const int64_t kv = (2 * (int64_t)a.B * ((a.Hkv + rpi - 1) / rpi) + kWaves - 1) / kWaves;
+    return launch(&rope_token_kernel<T, KV, D>, kv + ((int64_t)a.T * a.chunks + kWaves - 1) / kWaves, a, s);
+  }
   const bool f = few(a, a.Hq);
   cut(a, a.Hq, f ? kFewRows : kManyRows);
   const int64_t kv = 2 * (int64_t)a.tiles * a.Hkv / kWaves + 1;
@@ -707,7 +837,8 @@ hipError_t backward_for(RopeArgs a, hipStream_t s) {
   cut(a, a.Hq + a.Hkv, kFewRows);
   const int64_t wgs = ((int64_t)a.T * a.chunks + kWaves - 1) / kWaves;
   if (wgs < a.wgs) a.wgs = (int32_t)wgs;
-  hipError_t e = launch(&rope_backward_kernel<T, D, kFewRows>, a.wgs, a, s);
+  hipError_t e = few(a, a.Hq + a.Hkv) ? launch(&rope_backward_kernel<T, D, kFewRows, false>, a.wgs, a, s)
+                                      : launch(&rope_backward_kernel<T, D, kFewRows, true>, a.wgs, a, s);
   if (e != hipSuccess || !a.wq) return e;
   RopeArgs args = a;
   void* params[] = {&args};
