@@ -563,44 +563,52 @@ __device__ __forceinline__ void kv_token(const RopeArgs& a, uint32_t item) {
     float m = 0.f, scale;
 #pragma unroll
     for (int i = 0; i < 8; ++i) m = fmaxf(m, fabsf(y[i]));
-    const bool raised = raise_scale(o, old, group_max<LPR>(m), scale);
-    if (!live) return;
-    if (j == 0) *sp = scale;
+    const bool raised = raise_scale(o, old, group_max<LPR>(m), scale) && o > 0 && live;
     const Div div = make_div(scale);
     float z[2][4];
 #pragma unroll
     for (int i = 0; i < 8; ++i) z[i / 4][i % 4] = quotient(y[i], div);
     const u32x2 codes = {enc4(z[0]), enc4(z[1])};
     uint8_t* tile = static_cast<uint8_t*>(is_v ? a.v_cache : a.k_cache) + ct * 16 * D;
-    if (!is_v) {
-      *reinterpret_cast<u32x2*>(tile + o * D + d0) = codes;
-      if (raised) {
-        for (int i = j; i < o * D / 16; i += LPR) {
-          u32x4* q = reinterpret_cast<u32x4*>(tile) + i;
-          u32x4 x = *q;
-#pragma unroll
-          for (int n = 0; n < 4; ++n) x[n] = reencode4(x[n], old, div);
-          *q = x;
-        }
-      }
-    } else if (!raised || o == 0) {
+    if (live && j == 0) *sp = scale;
+    if (live && !is_v) *reinterpret_cast<u32x2*>(tile + o * D + d0) = codes;
+    if (live && is_v && !raised) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const uint32_t word = codes[i / 4];
         tile[(d0 + i) * 16 + o] = (uint8_t)(word >> (8 * (i % 4)));
       }
-    } else {
-      u32x4* q = reinterpret_cast<u32x4*>(tile) + d0;  // a lane's dims, 16 slots each
-      u32x4 x[8];
+    }
+    // tiles under raised scales: each by the whole wave, all of their loads first
+    const uint64_t again = __ballot(raised);
+    if (!again) return;
+    constexpr int N = D / 64;  // 16-byte pieces of a tile per lane
+    uint8_t* first = static_cast<uint8_t*>(is_v ? a.v_cache : a.k_cache) + ((int64_t)p * a.Hkv + hc * RPI) * 16 * D;
+    const int pieces = is_v ? D : o * (D / 16);  // earlier tokens' (K), every dim's (V)
+    u32x4 x[RPI][N];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = q[i];
+    for (int r = 0; r < RPI; ++r)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const uint32_t word = codes[i / 4], code = (word >> (8 * (i % 4)) & 0xFFu) * 0x01010101u;
-        u32x4 n;
+      for (int n = 0; n < N; ++n)
+        if ((again >> (r * LPR) & 1) && lane_id() + 64 * n < pieces)
+          x[r][n] = *reinterpret_cast<const u32x4*>(first + r * 16 * D + 16 * (lane_id() + 64 * n));
 #pragma unroll
-        for (int k = 0; k < 4; ++k) n[k] = reencode4(x[i][k], old, div);
-        q[i] = merge16(merge16(x[i], n, 0, o), u32x4{code, code, code, code}, o, o + 1);
+    for (int r = 0; r < RPI; ++r) {
+      if (!(again >> (r * LPR) & 1)) continue;
+      const float was = __shfl(old, r * LPR, 64);
+      const Div dr = make_div(__shfl(scale, r * LPR, 64));
+#pragma unroll
+      for (int n = 0; n < N; ++n) {
+        const int pc = lane_id() + 64 * n;
+        u32x4 q;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) q[k] = reencode4(x[r][n][k], was, dr);
+        if (is_v) {  // the piece is dim pc: with its new code, which lane pc / 8 of the row holds
+          const uint32_t c0 = __shfl(codes[0], r * LPR + pc / 8, 64), c1 = __shfl(codes[1], r * LPR + pc / 8, 64);
+          const uint32_t code = ((pc & 4 ? c1 : c0) >> (8 * (pc & 3)) & 0xFFu) * 0x01010101u;
+          q = merge16(merge16(x[r][n], q, 0, o), u32x4{code, code, code, code}, o, o + 1);
+        }
+        if (pc < pieces) *reinterpret_cast<u32x4*>(first + r * 16 * D + 16 * pc) = q;
       }
     }
   }
