@@ -255,7 +255,9 @@ int check_logits(const pdaops_logits_problem* pr, pda::LogitsArgs* a) {
 int vectors_of(const pda::LogitsArgs& a) { return a.bf16 ? a.V / 8 : a.V / 4; }
 
 // Parts per row: enough workgroups for the compute units, of at least 512 vectors
-// (two for each thread) each.
+// (two for each thread) each. Half or twice as many workgroups, or least vectors, are
+// within 10% on every size tried (1 to 3,000 rows of 8,000 to 150,000 words) but for
+// rows of 8,000 words, which 256 vectors a part cut in two: 5.3 - 9.3 us per call, 4.2 - 7.1 whole.
 void split_rows(pda::LogitsArgs* a) {
   constexpr int64_t kWgs = 1024, kLeast = 512;
   const int64_t v = vectors_of(*a);
@@ -321,12 +323,14 @@ int policy_run(const void* logits, const void* targets, const float* old_logprob
                        {dlogits, e, "dlogits", false}, {logprobs, 4, "logprobs", false}, {entropy, 4, "entropy", false}});
   if (rc != PDA_OK) return rc;
   if (a.T > kMaxWaves / 64) return host_fail(PDA_EINVAL, "num_tokens = %d is too much for one call", a.T);
-  // Rows in registers where they fit and there are enough of them to keep the
-  // compute units busy; otherwise in parts, read twice.
-  constexpr int kManyRows = 192;
-  if (a.T < kManyRows || vectors_of(a) > pda::kRowThreads * pda::kRowVectors) {
-    if (any) split_rows(&a);
-  }
+  // Rows in registers where they fit and either there are enough of them for the
+  // compute units or they are short; otherwise in parts, read twice (us per call in
+  // a HIP graph, registers / parts; bf16 unless said: 128 rows of 131,072 words 24.1 / 20.9, 192 26.0 /
+  // 33.3, 512 58 / 68; 64 of 32,000 11.6 / 10.6, 128 12.4 / 12.6; f32, 64 of 50,001 14.6 / 12.5, 128 15.5 / 16.1; 1 of 16,000
+  // 7.5 / 9.2, 512 13 / 17).
+  constexpr int kManyRows = 128, kShortVectors = 2048;
+  const int v = vectors_of(a);
+  if (any && ((a.T < kManyRows && v > kShortVectors) || v > pda::kRowThreads * pda::kRowVectors)) split_rows(&a);
   const int64_t terms = ((int64_t)a.T * pda::kTerms * 4 + 255) / 256 * 256;
   pda::HeldWorkspace ws;
   if ((rc = pda::hold_workspace(stream, kHeader + terms + (int64_t)a.T * a.splits * 16, &ws)) != PDA_OK) return rc;

@@ -149,6 +149,13 @@ def test_policy_loss_of_many_rows(lib, t, V, T):
     check_policy(lib, TYPES[t], T, V, 1, 0.9, True, 3.0, 0.05, 0.01, 1.0, 0.02, 1.0, V)
 
 
+@pytest.mark.parametrize("t,V,T", [("bf16", 163_857, 130), ("f32", 81_930, 131), ("f32", 150_001, 200), ("bf16", 32_000, 127),
+                                   ("bf16", 32_000, 128), ("bf16", 16_391, 5), ("bf16", 16_392, 5)])
+def test_policy_loss_beside_the_rule(lib, t, V, T):
+    """Rows too long for registers, read twice; the sizes on both sides of the rule that chooses."""
+    check_policy(lib, TYPES[t], T, V, 0, 1.0, True, 0.0, 0.1, 0.01, 1.0, 0.01, 1.0, V + T)
+
+
 def check_policy(lib, dt, T, V, pad, temp, ref, dual, kl, ent, scale, masked, wide, seed):
     print(f"[policy] {dt} V={V} T={T}", flush=True)
     z, y = batch(T, V, dt, seed, masked=masked)
