@@ -87,7 +87,8 @@ typedef struct pdaops_cache {
  *                seq_lens[b] - n_b + i and goes to that slot of the cache
  *   positions    [T] int32 rows of cos_sin, or NULL: the position in the sequence
  *   q_out        [T, Hq, D] out_dtype (may be q itself where types agree)
- *   k_cache, v_cache, kv_scales, block_table: as for pda_paged_kv_append
+ *   k_cache, v_cache, kv_scales, block_table: as for pda_paged_kv_append (an fp8
+ *                cache takes finite values)
  *
  * An fp8 cache keeps each (block, KV head) tile's scales by the rule of
  * pda_paged_kv_append, with the tile's new tokens taken together: where their

@@ -6,8 +6,9 @@
 #include "pda_ops_internal.h"
 
 #include <cmath>
+#include <exception>
 #include <initializer_list>
-#include <utility>
+#include <new>
 
 namespace {
 
@@ -357,6 +358,19 @@ int policy_run(const void* logits, const void* targets, const float* old_logprob
   return h == hipSuccess ? PDA_OK : pda::host_fail_hip(h, "policy loss kernel launch");
 }
 
+// A C entry: what is thrown below it (no memory for the workspace's record, a
+// failed lock) becomes an error code.
+template <typename F>
+int entry(F run) {
+  try {
+    return run();
+  } catch (const std::bad_alloc&) {
+    return PDA_ENOMEM;
+  } catch (const std::exception&) {
+    return PDA_EHIP;
+  }
+}
+
 }  // namespace
 
 extern "C" {
@@ -366,35 +380,45 @@ int pdaops_paged_qk_norm_rope_append(const void* q, const void* k, const void* v
                                      const int32_t* q_offsets, void* q_out, void* k_cache, void* v_cache,
                                      float* kv_scales, const int32_t* block_table, const int32_t* seq_lens,
                                      const pdaops_rope_problem* problem, const pdaops_cache* cache, hipStream_t stream) {
-  return append_run(q, k, v, q_weight, k_weight, cos_sin, positions, q_offsets, q_out, k_cache, v_cache, kv_scales,
-                    block_table, seq_lens, problem, cache, stream);
+  return entry([&] {
+    return append_run(q, k, v, q_weight, k_weight, cos_sin, positions, q_offsets, q_out, k_cache, v_cache, kv_scales,
+                      block_table, seq_lens, problem, cache, stream);
+  });
 }
 
 int pdaops_qk_norm_rope(const void* q, const void* k, const void* q_weight, const void* k_weight, const float* cos_sin,
                         const int32_t* positions, void* q_out, void* k_out, const pdaops_rope_problem* problem,
                         hipStream_t stream) {
-  return rope_run(q, k, q_weight, k_weight, cos_sin, positions, q_out, k_out, problem, stream);
+  return entry([&] {
+    return rope_run(q, k, q_weight, k_weight, cos_sin, positions, q_out, k_out, problem, stream);
+  });
 }
 
 int pdaops_qk_norm_rope_backward(const void* q, const void* k, const void* q_weight, const void* k_weight,
                                  const float* cos_sin, const int32_t* positions, const void* grad_q_out,
                                  const void* grad_k_out, void* grad_q, void* grad_k, float* grad_q_weight,
                                  float* grad_k_weight, const pdaops_rope_problem* problem, hipStream_t stream) {
-  return rope_backward_run(q, k, q_weight, k_weight, cos_sin, positions, grad_q_out, grad_k_out, grad_q, grad_k,
-                           grad_q_weight, grad_k_weight, problem, stream);
+  return entry([&] {
+    return rope_backward_run(q, k, q_weight, k_weight, cos_sin, positions, grad_q_out, grad_k_out, grad_q, grad_k,
+                             grad_q_weight, grad_k_weight, problem, stream);
+  });
 }
 
 int pdaops_token_logprobs(const void* logits, const void* targets, float* logprobs, float* entropy,
                           const pdaops_logits_problem* problem, hipStream_t stream) {
-  return logprobs_run(logits, targets, logprobs, entropy, problem, stream);
+  return entry([&] {
+    return logprobs_run(logits, targets, logprobs, entropy, problem, stream);
+  });
 }
 
 int pdaops_policy_loss(const void* logits, const void* targets, const float* old_logprobs, const float* ref_logprobs,
                        const float* advantages, const float* weights, float* stats, void* dlogits, float* logprobs,
                        float* entropy, const pdaops_logits_problem* problem, const pdaops_policy_options* options,
                        hipStream_t stream) {
-  return policy_run(logits, targets, old_logprobs, ref_logprobs, advantages, weights, stats, dlogits, logprobs, entropy,
-                    problem, options, stream);
+  return entry([&] {
+    return policy_run(logits, targets, old_logprobs, ref_logprobs, advantages, weights, stats, dlogits, logprobs, entropy,
+                      problem, options, stream);
+  });
 }
 
 }  // extern "C"
