@@ -233,9 +233,9 @@ typedef struct pdaops_policy_options {
  *            policy) and 1
  *   logprobs, entropy  [T] f32, or NULL
  *
- * Rows of up to 327,680 bytes stay in a workgroup's registers between the sums and
- * the gradient: the logits are read once. Longer rows, and few rows (which are cut
- * into parts), are read twice. The sums are in a fixed order.
+ * Rows of up to 458,752 bytes stay in a workgroup's registers and LDS between the
+ * sums and the gradient: the logits are read once. Longer rows, and few long ones
+ * (which are cut into parts), are read twice. The sums are in a fixed order.
  *
  * Errors as for pdaops_token_logprobs, and PDA_EINVAL for coefficients that are
  * negative or not finite. Uses the stream's workspace (32 bytes per row, 16 per part).

@@ -324,14 +324,14 @@ int policy_run(const void* logits, const void* targets, const float* old_logprob
                        {dlogits, e, "dlogits", false}, {logprobs, 4, "logprobs", false}, {entropy, 4, "entropy", false}});
   if (rc != PDA_OK) return rc;
   if (a.T > kMaxWaves / 64) return host_fail(PDA_EINVAL, "num_tokens = %d is too much for one call", a.T);
-  // Rows in registers where they fit and either there are enough of them for the
-  // compute units or they are short; otherwise in parts, read twice (us per call in
-  // a HIP graph, registers / parts; bf16 unless said: 128 rows of 131,072 words 24.1 / 20.9, 192 26.0 /
-  // 33.3, 512 58 / 68; 64 of 32,000 11.6 / 10.6, 128 12.4 / 12.6; f32, 64 of 50,001 14.6 / 12.5, 128 15.5 / 16.1; 1 of 16,000
-  // 7.5 / 9.2, 512 13 / 17).
-  constexpr int kManyRows = 128, kShortVectors = 2048;
+  // Rows in registers (and LDS) where they fit and either there are enough of them
+  // for the compute units or they are short; otherwise in parts, read twice (us per
+  // call in a HIP graph, registers / parts; bf16: 128 rows of 131,072 words 24.1 / 20.9, 192 26.0 / 33.3,
+  // 512 58 / 68; 128 of 200,000 41 / 35, 192 45 / 48, 2,048 359 / 471; 64 of 32,000 11.6 / 10.6, 128 12.4 / 12.6; 1 of
+  // 16,000 7.5 / 9.2, 512 13 / 17; f32: 64 of 50,001 14.6 / 12.5, 128 15.5 / 16.1; 128 of 110,000 31 / 34, 2,048 348 / 523).
+  constexpr int kManyBf16 = 160, kManyF32 = 112, kShortVectors = 2048;
   const int v = vectors_of(a);
-  if (any && ((a.T < kManyRows && v > kShortVectors) || v > pda::kRowThreads * pda::kRowVectors)) split_rows(&a);
+  if (any && ((a.T < (a.bf16 ? kManyBf16 : kManyF32) && v > kShortVectors) || v > pda::kRowVectors)) split_rows(&a);
   const int64_t terms = ((int64_t)a.T * pda::kTerms * 4 + 255) / 256 * 256;
   pda::HeldWorkspace ws;
   if ((rc = pda::hold_workspace(stream, kHeader + terms + (int64_t)a.T * a.splits * 16, &ws)) != PDA_OK) return rc;

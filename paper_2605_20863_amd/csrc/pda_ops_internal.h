@@ -70,8 +70,8 @@ struct LogitsArgs {
   float clip_low, clip_high, dual, kl, ent_coef, grad_scale;
 };
 
-// Vectors of a row that one workgroup's registers hold.
-constexpr int kRowThreads = 1024, kRowVectors = 20;
+// Vectors of a row that one workgroup's registers and LDS hold: 1,024 threads' 19 and 9.
+constexpr int kRowVectors = 1024 * (19 + 9);
 
 hipError_t launch_token_logprobs(const LogitsArgs& a, hipStream_t s);
 hipError_t launch_policy_loss(const LogitsArgs& a, hipStream_t s);

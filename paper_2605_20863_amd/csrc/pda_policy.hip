@@ -28,7 +28,10 @@ constexpr float kFar = -1e25f;  // bound on differences in products with a zero:
 constexpr float kClamp = 20.f;  // bound on log ratios
 constexpr int kPartThreads = 256;
 
-// A row's address has the alignment of its elements only.
+// Rows have the alignment of their elements only; vectors of the logits are taken
+// from each row's first 16-byte boundary on, those of the gradient wherever that
+// leaves them (8192 x 50,257 bf16, policy loss: 363 us per call with vectors from the
+// rows' starts, 308 so).
 typedef u32x4 __attribute__((aligned(2))) u32x4_any;
 
 template <typename T>
@@ -58,7 +61,23 @@ __device__ __forceinline__ float load1(const T* p) {
   else return *p;
 }
 
-// Vector i of a row: elements i * kPer .. all of them in the row. STREAM: what is
+// A row's whole vectors, behind its first `head` elements.
+struct Span {
+  int head, vectors;
+};
+template <typename T>
+__device__ __forceinline__ Span row_span(const T* row, int V) {
+  const int head = min((int)((0 - reinterpret_cast<uintptr_t>(row)) & 15) / (int)sizeof(T), V);
+  return Span{head, (V - head) / kPer<T>};
+}
+// The element outside of the vectors that is this thread's, -1 if none is.
+template <typename T>
+__device__ __forceinline__ int odd_of(const Span& s, int V) {
+  const int t = (int)threadIdx.x, in = s.vectors * kPer<T>;
+  return t >= V - in ? -1 : t < s.head ? t : t + in;
+}
+
+// Vector i from `row` on, all of it in the row. STREAM: what is
 // not read again soon, past the caches (log-probabilities of 8192 x 131072 bf16:
 // 364 - 374 us per call without, 355 - 358 with; policy loss of 4096 x 131072, loads
 // and stores: 427 - 430 and 416 - 417).
@@ -107,25 +126,30 @@ __device__ __forceinline__ Soft merge(const Soft& a, const Soft& b, float c) {
 // than keep them all in registers of their own (twice the vector's for bf16).
 __device__ __forceinline__ void again(u32x4& v) { asm volatile("" : "+v"(v)); }
 
-// Adds the N vectors' elements to x.
+// Adds the first `live` of N vectors' elements to x (a number that is the same in
+// the wave: 8192 x 17,000 bf16, with vectors for 32,768, 125 us per call with all of them, 104 so).
 template <typename T, int N>
-__device__ __forceinline__ void add(Soft& x, u32x4 (&v)[N], float c) {
+__device__ __forceinline__ void add(Soft& x, u32x4 (&v)[N], float c, int live = N) {
   float m = x.m;
 #pragma unroll
-  for (int n = 0; n < N; ++n)
+  for (int n = 0; n < N; ++n) {
+    if (n >= live) continue;
 #pragma unroll
     for (int e = 0; e < kPer<T>; ++e) m = fmaxf(m, element<T>(v[n], e));
+  }
   x = rebase(x, m, c);
 #pragma unroll
   for (int n = 0; n < N; ++n) again(v[n]);
 #pragma unroll
-  for (int n = 0; n < N; ++n)
+  for (int n = 0; n < N; ++n) {
+    if (n >= live) continue;
 #pragma unroll
     for (int e = 0; e < kPer<T>; ++e) {
       const float d = element<T>(v[n], e) - m, p = __builtin_amdgcn_exp2f(d * c);
       x.s += p;
       x.u = fmaf(p, fmaxf(d, kFar), x.u);
     }
+  }
 }
 
 // Adds one element.
@@ -135,13 +159,6 @@ __device__ __forceinline__ void add1(Soft& x, float l, float c) {
   const float d = l - m, p = __builtin_amdgcn_exp2f(d * c);
   x.s += p;
   x.u = fmaf(p, fmaxf(d, kFar), x.u);
-}
-
-// The element past a row's whole vectors that is thread `threadIdx.x`'s, -1 if none is.
-template <typename T>
-__device__ __forceinline__ int tail_of(int V) {
-  const int at = V / kPer<T> * kPer<T> + (int)threadIdx.x;
-  return (int)threadIdx.x < kPer<T> && at < V ? at : -1;
 }
 
 // Over the aligned group of N lanes, in each of them.
@@ -280,10 +297,11 @@ __global__ __launch_bounds__(kPartThreads) void sums_kernel(LogitsArgs a) {
     return;
   }
   const T* row = static_cast<const T*>(a.logits) + (int64_t)t * a.stride;
-  const int first = p * a.chunk, end = min(first + a.chunk, a.V / kPer<T>), tail = tail_of<T>(a.V);
+  const Span sp = row_span(row, a.V);
+  const int first = p * a.chunk, end = min(first + a.chunk, sp.vectors), odd = odd_of<T>(sp, a.V);
   const float c = a.inv_temp * kLog2e, ly = load1(row + y);
-  Soft x = sum_vectors<T, U, STREAM>(row, first, end, c);
-  if (p == a.splits - 1 && tail >= 0) add1(x, load1(row + tail), c);
+  Soft x = sum_vectors<T, U, STREAM>(row + sp.head, first, end, c);
+  if (p == a.splits - 1 && odd >= 0) add1(x, load1(row + odd), c);
   x = group_merge<kPartThreads>(x, c);
   if (threadIdx.x) return;
   if (!whole) {
@@ -320,13 +338,13 @@ __global__ __launch_bounds__(kPartThreads) void finish_kernel(LogitsArgs a) {
   }
 }
 
-// Zeros in vectors first .. end - 1, and past a row's last one.
+// Zeros in vectors first .. end - 1, and with `odds` in the elements outside of the vectors.
 template <typename T>
-__device__ __forceinline__ void zero_vectors(T* out, int first, int end, int V) {
+__device__ __forceinline__ void zero_vectors(T* out, const Span& sp, int first, int end, bool odds, int V) {
   const float z[kPer<T>] = {};
-  for (int i = first + (int)threadIdx.x; i < end; i += (int)blockDim.x) store_vec(out, i, z);
-  const int tail = tail_of<T>(V);
-  if (end == V / kPer<T> && tail >= 0) store1(out + tail, 0.f);
+  for (int i = first + (int)threadIdx.x; i < end; i += (int)blockDim.x) store_vec(out + sp.head, i, z);
+  const int odd = odd_of<T>(sp, V);
+  if (odds && odd >= 0) store1(out + odd, 0.f);
 }
 
 // The target's gradient, by the thread that wrote the others around it.
@@ -347,15 +365,17 @@ template <typename T>
 __global__ __launch_bounds__(kPartThreads) void policy_part_kernel(LogitsArgs a) {
   const int t = (int)(blockIdx.x / (uint32_t)a.splits), p = (int)(blockIdx.x - (uint32_t)t * a.splits);
   const int y = target_of(a, t);
-  const int first = p * a.chunk, end = min(first + a.chunk, a.V / kPer<T>);
+  const T* row = static_cast<const T*>(a.logits) + (int64_t)t * a.stride;
+  const Span sp = row_span(row, a.V);
+  const int first = p * a.chunk, end = min(first + a.chunk, sp.vectors);
+  const bool odds = p == a.splits - 1;
   T* out = static_cast<T*>(a.dlogits) + (int64_t)t * a.d_stride;
   float terms[kTerms] = {};
   if (y < 0) {
     if (p == 0 && threadIdx.x == 0) write_row(a, t, RowStats{0.f, 0.f, 0.f}, terms);
-    if (a.dlogits) zero_vectors(out, first, end, a.V);
+    if (a.dlogits) zero_vectors(out, sp, first, end, odds, a.V);
     return;
   }
-  const T* row = static_cast<const T*>(a.logits) + (int64_t)t * a.stride;
   const float c = a.inv_temp * kLog2e, w = a.weight[t];
   float ly;
   const Soft x = merge_parts(a, t, c, ly);
@@ -365,51 +385,64 @@ __global__ __launch_bounds__(kPartThreads) void policy_part_kernel(LogitsArgs a)
   if (!a.dlogits) return;
   const Grad d = row_grad(a, x, r, g, w, c);
   if (d.zero) {
-    zero_vectors(out, first, end, a.V);
+    zero_vectors(out, sp, first, end, odds, a.V);
     return;
   }
   for (int i = first + (int)threadIdx.x; i < end; i += kPartThreads) {
-    const u32x4 v = load_vec<false>(row, i);
+    const u32x4 v = load_vec<false>(row + sp.head, i);
     float o[kPer<T>];
 #pragma unroll
     for (int e = 0; e < kPer<T>; ++e) o[e] = grad_of(d, element<T>(v, e));
-    store_vec(out, i, o);
-    if (i == y / kPer<T>) store_target(out, y, ly, d);
+    store_vec(out + sp.head, i, o);
+    if (y >= sp.head && i == (y - sp.head) / kPer<T>) store_target(out, y, ly, d);
   }
-  const int tail = tail_of<T>(a.V);
-  if (p == a.splits - 1 && tail >= 0) {
-    store1(out + tail, grad_of(d, load1(row + tail)));
-    if (tail == y) store_target(out, y, ly, d);
+  const int odd = odd_of<T>(sp, a.V);
+  if (odds && odd >= 0) {
+    store1(out + odd, grad_of(d, load1(row + odd)));
+    if (odd == y) store_target(out, y, ly, d);
   }
 }
 
 // ------------------------------------------------------------- rows in registers
 
-// Workgroup per row, whose vectors stay in its threads' registers between the
-// sums and the gradient: one read and one write of the row.
-template <typename T, int NT, int N>
+// Workgroup per row, whose vectors stay in its threads' registers (N of a thread)
+// and LDS (L of a thread) between the sums and the gradient: one read and one
+// write of the row.
+template <typename T, int NT, int N, int L>
 __global__ __launch_bounds__(NT) void policy_row_kernel(LogitsArgs a) {
-  const int t = (int)blockIdx.x, y = target_of(a, t), vectors = a.V / kPer<T>;
+  const int t = (int)blockIdx.x, y = target_of(a, t);
+  const T* row = static_cast<const T*>(a.logits) + (int64_t)t * a.stride;
+  const Span sp = row_span(row, a.V);
   T* out = static_cast<T*>(a.dlogits) + (int64_t)t * a.d_stride;
   float terms[kTerms] = {};
   if (y < 0) {
     if (threadIdx.x == 0) write_row(a, t, RowStats{0.f, 0.f, 0.f}, terms);
-    if (a.dlogits) zero_vectors(out, 0, vectors, a.V);
+    if (a.dlogits) zero_vectors(out, sp, 0, sp.vectors, true, a.V);
     return;
   }
-  const T* row = static_cast<const T*>(a.logits) + (int64_t)t * a.stride;
-  const int tail = tail_of<T>(a.V);
+  const int odd = odd_of<T>(sp, a.V);
   const float c = a.inv_temp * kLog2e, ly = load1(row + y), w = a.weight[t];
+  __shared__ u32x4 more[L ? L : 1][L ? NT : 1];
+  static_assert(L % 3 == 0, "three at a time");
+#pragma unroll
+  for (int l = 0; l < L; ++l) {
+    const int i = (int)threadIdx.x + (N + l) * NT;
+    more[l][threadIdx.x] = i < sp.vectors ? load_vec<true>(row + sp.head, i) : nothing<T>();
+  }
   u32x4 v[N];
 #pragma unroll
   for (int n = 0; n < N; ++n) {
     const int i = (int)threadIdx.x + n * NT;
-    v[n] = i < vectors ? load_vec<true>(row, i) : nothing<T>();
+    v[n] = i < sp.vectors ? load_vec<true>(row + sp.head, i) : nothing<T>();
   }
-  const float lt = tail >= 0 ? load1(row + tail) : -__builtin_huge_valf();
+  const float lodd = odd >= 0 ? load1(row + odd) : -__builtin_huge_valf();
   Soft x = none();
-  add<T>(x, v, c);
-  add1(x, lt, c);
+  add<T>(x, v, c, (sp.vectors - __builtin_amdgcn_readfirstlane((int)threadIdx.x) + NT - 1) / NT);
+  for (int l = 0; l < L; l += 3) {
+    u32x4 m[3] = {more[l][threadIdx.x], more[l + 1][threadIdx.x], more[l + 2][threadIdx.x]};
+    add<T>(x, m, c);
+  }
+  add1(x, lodd, c);
   x = group_merge<NT>(x, c);
   const RowStats r = row_stats(a, x, ly);
   const float g = policy_terms(a, t, r, w, terms);
@@ -417,23 +450,30 @@ __global__ __launch_bounds__(NT) void policy_row_kernel(LogitsArgs a) {
   if (!a.dlogits) return;
   const Grad d = row_grad(a, x, r, g, w, c);
   if (d.zero) {
-    zero_vectors(out, 0, vectors, a.V);
+    zero_vectors(out, sp, 0, sp.vectors, true, a.V);
     return;
   }
+  auto put = [&](int i, const u32x4& l) {
+    float o[kPer<T>];
+#pragma unroll
+    for (int e = 0; e < kPer<T>; ++e) o[e] = grad_of(d, element<T>(l, e));
+    store_vec(out + sp.head, i, o);
+    if (y >= sp.head && i == (y - sp.head) / kPer<T>) store_target(out, y, ly, d);
+  };
 #pragma unroll
   for (int n = 0; n < N; ++n) {
     const int i = (int)threadIdx.x + n * NT;
-    if (i >= vectors) break;
+    if (i >= sp.vectors) break;
     again(v[n]);
-    float o[kPer<T>];
-#pragma unroll
-    for (int e = 0; e < kPer<T>; ++e) o[e] = grad_of(d, element<T>(v[n], e));
-    store_vec(out, i, o);
-    if (i == y / kPer<T>) store_target(out, y, ly, d);
+    put(i, v[n]);
   }
-  if (tail >= 0) {
-    store1(out + tail, grad_of(d, lt));
-    if (tail == y) store_target(out, y, ly, d);
+  for (int l = 0; l < L; ++l) {
+    const int i = (int)threadIdx.x + (N + l) * NT;
+    if (i < sp.vectors) put(i, more[l][threadIdx.x]);
+  }
+  if (odd >= 0) {
+    store1(out + odd, grad_of(d, lodd));
+    if (odd == y) store_target(out, y, ly, d);
   }
 }
 
@@ -486,9 +526,9 @@ hipError_t logprobs_for(const LogitsArgs& a, hipStream_t s) {
   return launch(reinterpret_cast<const void*>(&finish_kernel), (a.T + rows - 1) / rows, kPartThreads, a, s);
 }
 
-template <typename T, int NT, int N>
+template <typename T, int NT, int N, int L = 0>
 hipError_t rows_for(const LogitsArgs& a, hipStream_t s) {
-  return launch(reinterpret_cast<const void*>(&policy_row_kernel<T, NT, N>), a.T, NT, a, s);
+  return launch(reinterpret_cast<const void*>(&policy_row_kernel<T, NT, N, L>), a.T, NT, a, s);
 }
 
 template <typename T>
@@ -504,7 +544,8 @@ hipError_t policy_for(const LogitsArgs& a, hipStream_t s) {
         : v <= 256 * 8 ? rows_for<T, 256, 8>(a, s)
         : v <= 256 * 16 ? rows_for<T, 256, 16>(a, s)
         : v <= 512 * 16 ? rows_for<T, 512, 16>(a, s)
-        : v <= 1024 * 16 ? rows_for<T, 1024, 16>(a, s) : rows_for<T, kRowThreads, kRowVectors>(a, s);
+        : v <= 1024 * 16 ? rows_for<T, 1024, 16>(a, s)
+        : v <= 1024 * 20 ? rows_for<T, 1024, 20>(a, s) : rows_for<T, 1024, 19, 9>(a, s);
   }
   if (e != hipSuccess) return e;
   return launch(reinterpret_cast<const void*>(&stats_kernel), 1, 1024, a, s);

@@ -149,8 +149,11 @@ def test_policy_loss_of_many_rows(lib, t, V, T):
     check_policy(lib, TYPES[t], T, V, 1, 0.9, True, 3.0, 0.05, 0.01, 1.0, 0.02, 1.0, V)
 
 
-@pytest.mark.parametrize("t,V,T", [("bf16", 163_857, 130), ("f32", 81_930, 131), ("f32", 150_001, 200), ("bf16", 32_000, 127),
-                                   ("bf16", 32_000, 128), ("bf16", 16_391, 5), ("bf16", 16_392, 5)])
+@pytest.mark.parametrize("t,V,T", [("bf16", 163_857, 130), ("f32", 81_930, 131), ("f32", 114_691, 128),
+                                   ("f32", 114_692, 129), ("bf16", 229_383, 130), ("f32", 150_001, 140), ("bf16", 32_000, 127),
+                                   ("bf16", 32_000, 128), ("bf16", 16_391, 5), ("bf16", 16_392, 5),
+                                   ("bf16", 163_857, 170), ("bf16", 229_383, 161), ("bf16", 229_384, 161),
+                                   ("bf16", 32_000, 159), ("bf16", 32_000, 160), ("f32", 20_001, 111), ("f32", 20_001, 112)])
 def test_policy_loss_beside_the_rule(lib, t, V, T):
     """Rows too long for registers, read twice; the sizes on both sides of the rule that chooses."""
     check_policy(lib, TYPES[t], T, V, 0, 1.0, True, 0.0, 0.1, 0.01, 1.0, 0.01, 1.0, V + T)
