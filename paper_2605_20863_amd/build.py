@@ -1,10 +1,12 @@
-"""Build the HIP library ``libpda.so`` in place for gfx950.
+"""Build the HIP library ``libpda.so`` in place for gfx950, and beside it the
+Python module that reads torch tensors for its calls.
 
     python -m paper_2605_20863_amd.build
 
 compiles every source under ``csrc/`` with hipcc (one object per source, in
 parallel) and links ``paper_2605_20863_amd/libpda.so`` (written to a temporary
-name, then renamed, so a concurrent loader never sees a half-written file).
+name, then renamed, so a concurrent loader never sees a half-written file). The
+module (csrc/pda_torch.cpp, host code) is compiled by g++ against torch's headers.
 """
 
 import os
@@ -16,6 +18,7 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libpda.so")
+MODULE = os.path.join(PKG, "_pda_torch.so")
 
 SOURCES = ["pda_kernels.hip", "pda_append.hip", "pda_prefill.hip", "pda_scratch.hip", "pda_rope.hip", "pda_policy.hip",
            "pda_host.cpp", "pda_ops_host.cpp"]
@@ -68,13 +71,30 @@ def _run(cmd, verbose):
     noise = "is not a recognized feature for this target"
     log = "\n".join(l for l in (res.stdout + res.stderr).splitlines() if noise not in l)
     if res.returncode != 0:
-        raise RuntimeError(f"hipcc failed ({res.returncode}):\n{log}")
+        raise RuntimeError(f"{os.path.basename(cmd[0])} failed ({res.returncode}):\n{log}")
     if verbose and log.strip():
         print(log)
 
 
+def module_command(out):
+    """Compiles and links the torch module (its symbols come from the torch that the process has loaded)."""
+    import sysconfig
+
+    import torch
+
+    t = os.path.dirname(torch.__file__)
+    rocm = os.path.dirname(os.path.dirname(os.path.realpath(hipcc())))
+    return ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", "-D__HIP_PLATFORM_AMD__",
+            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-I", os.path.join(ROOT, "include"),
+            "-isystem", os.path.join(rocm, "include"), "-isystem", sysconfig.get_paths()["include"],
+            "-isystem", os.path.join(t, "include"), "-isystem", os.path.join(t, "include", "torch", "csrc", "api", "include"),
+            os.path.join(CSRC, "pda_torch.cpp"), "-L", os.path.join(t, "lib"), f"-Wl,-rpath,{os.path.join(t, 'lib')}",
+            "-lc10", "-ltorch_cpu", "-ltorch_python", "-o", out]
+
+
 def build(verbose: bool = False) -> str:
-    """Compile every source to an object (in parallel), then link libpda.so."""
+    """Compile every source to an object (in parallel), then link libpda.so; the torch module beside them, with torch."""
+    import importlib.util
     import tempfile
     from concurrent.futures import ThreadPoolExecutor
 
@@ -89,6 +109,10 @@ def build(verbose: bool = False) -> str:
         objs = [os.path.join(tmp, s + ".o") for s in SOURCES]
         cmds = [[*common, *SOURCE_FLAGS.get(s, []), "-c", os.path.join(CSRC, s), "-o", o]
                 for s, o in zip(SOURCES, objs)]
+        module_tmp = os.path.join(tmp, "module.so")
+        with_torch = importlib.util.find_spec("torch") is not None
+        if with_torch:
+            cmds.append(module_command(module_tmp))
         with ThreadPoolExecutor(max_workers=len(cmds)) as pool:
             for f in [pool.submit(_run, c, verbose) for c in cmds]:
                 f.result()
@@ -98,6 +122,9 @@ def build(verbose: bool = False) -> str:
             if os.path.exists(out_tmp):
                 os.unlink(out_tmp)
             raise
+        if with_torch:
+            shutil.copy(module_tmp, MODULE + f".tmp{os.getpid()}")
+            os.replace(MODULE + f".tmp{os.getpid()}", MODULE)
     os.replace(out_tmp, LIB)
     return LIB
 
