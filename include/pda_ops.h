@@ -190,7 +190,8 @@ typedef struct pdaops_logits_problem {
  * Log-probabilities of the target tokens (and entropies, unless NULL) [T] f32:
  *     z = logits / temperature,  logprob = z_y - log sum exp z,  entropy = -sum p log p
  * in float32, each row read once. Few rows are cut into parts that several
- * workgroups read and a second launch joins, by a rule on T and V alone.
+ * workgroups read, by a rule on T and V alone; the last of them, or a second
+ * launch, joins them in a fixed order.
  *
  * Errors: PDA_EINVAL for bad sizes, types, strides, temperature, NULL or misaligned
  * pointers. Uses the stream's workspace (16 bytes per part).

@@ -243,7 +243,7 @@ struct Workspace {
   std::mutex mu;
   void* ptr = nullptr;  // `bytes` usable bytes; the short decode's arrival counts lie right before
   int64_t bytes = 0;
-  uint32_t epoch = 0;  // of the last short decode made outside capture
+  uint32_t epoch = 0;  // of the last call made outside capture that counts arrivals
   // the capture whose graph clears the captured calls' counts already (0: none)
   unsigned long long cleared_in = 0;
   // The combine kernel zeroes the chunk counter after each decode kernel; if a
@@ -370,6 +370,17 @@ int ensure_workspace(Workspace* ws, int64_t bytes, hipStream_t s) {
   return PDA_OK;
 }
 
+// The number of the next call that counts arrivals outside of a capture (caller holds ws->mu).
+int next_epoch(Workspace* ws, char* base, hipStream_t s, uint32_t* epoch) {
+  if (++ws->epoch == 0) {  // after 2^32 calls: start again
+    const hipError_t e = hipMemsetAsync(base - pda::kShortCountBytes, 0, pda::kShortCountBytes, s);
+    if (e != hipSuccess) return fail_hip(e, "hipMemsetAsync");
+    ws->epoch = 1;
+  }
+  *epoch = ws->epoch;
+  return PDA_OK;
+}
+
 }  // namespace
 
 namespace pda {
@@ -401,7 +412,15 @@ int hold_workspace(hipStream_t s, int64_t bytes, HeldWorkspace* out) {
   if ((rc = ensure_workspace(ws, bytes, s)) != PDA_OK) return rc;
   out->base = static_cast<char*>(ws->ptr);
   out->cus = di->cus;
+  out->record = ws;
   return PDA_OK;
+}
+
+int take_counts(hipStream_t s, const HeldWorkspace& held, Counts* out) {
+  if (capturing(s)) return PDA_OK;
+  const int rc = next_epoch(static_cast<Workspace*>(held.record), held.base, s, &out->epoch);
+  if (rc == PDA_OK) out->words = reinterpret_cast<uint64_t*>(held.base - kShortCountBytes);
+  return rc;
 }
 
 }  // namespace pda
@@ -617,13 +636,8 @@ int run(const void* q, const void* k_cache, const void* v_cache, const int32_t* 
       const unsigned long long id = capture_id(stream);
       a.short_clear = id == 0 || id != ws->cleared_in;
       ws->cleared_in = id;
-    } else {
-      if (++ws->epoch == 0) {  // after 2^32 calls: start again
-        if ((e = hipMemsetAsync(base - pda::kShortCountBytes, 0, pda::kShortCountBytes, stream)) != hipSuccess)
-          return fail_hip(e, "hipMemsetAsync");
-        ws->epoch = 1;
-      }
-      a.short_epoch = ws->epoch;
+    } else if ((rc = next_epoch(ws, base, stream, &a.short_epoch)) != PDA_OK) {
+      return rc;
     }
   }
   if (gr.on && (e = pda::launch_prefix(a, gr.num_groups, stream)) != hipSuccess)

@@ -21,7 +21,17 @@ struct HeldWorkspace {
   std::unique_lock<std::mutex> lock;
   char* base = nullptr;
   int cus = 0;
+  void* record = nullptr;
 };
 int hold_workspace(hipStream_t s, int64_t bytes, HeldWorkspace* out);
+
+// Arrival counts for one call on a held workspace: kShortUnits words,
+// kShortCountStride apart, and the epoch that this call counts from. `words` stays
+// null while the stream is captured, whose replays would all have one epoch.
+struct Counts {
+  uint64_t* words = nullptr;
+  uint32_t epoch = 0;
+};
+int take_counts(hipStream_t s, const HeldWorkspace& ws, Counts* out);
 
 }  // namespace pda

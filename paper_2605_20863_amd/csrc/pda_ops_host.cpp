@@ -95,6 +95,16 @@ int check_rope(const pdaops_rope_problem* pr, bool has_q_weight, bool has_k_weig
   return PDA_OK;
 }
 
+// Arrival counts for the call, unless it is captured.
+template <typename Args>
+int count(hipStream_t s, const pda::HeldWorkspace& ws, Args* a) {
+  pda::Counts c;
+  const int rc = pda::take_counts(s, ws, &c);
+  a->counts = c.words;
+  a->epoch = c.epoch;
+  return rc;
+}
+
 int32_t* status_word(char* base) { return reinterpret_cast<int32_t*>(base) + pda::kHdrStatus; }
 
 int append_run(const void* q, const void* k, const void* v, const void* q_weight, const void* k_weight,
@@ -228,6 +238,7 @@ int rope_backward_run(const void* q, const void* k, const void* q_weight, const 
   a.dwk = grad_k_weight;
   a.dw_part = reinterpret_cast<float*>(ws.base + kHeader);
   a.wgs = (int32_t)kWgsPerCu * (ws.cus < kMostCus ? ws.cus : (int32_t)kMostCus);
+  if (norm && (rc = count(stream, ws, &a)) != PDA_OK) return rc;
   a.status = status_word(ws.base);
   const hipError_t e = pda::launch_rope_backward(a, stream);
   return e == hipSuccess ? PDA_OK : pda::host_fail_hip(e, "norm and rotation gradient kernel launch");
@@ -292,6 +303,7 @@ int logprobs_run(const void* logits, const void* targets, float* logprobs, float
   a.ent = entropy;
   a.part = reinterpret_cast<float4*>(ws.base + kHeader);
   a.status = status_word(ws.base);
+  if (a.splits > 1 && a.T <= pda::kShortUnits && (rc = count(stream, ws, &a)) != PDA_OK) return rc;
   const hipError_t e = pda::launch_token_logprobs(a, stream);
   return e == hipSuccess ? PDA_OK : pda::host_fail_hip(e, "log-probability kernel launch");
 }
@@ -354,6 +366,7 @@ int policy_run(const void* logits, const void* targets, const float* old_logprob
   a.terms = reinterpret_cast<float*>(ws.base + kHeader);
   a.part = reinterpret_cast<float4*>(ws.base + kHeader + terms);
   a.status = status_word(ws.base);
+  if (any && a.T <= pda::kCountedRows && (rc = count(stream, ws, &a)) != PDA_OK) return rc;
   const hipError_t h = pda::launch_policy_loss(a, stream);
   return h == hipSuccess ? PDA_OK : pda::host_fail_hip(h, "policy loss kernel launch");
 }

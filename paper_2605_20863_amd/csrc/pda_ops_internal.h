@@ -4,6 +4,8 @@
 
 #include "pda_internal.h"
 
+#include <hip/hip_runtime.h>
+
 namespace pda {
 
 // Further device-side status bits (pda_internal.h has the first).
@@ -42,6 +44,8 @@ struct RopeArgs {
   float *dwq, *dwk;          // [D]
   float* dw_part;            // [workgroups, 2, D]
   int32_t wgs;               // of the gradient's kernel
+  uint64_t* counts;          // null: the weights' gradients are summed by a launch of their own
+  uint32_t epoch;
   // the launcher's: chunks of `rows` rows that a token's heads are cut into, one wave each
   int32_t chunks, rows;
 };
@@ -68,7 +72,19 @@ struct LogitsArgs {
   int64_t d_stride;
   float* terms;         // [T, kTerms]
   float clip_low, clip_high, dual, kl, ent_coef, grad_scale;
+  // arrival counts (one, or one of each row); null: rows and sums are finished by launches of their own
+  uint64_t* counts;
+  uint32_t epoch;
 };
+
+// Calls outside of a capture whose workgroups count their arrivals, so that the
+// last one finishes the work: up to this many rows (policy loss), workgroups
+// (weights' gradients) or, with a word each, kShortUnits rows in parts
+// (log-probabilities). us per call, with a further launch / counted: log-probabilities of
+// 64 x 131,072 10.0 / 8.5, of 1 x 150,000 7.9 / 6.0; gradient of 1 token 8.0 / 6.7, of 50
+// 8.2 / 7.9 (63 workgroups); policy loss of 20 x 4,046 8.0 / 6.7, of 32 x 8,000 8.2 / 7.3,
+// of 64 x 8,000 8.3 / 8.1, of 512 x 2,000 8.7 / 16.8 (arrivals at one word take turns).
+constexpr int kCountedRows = 32, kCountedWgs = 64;
 
 // Vectors of a row that one workgroup's registers and LDS hold: 1,024 threads' 19 and 9.
 constexpr int kRowVectors = 1024 * (19 + 9);

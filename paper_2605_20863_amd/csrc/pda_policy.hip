@@ -16,6 +16,7 @@
 // larger m; s and u are float32. Logits are subtracted before they are scaled, so
 // that a row of the type's lowest values is an even distribution.
 
+#include "pda_arrive.h"
 #include "pda_elem.h"
 #include "pda_ops_internal.h"
 
@@ -233,9 +234,42 @@ __device__ __forceinline__ float policy_terms(const LogitsArgs& a, int t, const 
 }
 
 __device__ __forceinline__ void write_terms(const LogitsArgs& a, int t, const float (&v)[kTerms]) {
-  f32x4* p = reinterpret_cast<f32x4*>(a.terms + (int64_t)t * kTerms);
-  p[0] = f32x4{v[0], v[1], v[2], v[3]};
-  p[1] = f32x4{v[4], v[5], v[6], v[7]};
+#pragma unroll
+  for (int i = 0; i < kTerms; i += 2) store_part(a.terms + (int64_t)t * kTerms + i, v[i], v[i + 1]);
+}
+
+// The rows' terms summed in float64, in an order that no NT changes: row t goes to
+// sum t % kSums, U rows of each at a time, and the sums are added as a tree.
+constexpr int kSums = 128;
+template <int NT, int U>
+__device__ __forceinline__ void sum_terms(const LogitsArgs& a) {
+  constexpr int S = kSums * kTerms / NT;  // sums of a thread
+  __shared__ double sums[kSums][kTerms];
+  const int k = (int)threadIdx.x % kTerms, r = (int)threadIdx.x / kTerms;
+  double x[S] = {};
+  for (int t0 = 0; t0 < a.T; t0 += U * kSums) {
+    float v[S][U];
+#pragma unroll
+    for (int s = 0; s < S; ++s)
+#pragma unroll
+      for (int i = 0; i < U; ++i) {
+        const int t = t0 + i * kSums + r + s * (NT / kTerms);
+        v[s][i] = load_part(a.terms + (int64_t)min(t, a.T - 1) * kTerms + k);
+        if (t >= a.T) v[s][i] = 0.f;
+      }
+#pragma unroll
+    for (int s = 0; s < S; ++s)
+#pragma unroll
+      for (int i = 0; i < U; ++i) x[s] += (double)v[s][i];
+  }
+#pragma unroll
+  for (int s = 0; s < S; ++s) sums[r + s * (NT / kTerms)][k] = x[s];
+  __syncthreads();
+  for (int n = kSums / 2; n > 0; n /= 2) {
+    for (int i = (int)threadIdx.x; i < n * kTerms; i += NT) sums[i / kTerms][i % kTerms] += sums[i / kTerms + n][i % kTerms];
+    __syncthreads();
+  }
+  if (threadIdx.x < kTerms) a.stats[threadIdx.x] = (float)sums[0][threadIdx.x];
 }
 
 // dl_v = p_v (base + slope x), x = l_v - m, p_v = exp2(x c - log2 s); + at_y for the target.
@@ -282,15 +316,24 @@ __device__ __forceinline__ Soft sum_vectors(const T* row, int first, int end, fl
   return x;
 }
 
+// A row's parts merged, in every lane of a wave.
+__device__ __forceinline__ Soft merge_parts(const LogitsArgs& a, int t, float c) {
+  const int l = (int)(threadIdx.x & 63);
+  const float* q = reinterpret_cast<const float*>(a.part + (int64_t)t * a.splits + min(l, a.splits - 1));
+  const Soft x = {load_part(q), load_part(q + 1), load_part(q + 2)};
+  return lanes_merge<64>(l < a.splits ? x : none(), c);
+}
+
 // Workgroup (row, part). A whole row's log-probability and entropy are written;
-// of a part, or for policy_part_kernel, the sums.
+// of a part, or for policy_part_kernel, the sums. With counts the last part's
+// workgroup of a row finishes it.
 template <typename T, int U, bool STREAM>
 __global__ __launch_bounds__(kPartThreads) void sums_kernel(LogitsArgs a) {
   const int t = (int)(blockIdx.x / (uint32_t)a.splits), p = (int)(blockIdx.x - (uint32_t)t * a.splits);
   const int y = target_of(a, t);
   const bool whole = a.splits == 1 && !a.terms;
   if (y < 0) {
-    if (whole && threadIdx.x == 0) {
+    if ((whole || (p == 0 && a.counts && !a.terms)) && threadIdx.x == 0) {
       a.logp[t] = 0.f;
       if (a.ent) a.ent[t] = 0.f;
     }
@@ -303,22 +346,30 @@ __global__ __launch_bounds__(kPartThreads) void sums_kernel(LogitsArgs a) {
   Soft x = sum_vectors<T, U, STREAM>(row + sp.head, first, end, c);
   if (p == a.splits - 1 && odd >= 0) add1(x, load1(row + odd), c);
   x = group_merge<kPartThreads>(x, c);
-  if (threadIdx.x) return;
-  if (!whole) {
-    a.part[(int64_t)t * a.splits + p] = float4{x.m, x.s, x.u, ly};
+  if (whole) {
+    if (threadIdx.x) return;
+    const RowStats r = row_stats(a, x, ly);
+    a.logp[t] = r.lp;
+    if (a.ent) a.ent[t] = r.ent;
     return;
   }
+  uint64_t before = 0;
+  if (threadIdx.x == 0) {
+    float* part = reinterpret_cast<float*>(a.part + (int64_t)t * a.splits + p);
+    store_part(part, x.m, x.s);
+    store_part(part + 2, x.u, ly);
+  }
+  if (!a.counts || a.terms) return;
+  if (threadIdx.x == 0) {
+    parts_written();
+    before = arrive(a.counts + t * kShortCountStride, a.epoch);
+  }
+  if (!last_of(before, a.epoch, a.splits) || threadIdx.x >= 64) return;
+  x = merge_parts(a, t, c);
+  if (threadIdx.x) return;
   const RowStats r = row_stats(a, x, ly);
   a.logp[t] = r.lp;
   if (a.ent) a.ent[t] = r.ent;
-}
-
-// A row's parts merged, in every lane of a wave; ly: its target's logit.
-__device__ __forceinline__ Soft merge_parts(const LogitsArgs& a, int t, float c, float& ly) {
-  const int l = (int)(threadIdx.x & 63);
-  const float4 q = a.part[(int64_t)t * a.splits + min(l, a.splits - 1)];
-  ly = q.w;
-  return lanes_merge<64>(l < a.splits ? Soft{q.x, q.y, q.z} : none(), c);
 }
 
 // A wave per row.
@@ -328,9 +379,8 @@ __global__ __launch_bounds__(kPartThreads) void finish_kernel(LogitsArgs a) {
   const int64_t y = a.targets64 ? static_cast<const int64_t*>(a.targets)[t] : static_cast<const int32_t*>(a.targets)[t];
   RowStats r = {0.f, 0.f, 0.f};
   if (y >= 0 && y < a.V) {
-    float ly;
-    const Soft x = merge_parts(a, t, a.inv_temp * kLog2e, ly);
-    r = row_stats(a, x, ly);
+    const Soft x = merge_parts(a, t, a.inv_temp * kLog2e);
+    r = row_stats(a, x, a.part[(int64_t)t * a.splits].w);
   }
   if ((threadIdx.x & 63) == 0) {
     a.logp[t] = r.lp;
@@ -353,16 +403,20 @@ __device__ __forceinline__ void store_target(T* out, int y, float ly, const Grad
   store1(out + y, grad_of(d, ly) + d.at_y);
 }
 
-// What thread 0 of a row writes beside the gradient.
-__device__ __forceinline__ void write_row(const LogitsArgs& a, int t, const RowStats& r, const float (&terms)[kTerms]) {
+// What thread 0 of a row writes beside the gradient; with counts also its arrival.
+__device__ __forceinline__ uint64_t write_row(const LogitsArgs& a, int t, const RowStats& r, const float (&terms)[kTerms]) {
+  write_terms(a, t, terms);
   if (a.logp) a.logp[t] = r.lp;
   if (a.ent) a.ent[t] = r.ent;
-  write_terms(a, t, terms);
+  if (!a.counts) return 0;
+  parts_written();
+  return arrive(a.counts, a.epoch);
 }
 
 // Workgroup (row, part), after sums_kernel: the loss's terms and the gradient.
+// Returns thread 0's arrival.
 template <typename T>
-__global__ __launch_bounds__(kPartThreads) void policy_part_kernel(LogitsArgs a) {
+__device__ __forceinline__ uint64_t policy_part(const LogitsArgs& a) {
   const int t = (int)(blockIdx.x / (uint32_t)a.splits), p = (int)(blockIdx.x - (uint32_t)t * a.splits);
   const int y = target_of(a, t);
   const T* row = static_cast<const T*>(a.logits) + (int64_t)t * a.stride;
@@ -371,22 +425,22 @@ __global__ __launch_bounds__(kPartThreads) void policy_part_kernel(LogitsArgs a)
   const bool odds = p == a.splits - 1;
   T* out = static_cast<T*>(a.dlogits) + (int64_t)t * a.d_stride;
   float terms[kTerms] = {};
+  uint64_t before = 0;
   if (y < 0) {
-    if (p == 0 && threadIdx.x == 0) write_row(a, t, RowStats{0.f, 0.f, 0.f}, terms);
+    if (p == 0 && threadIdx.x == 0) before = write_row(a, t, RowStats{0.f, 0.f, 0.f}, terms);
     if (a.dlogits) zero_vectors(out, sp, first, end, odds, a.V);
-    return;
+    return before;
   }
-  const float c = a.inv_temp * kLog2e, w = a.weight[t];
-  float ly;
-  const Soft x = merge_parts(a, t, c, ly);
+  const float c = a.inv_temp * kLog2e, w = a.weight[t], ly = a.part[(int64_t)t * a.splits].w;
+  const Soft x = merge_parts(a, t, c);
   const RowStats r = row_stats(a, x, ly);
   const float g = policy_terms(a, t, r, w, terms);
-  if (p == 0 && threadIdx.x == 0) write_row(a, t, r, terms);
-  if (!a.dlogits) return;
+  if (p == 0 && threadIdx.x == 0) before = write_row(a, t, r, terms);
+  if (!a.dlogits) return before;
   const Grad d = row_grad(a, x, r, g, w, c);
   if (d.zero) {
     zero_vectors(out, sp, first, end, odds, a.V);
-    return;
+    return before;
   }
   for (int i = first + (int)threadIdx.x; i < end; i += kPartThreads) {
     const u32x4 v = load_vec<false>(row + sp.head, i);
@@ -401,6 +455,14 @@ __global__ __launch_bounds__(kPartThreads) void policy_part_kernel(LogitsArgs a)
     store1(out + odd, grad_of(d, load1(row + odd)));
     if (odd == y) store_target(out, y, ly, d);
   }
+  return before;
+}
+
+template <typename T>
+__global__ __launch_bounds__(kPartThreads) void policy_part_kernel(LogitsArgs a) {
+  const uint64_t before = policy_part<T>(a);
+  // rows arrive with their first part
+  if (a.counts && blockIdx.x % (uint32_t)a.splits == 0 && last_of(before, a.epoch, a.T)) sum_terms<kPartThreads, 1>(a);
 }
 
 // ------------------------------------------------------------- rows in registers
@@ -408,17 +470,19 @@ __global__ __launch_bounds__(kPartThreads) void policy_part_kernel(LogitsArgs a)
 // Workgroup per row, whose vectors stay in its threads' registers (N of a thread)
 // and LDS (L of a thread) between the sums and the gradient: one read and one
 // write of the row.
+// Returns thread 0's arrival.
 template <typename T, int NT, int N, int L>
-__global__ __launch_bounds__(NT) void policy_row_kernel(LogitsArgs a) {
+__device__ __forceinline__ uint64_t policy_row(const LogitsArgs& a) {
   const int t = (int)blockIdx.x, y = target_of(a, t);
   const T* row = static_cast<const T*>(a.logits) + (int64_t)t * a.stride;
   const Span sp = row_span(row, a.V);
   T* out = static_cast<T*>(a.dlogits) + (int64_t)t * a.d_stride;
   float terms[kTerms] = {};
+  uint64_t before = 0;
   if (y < 0) {
-    if (threadIdx.x == 0) write_row(a, t, RowStats{0.f, 0.f, 0.f}, terms);
+    if (threadIdx.x == 0) before = write_row(a, t, RowStats{0.f, 0.f, 0.f}, terms);
     if (a.dlogits) zero_vectors(out, sp, 0, sp.vectors, true, a.V);
-    return;
+    return before;
   }
   const int odd = odd_of<T>(sp, a.V);
   const float c = a.inv_temp * kLog2e, ly = load1(row + y), w = a.weight[t];
@@ -446,12 +510,12 @@ __global__ __launch_bounds__(NT) void policy_row_kernel(LogitsArgs a) {
   x = group_merge<NT>(x, c);
   const RowStats r = row_stats(a, x, ly);
   const float g = policy_terms(a, t, r, w, terms);
-  if (threadIdx.x == 0) write_row(a, t, r, terms);
-  if (!a.dlogits) return;
+  if (threadIdx.x == 0) before = write_row(a, t, r, terms);
+  if (!a.dlogits) return before;
   const Grad d = row_grad(a, x, r, g, w, c);
   if (d.zero) {
     zero_vectors(out, sp, 0, sp.vectors, true, a.V);
-    return;
+    return before;
   }
   auto put = [&](int i, const u32x4& l) {
     float o[kPer<T>];
@@ -475,31 +539,18 @@ __global__ __launch_bounds__(NT) void policy_row_kernel(LogitsArgs a) {
     store1(out + odd, grad_of(d, lodd));
     if (odd == y) store_target(out, y, ly, d);
   }
+  return before;
 }
 
-// The rows' terms summed in a fixed order, in float64.
-__global__ __launch_bounds__(1024) void stats_kernel(LogitsArgs a) {
-  __shared__ double sums[1024 / kTerms][kTerms];
-  const int k = (int)threadIdx.x % kTerms, r = (int)threadIdx.x / kTerms;
-  double x = 0.;
-  int t = r;
-  constexpr int step = 1024 / kTerms, U = 8;  // eight rows' terms of a thread in flight
-  for (; t + (U - 1) * step < a.T; t += U * step) {
-    float v[U];
-#pragma unroll
-    for (int i = 0; i < U; ++i) v[i] = a.terms[(int64_t)(t + i * step) * kTerms + k];
-#pragma unroll
-    for (int i = 0; i < U; ++i) x += (double)v[i];
+template <typename T, int NT, int N, int L>
+__global__ __launch_bounds__(NT) void policy_row_kernel(LogitsArgs a) {
+  const uint64_t before = policy_row<T, NT, N, L>(a);
+  if constexpr (N <= 8) {  // few long rows go in parts
+    if (a.counts && last_of(before, a.epoch, a.T)) sum_terms<NT, 1>(a);
   }
-  for (; t < a.T; t += step) x += (double)a.terms[(int64_t)t * kTerms + k];
-  sums[r][k] = x;
-  __syncthreads();
-  for (int n = 1024 / kTerms / 2; n > 0; n /= 2) {
-    if (r < n) sums[r][k] += sums[r + n][k];
-    __syncthreads();
-  }
-  if (r == 0) a.stats[k] = (float)sums[0][k];
 }
+
+__global__ __launch_bounds__(1024) void stats_kernel(LogitsArgs a) { sum_terms<1024, 8>(a); }
 
 hipError_t launch(const void* kernel, int64_t wgs, int threads, const LogitsArgs& a, hipStream_t s) {
   LogitsArgs args = a;
@@ -521,7 +572,7 @@ hipError_t sums_for(const LogitsArgs& a, hipStream_t s) {
 template <typename T>
 hipError_t logprobs_for(const LogitsArgs& a, hipStream_t s) {
   hipError_t e = sums_for<T>(a, s);
-  if (e != hipSuccess || a.splits == 1) return e;
+  if (e != hipSuccess || a.splits == 1 || a.counts) return e;
   constexpr int rows = kPartThreads / 64;
   return launch(reinterpret_cast<const void*>(&finish_kernel), (a.T + rows - 1) / rows, kPartThreads, a, s);
 }
@@ -547,7 +598,7 @@ hipError_t policy_for(const LogitsArgs& a, hipStream_t s) {
         : v <= 1024 * 16 ? rows_for<T, 1024, 16>(a, s)
         : v <= 1024 * 20 ? rows_for<T, 1024, 20>(a, s) : rows_for<T, 1024, 19, 9>(a, s);
   }
-  if (e != hipSuccess) return e;
+  if (e != hipSuccess || a.counts) return e;
   return launch(reinterpret_cast<const void*>(&stats_kernel), 1, 1024, a, s);
 }
 

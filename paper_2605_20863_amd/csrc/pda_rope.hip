@@ -16,6 +16,7 @@
 // are float32 (the weights' gradient over all tokens: float32 in a wave, then
 // float64); every output is rounded once.
 
+#include "pda_arrive.h"
 #include "pda_elem.h"
 #include "pda_ops_internal.h"
 
@@ -681,6 +682,9 @@ __global__ __launch_bounds__(64 * kWaves) void rope_kernel(RopeArgs a) {
   token_rows<T, D, NI, true, (NI > kFewRows)>(a, t, row0, end, [&]() { return clamp_position(a, a.positions[t]); });
 }
 
+// Rows of parts that rope_weight_grad_kernel sums side by side.
+constexpr int kSumRows = 64;
+
 // Gradient. Every wave takes (token, chunk of rows) pairs in turn and keeps its
 // rows' part of the weights' gradients; a workgroup's go to dw_part.
 template <typename T, int D, int NI, bool STREAM>
@@ -761,14 +765,40 @@ __global__ __launch_bounds__(64 * kWaves) void rope_backward_kernel(RopeArgs a) 
     float x = 0.f;
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) x += sums[w][i / D][i % D];
-    a.dw_part[(int64_t)blockIdx.x * 2 * D + i] = x;
+    store_part(a.dw_part + (int64_t)blockIdx.x * 2 * D + i, x);
+  }
+  if (STREAM || !a.counts) return;  // calls that count are small
+  parts_written();
+  __syncthreads();
+  uint64_t before = 0;
+  if (threadIdx.x == 0) before = arrive(a.counts, a.epoch);
+  if (!last_of(before, a.epoch, a.wgs)) return;
+  // the parts' tree of rope_weight_grad_kernel, whose sums hold one part each here
+  static_assert(kCountedWgs <= kSumRows && kSumRows == 64, "one part a sum");
+  for (int i = (int)threadIdx.x; i < 2 * D; i += 64 * kWaves) {
+    float v[8][8];
+#pragma unroll
+    for (int r = 0; r < 8; ++r)
+#pragma unroll
+      for (int n = 0; n < 8; ++n) {
+        v[r][n] = load_part(a.dw_part + (int64_t)min(r + 8 * n, a.wgs - 1) * 2 * D + i);
+        if (r + 8 * n >= a.wgs) v[r][n] = 0.f;
+      }
+    double x[8];
+#pragma unroll
+    for (int r = 0; r < 8; ++r) {
+      const float(&s)[8] = v[r];
+      x[r] = (((double)s[0] + (double)s[4]) + ((double)s[2] + (double)s[6])) +
+             (((double)s[1] + (double)s[5]) + ((double)s[3] + (double)s[7]));
+    }
+    const double y = ((x[0] + x[4]) + (x[2] + x[6])) + ((x[1] + x[5]) + (x[3] + x[7]));
+    (i < D ? a.dwq : a.dwk)[i % D] = (float)y;
   }
 }
 
 // Sums the workgroups' parts in a fixed order: a workgroup per 16 dims of q's or
 // k's weights, a row of parts for each 16 of its threads, four loads of a thread
 // in flight.
-constexpr int kSumRows = 64;
 __global__ __launch_bounds__(16 * kSumRows) void rope_weight_grad_kernel(RopeArgs a) {
   __shared__ double sums[kSumRows][16];
   const int i = (int)threadIdx.x % 16, r = (int)threadIdx.x / 16, at = (int)blockIdx.x * 16 + i;
@@ -852,9 +882,11 @@ hipError_t backward_for(RopeArgs a, hipStream_t s) {
   cut(a, a.Hq + a.Hkv, kFewRows);
   const int64_t wgs = ((int64_t)a.T * a.chunks + kWaves - 1) / kWaves;
   if (wgs < a.wgs) a.wgs = (int32_t)wgs;
-  hipError_t e = few(a, a.Hq + a.Hkv) ? launch(&rope_backward_kernel<T, D, kFewRows, false>, a.wgs, a, s)
-                                      : launch(&rope_backward_kernel<T, D, kFewRows, true>, a.wgs, a, s);
-  if (e != hipSuccess || !a.wq) return e;
+  const bool f = few(a, a.Hq + a.Hkv);
+  if (!f || a.wgs == 0 || a.wgs > kCountedWgs) a.counts = nullptr;
+  hipError_t e = f ? launch(&rope_backward_kernel<T, D, kFewRows, false>, a.wgs, a, s)
+                   : launch(&rope_backward_kernel<T, D, kFewRows, true>, a.wgs, a, s);
+  if (e != hipSuccess || !a.wq || a.counts) return e;
   RopeArgs args = a;
   void* params[] = {&args};
   return hipLaunchKernel(reinterpret_cast<const void*>(&rope_weight_grad_kernel), dim3(2 * a.D / 16),
