@@ -646,6 +646,11 @@ __global__ __launch_bounds__(64 * kWaves) void rope_token_kernel(RopeArgs a) {
   });
 }
 
+// All tokens of 64 sequences (193,538, 32 / 4 heads, bf16): 585 us, 5.5 TB/s read and
+// written (a 1 GiB device copy: 5.0); 512-token chunks of them 108 us, 5.5 TB/s. Short
+// chunks are bound by a wave's chain of loads, length to block to scale, angles and
+// tile: 4 tokens of 399 sequences, 32 / 8 heads, fp8: 21 us, 1.7 TB/s. An fp8 V tile
+// read beside its scale rather than before it is written: no gain (22.4 and 23.3 us).
 // Workgroups of KV waves first (their chains are the longer ones), the offsets'
 // check after the last, then of q waves.
 template <typename T, KvType KV, int D, int NI>
@@ -673,6 +678,7 @@ __global__ __launch_bounds__(64 * kWaves) void rope_append_kernel(RopeArgs a) {
 
 // ------------------------------------------------------------- training
 
+// 16,384 tokens, 64 / 4 heads, bf16: 102 us, 5.65 TB/s read and written.
 template <typename T, int D, int NI>
 __global__ __launch_bounds__(64 * kWaves) void rope_kernel(RopeArgs a) {
   const uint32_t w = blockIdx.x * kWaves + wave_id();
@@ -686,7 +692,10 @@ __global__ __launch_bounds__(64 * kWaves) void rope_kernel(RopeArgs a) {
 constexpr int kSumRows = 64;
 
 // Gradient. Every wave takes (token, chunk of rows) pairs in turn and keeps its
-// rows' part of the weights' gradients; a workgroup's go to dw_part.
+// rows' part of the weights' gradients; a workgroup's go to dw_part, which with
+// counts the last workgroup sums.
+// 16,384 tokens, 32 / 4 heads, bf16: 93 us with the sum of 1,024 parts (4 us), 5.0 TB/s
+// read and written; 1 token 6.7 us, where a second launch made it 8.0.
 template <typename T, int D, int NI, bool STREAM>
 __global__ __launch_bounds__(64 * kWaves) void rope_backward_kernel(RopeArgs a) {
   constexpr int RPI = Row<D>::RPI, LPR = Row<D>::LPR;
