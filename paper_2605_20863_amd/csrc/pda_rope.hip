@@ -513,7 +513,8 @@ __device__ __forceinline__ void kv_tile(const RopeArgs& a, uint32_t item, uint32
   }
 }
 
-// One new token per sequence (a decode step): a wave's lane groups each take one
+// One new token per sequence (a decode step), or few of each or in all into a
+// cache that has no scales (by_token): a wave's lane groups each take one
 // KV head's K or V row of a token, so that a step's waves are all on the chip at
 // once; V's elements go straight to their columns. Against a wave per (head, K or V) by
 // kv_tile: 14.4 us for 512 sequences, 64 / 8 heads, fp8; see rope_token_kernel.
@@ -521,14 +522,15 @@ template <typename T, KvType KV, int D>
 __device__ __forceinline__ void kv_token(const RopeArgs& a, uint32_t item) {
   constexpr int LPR = Row<D>::LPR, RPI = Row<D>::RPI;
   const bool is_v = item & 1;
-  const int per = (a.Hkv + RPI - 1) / RPI, pair = (int)(item >> 1), b = pair / per, hc = pair - b * per;
+  const int per = (a.Hkv + RPI - 1) / RPI, pair = (int)(item >> 1), t = pair / per, hc = pair - t * per;
+  const int n = KV == KvType::FP8 ? 1 : a.n, b = KV == KvType::FP8 ? t : t / n;
   const int j = lane_id() % LPR, d0 = 8 * j, h = hc * RPI + lane_id() / LPR;
   const bool live = h < a.Hkv;
   const int hh = live ? h : a.Hkv - 1;
-  const Raw<T> raw = load8<false, T>(is_v ? a.v : a.k, b * (is_v ? a.v_stride : a.k_stride) + (int64_t)hh * D + d0);
+  const Raw<T> raw = load8<false, T>(is_v ? a.v : a.k, t * (is_v ? a.v_stride : a.k_stride) + (int64_t)hh * D + d0);
   const int full = a.seq_lens[b], len = full < 0 ? 0 : full > a.len_cap ? a.len_cap : full;
   if (len != full && hc == 0 && !is_v && lane_id() == 0) atomicOr(a.status, kStatusLenClamped);
-  const int pos = len - 1;
+  const int pos = len - n + (t - b * n);
   if (pos < 0) return;
   const int p = a.block_table[(int64_t)b * a.max_blocks + pos / 16], o = pos % 16;
   float y[8], w[8] = {};
@@ -536,7 +538,7 @@ __device__ __forceinline__ void kv_token(const RopeArgs& a, uint32_t item) {
   const Turn tn = make_turn<D>(a);
   if (!is_v) {
     if (a.wq) load_weight<D>(a.wk, a.w_bf16, w);
-    g = load_angles<D>(a, tn, clamp_position(a, a.positions ? a.positions[b] : pos));
+    g = load_angles<D>(a, tn, clamp_position(a, a.positions ? a.positions[t] : pos));
   }
   if ((unsigned)p >= (uint64_t)a.num_blocks) {
     if (lane_id() == 0) atomicOr(a.status, kStatusBadBlock);
@@ -631,7 +633,7 @@ __device__ __forceinline__ void check_offsets(const RopeArgs& a) {
 
 template <typename T, KvType KV, int D>
 __global__ __launch_bounds__(64 * kWaves) void rope_token_kernel(RopeArgs a) {
-  const uint32_t per = ((uint32_t)a.Hkv + Row<D>::RPI - 1) / Row<D>::RPI, kv_waves = 2u * (uint32_t)a.B * per;
+  const uint32_t per = ((uint32_t)a.Hkv + Row<D>::RPI - 1) / Row<D>::RPI, kv_waves = 2u * (uint32_t)a.T * per;
   const uint32_t kv_wgs = (kv_waves + kWaves - 1) / kWaves;
   if (blockIdx.x < kv_wgs) {
     const uint32_t w = blockIdx.x * kWaves + wave_id();
@@ -642,7 +644,9 @@ __global__ __launch_bounds__(64 * kWaves) void rope_token_kernel(RopeArgs a) {
   if (w >= (uint32_t)a.T * (uint32_t)a.chunks) return;
   const int t = (int)(w / (uint32_t)a.chunks), c = (int)(w - (uint32_t)t * a.chunks);
   token_rows<T, D, kFewRows, false, false>(a, t, c * a.rows, min(c * a.rows + a.rows, a.Hq), [&]() {
-    return clamp_position(a, a.positions ? a.positions[t] : max(min(a.seq_lens[t], a.len_cap) - 1, 0));
+    if (a.positions) return clamp_position(a, a.positions[t]);
+    const int n = KV == KvType::FP8 ? 1 : a.n, b = KV == KvType::FP8 ? t : t / n;
+    return clamp_position(a, max(max(min(a.seq_lens[b], a.len_cap), 0) - n + (t - b * n), 0));
   });
 }
 
@@ -848,15 +852,25 @@ void cut(RopeArgs& a, int heads, int ni) {
   a.rows = (its + a.chunks - 1) / a.chunks * rpi;
 }
 
+// Whether rope_token_kernel takes the call: rows of V written an element at a time,
+// but no chain from tile to tile's tokens. us per call, rope_append_kernel /
+// rope_token_kernel, 32 / 8 heads unless said: 512 x 2 tokens, 64 / 4 heads, bf16 19.0 / 12.1; 399 x 3
+// bf16 18.5 / 16.1, f32 28.8 / 29.9; 399 x 4 20.9 / 21.3; 200 x 8 16.6 / 20.3; 100 x 16 12.9 /
+// 18.8; 4 x 16 5.4 / 3.9; 4 x 32 5.5 / 4.3; 1 x 256, 32 / 4 heads, 5.6 / 4.6; 20 x 8 5.2 / 5.1.
+template <KvType KV>
+bool by_token(const RopeArgs& a) {
+  return a.n == 1 || (KV != KvType::FP8 && a.n > 0 && (a.n <= 3 || (int64_t)a.T * a.Hkv <= 1024));
+}
+
 // Few rows a wave where that gives the compute units more waves than few.
 bool few(const RopeArgs& a, int heads) { return (int64_t)a.T * heads < 65536; }
 
 template <typename T, KvType KV, int D>
 hipError_t append_for(RopeArgs a, hipStream_t s) {
-  if (a.n == 1) {
+  if (by_token<KV>(a)) {
     cut(a, a.Hq, kFewRows);
     constexpr int rpi = Row<D>::RPI;
-    const int64_t kv = (2 * (int64_t)a.B * ((a.Hkv + rpi - 1) / rpi) + kWaves - 1) / kWaves;
+    const int64_t kv = (2 * (int64_t)a.T * ((a.Hkv + rpi - 1) / rpi) + kWaves - 1) / kWaves;
     return launch(&rope_token_kernel<T, KV, D>, kv + ((int64_t)a.T * a.chunks + kWaves - 1) / kWaves, a, s);
   }
   const bool f = few(a, a.Hq);
