@@ -384,17 +384,11 @@ __device__ __forceinline__ void kv_tile(const RopeArgs& a, uint32_t item, uint32
     const int s = min(max(slot_of(it), o), e - 1);
     raw[it] = load8<STREAM, T>(in, (t0 + s) * in_stride + (int64_t)h * D + d0);
   }
-  if ((unsigned)p >= (uint64_t)a.num_blocks) {
-    if (lane_id() == 0) atomicOr(a.status, kStatusBadBlock);
-    return;
-  }
-  const int64_t ct = (int64_t)p * a.Hkv + h;
-  float* sp = KV == KvType::FP8 ? a.kv_scales + (is_v ? a.num_blocks * a.Hkv : 0) + ct : nullptr;
-  const float old = KV == KvType::FP8 && o > 0 ? *sp : 0.f;
   float y[IT][8];
+  auto rows = [&]() {
 #pragma unroll
-  for (int it = 0; it < IT; ++it) unpack(raw[it], y[it]);
-  if (!is_v) {
+    for (int it = 0; it < IT; ++it) unpack(raw[it], y[it]);
+    if (is_v) return;
     const Turn tn = make_turn<D>(a);
     float w[8] = {};
     if (a.wq) load_weight<D>(a.wk, a.w_bf16, w);
@@ -405,7 +399,18 @@ __device__ __forceinline__ void kv_tile(const RopeArgs& a, uint32_t item, uint32
       const int pos = clamp_position(a, a.positions ? a.positions[t0 + s] : 16 * blk + s);
       norm_turn<D>(a, tn, load_angles<D>(a, tn, pos), w, y[it]);
     }
+  };
+  // without a scale to load, rows are turned before the tile's place is known
+  // (27 x 59 tokens, 32 / 8 heads, bf16: 12.1 us per call after it, 11.1 so)
+  if constexpr (KV != KvType::FP8) rows();
+  if ((unsigned)p >= (uint64_t)a.num_blocks) {
+    if (lane_id() == 0) atomicOr(a.status, kStatusBadBlock);
+    return;
   }
+  const int64_t ct = (int64_t)p * a.Hkv + h;
+  float* sp = KV == KvType::FP8 ? a.kv_scales + (is_v ? a.num_blocks * a.Hkv : 0) + ct : nullptr;
+  const float old = KV == KvType::FP8 && o > 0 ? *sp : 0.f;
+  if constexpr (KV == KvType::FP8) rows();
   float scale = 1.f;
   bool raised = false;
   if constexpr (KV == KvType::FP8) {
