@@ -340,8 +340,9 @@ int policy_run(const void* logits, const void* targets, const float* old_logprob
   // for the compute units or they are short; otherwise in parts, read twice (us per
   // call in a HIP graph, registers / parts; bf16: 128 rows of 131,072 words 24.1 / 20.9, 192 26.0 / 33.3,
   // 512 58 / 68; 128 of 200,000 41 / 35, 192 45 / 48, 2,048 359 / 471; 64 of 32,000 11.6 / 10.6, 128 12.4 / 12.6; 1 of
-  // 16,000 7.5 / 9.2, 512 13 / 17; f32: 64 of 50,001 14.6 / 12.5, 128 15.5 / 16.1; 128 of 110,000 31 / 34, 2,048 348 / 523).
-  constexpr int kManyBf16 = 160, kManyF32 = 112, kShortVectors = 2048;
+  // 16,000 7.5 / 9.2, 512 13 / 17; among eager calls 8 of 20,000 9.2 / 10.7, of 32,000 10.7 / 10.6, 64 of 20,000
+  // 11.2 / 12.5; f32: 64 of 50,001 14.6 / 12.5, 128 15.5 / 16.1; 128 of 110,000 31 / 34, 2,048 348 / 523).
+  constexpr int kManyBf16 = 160, kManyF32 = 112, kShortVectors = 3200;
   const int v = vectors_of(a);
   if (any && ((a.T < (a.bf16 ? kManyBf16 : kManyF32) && v > kShortVectors) || v > pda::kRowVectors)) split_rows(&a);
   const int64_t terms = ((int64_t)a.T * pda::kTerms * 4 + 255) / 256 * 256;

@@ -557,7 +557,7 @@ __device__ __forceinline__ uint64_t policy_row(const LogitsArgs& a) {
 template <typename T, int NT, int N, int L>
 __global__ __launch_bounds__(NT) void policy_row_kernel(LogitsArgs a) {
   const uint64_t before = policy_row<T, NT, N, L>(a);
-  if constexpr (N <= 8) {  // few long rows go in parts
+  if constexpr (NT == 256) {  // few longer rows go in parts
     if (a.counts && last_of(before, a.epoch, a.T)) sum_terms<NT, 1>(a);
   }
 }
