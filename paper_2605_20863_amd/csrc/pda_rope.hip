@@ -655,8 +655,8 @@ __global__ __launch_bounds__(64 * kWaves) void rope_token_kernel(RopeArgs a) {
   });
 }
 
-// All tokens of 64 sequences (193,538, 32 / 4 heads, bf16): 585 us, 5.5 TB/s read and
-// written (a 1 GiB device copy: 5.0); 512-token chunks of them 108 us, 5.5 TB/s. Short
+// All tokens of 64 sequences (193,538, 32 / 4 heads, bf16): 572 us, 5.6 TB/s read and
+// written (a 1 GiB device copy: 5.0); 512-token chunks, 28 / 4 heads, 108 us, 5.6 TB/s. Short
 // chunks are bound by a wave's chain of loads, length to block to scale, angles and
 // tile: 4 tokens of 399 sequences, 32 / 8 heads, fp8: 21 us, 1.7 TB/s. An fp8 V tile
 // read beside its scale rather than before it is written: no gain (22.4 and 23.3 us).
