@@ -13,6 +13,7 @@ from __future__ import annotations
 import ctypes
 import os
 import re
+import warnings
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
 # PDA_LIBRARY may point at another build of the same library (same C interface)
@@ -36,12 +37,15 @@ except ImportError:  # pure C-ABI use without torch: the ROCm installation's run
 
 _lib = ctypes.CDLL(LIB_PATH)
 
+# The torch module only saves host time: without it every call goes through the
+# checks below, to the same kernels.
+_pda_torch = None
 if _torch_rt is not None:
     try:
         from . import _pda_torch
-    except ImportError as e:
-        raise ImportError(f"the library's torch module does not load ({e}): build it first "
-                          "(python -m paper_2605_20863_amd.build)") from e
+    except ImportError as e:  # not built, or for a torch of another ABI
+        warnings.warn(f"_pda_torch does not load ({e}); calls of include/pda_ops.h take some microseconds more host "
+                      "time each until python -m paper_2605_20863_amd.build has built it", RuntimeWarning)
 
 # pda_dtype / pda_status / pda_variant
 F32, BF16, FP8_E4M3 = 0, 1, 2
@@ -220,9 +224,10 @@ for _name, _args in (
     if hasattr(_lib, _name):
         getattr(_lib, _name).argtypes = _args
         getattr(_lib, _name).restype = ctypes.c_int
-_entries = {n: ctypes.cast(getattr(_lib, n), _vp).value for n in (
-    "pdaops_paged_qk_norm_rope_append", "pdaops_qk_norm_rope", "pdaops_qk_norm_rope_backward", "pdaops_token_logprobs",
-    "pdaops_policy_loss") if hasattr(_lib, n)}
+# The torch module's functions with the addresses of their entries.
+_calls = {n: (getattr(_pda_torch, n), ctypes.cast(getattr(_lib, "pdaops_" + n), _vp).value) for n in (
+    "paged_qk_norm_rope_append", "qk_norm_rope", "qk_norm_rope_backward", "token_logprobs", "policy_loss")
+    if _pda_torch is not None and hasattr(_lib, "pdaops_" + n)}
 
 
 class PdaError(RuntimeError):
@@ -599,12 +604,13 @@ if _torch_rt is not None:
     _current_device = getattr(_torch_rt._C, "_cuda_getDevice", _torch_rt.cuda.current_device)
 
 
-def _direct(call, entry, first, stream, *args):
+def _direct(name, first, stream, *args):
     """The call's code from _pda_torch, or None: not made."""
     index = first.get_device()
-    if index < 0 or index != _current_device() or _raw_stream is None:
+    if index < 0 or index != _current_device() or _raw_stream is None or name not in _calls:
         return None
-    rc = call(_entries.get(entry), _raw_stream(index) if stream is None else stream.cuda_stream, *args)
+    call, entry = _calls[name]
+    rc = call(entry, _raw_stream(index) if stream is None else stream.cuda_stream, *args)
     if rc:
         _check(rc)
     return rc
@@ -702,7 +708,7 @@ def paged_qk_norm_rope_append(q, k, v, q_weight, k_weight, cos_sin, q_offsets, k
     The rotated queries go to q_out [T, Hq, D]; cache layouts and fp8 scales as for
     paged_kv_append.
     """
-    if _direct(_pda_torch.paged_qk_norm_rope_append, "pdaops_paged_qk_norm_rope_append", q, stream, q, k, v, q_weight, k_weight, cos_sin,
+    if _direct("paged_qk_norm_rope_append", q, stream, q, k, v, q_weight, k_weight, cos_sin,
                q_offsets, k_cache, v_cache, kv_scales, block_table, seq_lens, q_out, eps, interleaved, positions,
                max_seq_len) == OK:
         return q_out
@@ -741,7 +747,7 @@ def paged_qk_norm_rope_append(q, k, v, q_weight, k_weight, cos_sin, q_offsets, k
 def qk_norm_rope(q, k, q_weight, k_weight, cos_sin, positions, q_out, k_out, eps=1e-6, interleaved=False, stream=None):
     """Enqueue the norm and rotation of q [T, Hq, D] and k [T, Hkv, D] (as for
     paged_qk_norm_rope_append) at ``positions`` [T] int32 into q_out and k_out."""
-    if _direct(_pda_torch.qk_norm_rope, "pdaops_qk_norm_rope", q, stream, q, k, q_weight, k_weight, cos_sin, positions,
+    if _direct("qk_norm_rope", q, stream, q, k, q_weight, k_weight, cos_sin, positions,
                q_out, k_out, eps, interleaved) == OK:
         return q_out, k_out
     index = q.get_device()
@@ -762,7 +768,7 @@ def qk_norm_rope_backward(q, k, q_weight, k_weight, cos_sin, positions, grad_q_o
     """Enqueue the gradient of qk_norm_rope: grad_q, grad_k (q's dtype) from
     grad_q_out, grad_k_out, and with weights grad_q_weight, grad_k_weight [D]
     float32, which are written, not added to."""
-    if _direct(_pda_torch.qk_norm_rope_backward, "pdaops_qk_norm_rope_backward", q, stream, q, k, q_weight, k_weight,
+    if _direct("qk_norm_rope_backward", q, stream, q, k, q_weight, k_weight,
                cos_sin, positions, grad_q_out, grad_k_out, grad_q, grad_k, grad_q_weight, grad_k_weight, eps, interleaved) == OK:
         return grad_q, grad_k
     index = q.get_device()
@@ -821,7 +827,7 @@ def token_logprobs(logits, targets, logprobs, entropy=None, temperature=1.0, str
     """Enqueue the log-probabilities of ``targets`` (int64 or int32 [T]; negative:
     a row that takes no part) under logits [T, V] / temperature, and the rows'
     entropies, into float32 [T] tensors. Rows of logits may be apart."""
-    if _direct(_pda_torch.token_logprobs, "pdaops_token_logprobs", logits, stream, logits, targets, logprobs,
+    if _direct("token_logprobs", logits, stream, logits, targets, logprobs,
                entropy, temperature) == OK:
         return logprobs
     index = logits.get_device()
@@ -845,7 +851,7 @@ def policy_loss(logits, targets, old_logprobs, advantages, weights, stats, dlogi
     ``dlogits`` [T, V] of the logits' dtype (may be ``logits``; None: the loss alone)
     grad_scale times its gradient; ``logprobs`` and ``entropy`` the rows' values.
     """
-    if _direct(_pda_torch.policy_loss, "pdaops_policy_loss", logits, stream, logits, targets, old_logprobs, advantages,
+    if _direct("policy_loss", logits, stream, logits, targets, old_logprobs, advantages,
                weights, stats, dlogits, logprobs, entropy, ref_logprobs, clip_low, clip_high, dual_clip, kl_coef, entropy_coef,
                temperature, grad_scale) == OK:
         return stats
