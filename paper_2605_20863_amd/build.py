@@ -93,7 +93,8 @@ def module_command(out):
 
 
 def build(verbose: bool = False) -> str:
-    """Compile every source to an object (in parallel), then link libpda.so; the torch module beside them, with torch."""
+    """Compile every source to an object (in parallel), then link libpda.so; the torch module beside them, with torch
+    (a failure of the module's is raised once libpda.so, which needs none of it, is in place)."""
     import importlib.util
     import tempfile
     from concurrent.futures import ThreadPoolExecutor
@@ -109,11 +110,10 @@ def build(verbose: bool = False) -> str:
         objs = [os.path.join(tmp, s + ".o") for s in SOURCES]
         cmds = [[*common, *SOURCE_FLAGS.get(s, []), "-c", os.path.join(CSRC, s), "-o", o]
                 for s, o in zip(SOURCES, objs)]
-        module_tmp = os.path.join(tmp, "module.so")
-        with_torch = importlib.util.find_spec("torch") is not None
-        if with_torch:
-            cmds.append(module_command(module_tmp))
-        with ThreadPoolExecutor(max_workers=len(cmds)) as pool:
+        module_tmp, module = os.path.join(tmp, "module.so"), None
+        with ThreadPoolExecutor(max_workers=len(cmds) + 1) as pool:
+            if importlib.util.find_spec("torch") is not None:
+                module = pool.submit(lambda: _run(module_command(module_tmp), verbose))
             for f in [pool.submit(_run, c, verbose) for c in cmds]:
                 f.result()
         try:
@@ -122,10 +122,11 @@ def build(verbose: bool = False) -> str:
             if os.path.exists(out_tmp):
                 os.unlink(out_tmp)
             raise
-        if with_torch:
+        os.replace(out_tmp, LIB)
+        if module is not None:
+            module.result()
             shutil.copy(module_tmp, MODULE + f".tmp{os.getpid()}")
             os.replace(MODULE + f".tmp{os.getpid()}", MODULE)
-    os.replace(out_tmp, LIB)
     return LIB
 
 
