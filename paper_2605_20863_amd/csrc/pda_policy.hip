@@ -559,10 +559,12 @@ __device__ __forceinline__ uint64_t policy_row(const LogitsArgs& a) {
   return before;
 }
 
+// Only workgroups of this size finish a counted call's sums (few longer rows go in parts).
+constexpr int kFinishThreads = 256;
 template <typename T, int NT, int N, int L>
 __global__ __launch_bounds__(NT) void policy_row_kernel(LogitsArgs a) {
   const uint64_t before = policy_row<T, NT, N, L>(a);
-  if constexpr (NT == 256) {  // few longer rows go in parts
+  if constexpr (NT == kFinishThreads) {
     if (a.counts && last_of(before, a.epoch, a.T)) sum_terms<NT, 1>(a);
   }
 }
@@ -600,17 +602,18 @@ hipError_t rows_for(const LogitsArgs& a, hipStream_t s) {
 }
 
 template <typename T>
-hipError_t policy_for(const LogitsArgs& a, hipStream_t s) {
+hipError_t policy_for(LogitsArgs a, hipStream_t s) {
   hipError_t e = hipSuccess;
+  if (!a.splits && a.V / kPer<T> > kFinishThreads * 16) a.counts = nullptr;  // the sums take a launch of their own
   if (a.splits) {
     const int64_t wgs = (int64_t)a.T * a.splits;
     e = sums_for<T>(a, s);
     if (e == hipSuccess) e = launch(reinterpret_cast<const void*>(&policy_part_kernel<T>), wgs, kPartThreads, a, s);
   } else if (a.T) {
     const int v = a.V / kPer<T>;
-    e = v <= 256 * 4 ? rows_for<T, 256, 4>(a, s)
-        : v <= 256 * 8 ? rows_for<T, 256, 8>(a, s)
-        : v <= 256 * 16 ? rows_for<T, 256, 16>(a, s)
+    e = v <= kFinishThreads * 4 ? rows_for<T, kFinishThreads, 4>(a, s)
+        : v <= kFinishThreads * 8 ? rows_for<T, kFinishThreads, 8>(a, s)
+        : v <= kFinishThreads * 16 ? rows_for<T, kFinishThreads, 16>(a, s)
         : v <= 512 * 16 ? rows_for<T, 512, 16>(a, s)
         : v <= 1024 * 16 ? rows_for<T, 1024, 16>(a, s)
         : v <= 1024 * 20 ? rows_for<T, 1024, 20>(a, s) : rows_for<T, 1024, 19, 9>(a, s);
