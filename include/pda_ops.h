@@ -98,11 +98,13 @@ typedef struct pdaops_cache {
  * not append into the same block of an fp8 cache.
  *
  * Device-checked: lengths are clamped (status bit 1), tokens whose block-table
- * entry lies outside [0, num_blocks) are not written (bit 2), a sequence whose
- * offsets are not non-decreasing within [0, T] is left out (bit 8), positions
- * outside the table are clamped into it (bit 32). Tokens before position 0
- * (n_b > seq_lens[b]) are turned as at position 0 and not written; q_out rows of
- * no sequence are not written.
+ * entry lies outside [0, num_blocks) are not written (bit 2), positions outside the
+ * table are clamped into it (bit 32). Offsets that are not non-decreasing within
+ * [0, T] set bit 8: a sequence whose own two are not in order is left out, and
+ * tokens of the call's other sequences may be too (keys and values, q_out rows, or
+ * both); what is written is right. Tokens before position 0 (n_b > seq_lens[b]) are
+ * turned as at position 0 and not written; q_out rows of no sequence are not
+ * written.
  *
  * Errors: PDA_EINVAL for bad sizes, types, strides, NULL or misaligned pointers
  * (16 bytes for all but the int32 arrays and kv_scales), T not a multiple of B
