@@ -108,7 +108,9 @@ typedef struct pdaops_cache {
  *
  * Errors: PDA_EINVAL for bad sizes, types, strides, NULL or misaligned pointers
  * (16 bytes for all but the int32 arrays and kv_scales), T not a multiple of B
- * without offsets, or work for more than 2^26 waves; PDA_EUNSUPPORTED for head_dim
+ * without offsets, or too much work for one call: T ((Hq + Hkv) / (512 / D) + 2) or
+ * 2 Hkv times the bound on the call's cache tiles (T / 16 + 2 B with offsets, B ((T / B +
+ * 14) / 16 + 1) without) past 2^25, quotients rounded down; PDA_EUNSUPPORTED for head_dim
  * not in {64, 128}, rotary_dim not a multiple of 16 or block_size != 16.
  */
 int pdaops_paged_qk_norm_rope_append(const void* q,
@@ -131,7 +133,8 @@ int pdaops_paged_qk_norm_rope_append(const void* q,
 
 /* The same norm and rotation without a cache: q_out [T, Hq, D] and k_out [T, Hkv,
  * D] (out_dtype; q and k themselves where types and strides agree), at positions
- * [T] int32. Errors and status bits as above. */
+ * [T] int32. Errors and status bits as above; T ((Hq + Hkv) / (512 / D) + 2) may reach
+ * 2^26, here and for the gradient. */
 int pdaops_qk_norm_rope(const void* q,
                         const void* k,
                         const void* q_weight,
@@ -151,8 +154,8 @@ int pdaops_qk_norm_rope(const void* q,
  *     g = grad turned back,  dw = sum g x r,  dx = r (g w - x r mean(g w x r)).
  * q and k are the forward's inputs (without weights they are not read and may be
  * NULL). The sums are in a fixed order: repeated calls give identical results.
- * Uses the stream's workspace (8 D bytes per workgroup, at most 4 workgroups per
- * compute unit).
+ * Uses the stream's workspace (with weights 32,768 D bytes, whatever the call's size: room
+ * for the parts of 4 workgroups on each of up to 1,024 compute units).
  */
 int pdaops_qk_norm_rope_backward(const void* q,
                                  const void* k,
@@ -196,7 +199,8 @@ typedef struct pdaops_logits_problem {
  * launch, joins them in a fixed order.
  *
  * Errors: PDA_EINVAL for bad sizes, types, strides, temperature, NULL or misaligned
- * pointers. Uses the stream's workspace (16 bytes per part).
+ * pointers, or more than 2^22 rows (rows in parts are few: at most 1,023 of them). Uses
+ * the stream's workspace (16 bytes per part).
  */
 int pdaops_token_logprobs(const void* logits,
                           const void* targets,
@@ -241,7 +245,7 @@ typedef struct pdaops_policy_options {
  * (which are cut into parts), are read twice. The sums are in a fixed order.
  *
  * Errors as for pdaops_token_logprobs, and PDA_EINVAL for coefficients that are
- * negative or not finite. Uses the stream's workspace (32 bytes per row, 16 per part).
+ * negative or not finite, or more than 2^20 rows. Uses the stream's workspace (32 bytes per row, 16 per part).
  */
 int pdaops_policy_loss(const void* logits,
                        const void* targets,

@@ -135,7 +135,9 @@ int append_run(const void* q, const void* k, const void* v, const void* q_weight
   a.n = !q_offsets && B > 0 ? (int32_t)(T / B) : 0;
   a.tiles_per_seq = a.n > 0 ? (int32_t)(((int64_t)a.n + 14) / 16 + 1) : 0;
   const int64_t tiles = q_offsets ? T / 16 + 2 * B : B * a.tiles_per_seq;
-  if (tiles * 2 * a.Hkv > kMaxWaves / 2 || T * ((a.Hq + a.Hkv) / (512 / a.D) + 2) > kMaxWaves / 2)
+  if (T * ((a.Hq + a.Hkv) / (512 / a.D) + 2) > kMaxWaves / 2)
+    return host_fail(PDA_EINVAL, "num_tokens = %d of %d heads is too much for one call", a.T, a.Hq + a.Hkv);
+  if (tiles * 2 * a.Hkv > kMaxWaves / 2)
     return host_fail(PDA_EINVAL, "%lld cache tiles of %d KV heads are too much for one call", (long long)tiles, a.Hkv);
   if (T == 0 || B == 0) return PDA_OK;
   rc = check_pointers({{q, 16, "q", true}, {k, 16, "k", true}, {v, 16, "v", true}, {q_weight, 16, "q_weight", false},
