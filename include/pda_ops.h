@@ -236,8 +236,11 @@ typedef struct pdaops_policy_options {
  *
  *   old_logprobs, advantages, weights [T] f32; ref_logprobs [T] f32 or NULL
  *   stats    [8] f32: sums over rows of weights times loss, policy, kl, entropy,
- *            clipped (1 where a clip holds), ratio, e^-d - 1 + d (KL to the rollout's
- *            policy) and 1
+ *            clipped (1 where a clip holds), ratio, e^-d - 1 + d and 1. The seventh,
+ *            a distance from the rollout's policy (0 where they agree, else positive),
+ *            has the mean KL(policy || rollout) over tokens drawn from the policy;
+ *            over the rollout's own tokens its mean is no KL but chi-square less KL,
+ *            both of (rollout || policy)
  *   logprobs, entropy  [T] f32, or NULL
  *
  * Rows of up to 458,752 bytes stay in a workgroup's registers and LDS between the

@@ -55,6 +55,7 @@ _VARIANTS = {"auto": VARIANT_AUTO, "vector": VARIANT_VECTOR, "mfma": VARIANT_MFM
 STATUS_LEN_CLAMPED, STATUS_BAD_BLOCK, STATUS_PREFIX_SHORTENED, STATUS_BAD_OFFSETS = 1, 2, 4, 8
 STATUS_HALF_RANGE = 16
 STATUS_BAD_POSITION, STATUS_BAD_TARGET = 32, 64
+# "old_kl" is e^-d - 1 + d of the log ratio d: include/pda_ops.h says what its mean estimates.
 POLICY_STATS = ("loss", "policy", "kl", "entropy", "clipped", "ratio", "old_kl", "weight")
 NOALLOC_SCRATCH_BYTES = 32 << 20   # PDA_NOALLOC_SCRATCH_BYTES
 
