@@ -25,7 +25,7 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLowest = -3.402823466e38f;
-constexpr float kFar = -1e25f;  // bound on differences in products with a zero: its exponential is 0
+constexpr float kFar = -1e25f;  // bound on differences in products with a zero: their exponential is 0 below temperatures of 1e23
 constexpr float kClamp = 20.f;  // bound on log ratios
 constexpr int kPartThreads = 256;
 
@@ -114,8 +114,8 @@ __device__ __forceinline__ Soft none() { return Soft{kLowest, 0.f, 0.f}; }
 
 // x's sums as of the larger maximum m.
 __device__ __forceinline__ Soft rebase(const Soft& x, float m, float c) {
-  const float d = fmaxf(x.m - m, kFar), f = __builtin_amdgcn_exp2f(d * c);
-  return Soft{m, x.s * f, f * fmaf(x.s, d, x.u)};
+  const float d = x.m - m, f = __builtin_amdgcn_exp2f(d * c);
+  return Soft{m, x.s * f, f * fmaf(x.s, fmaxf(d, kFar), x.u)};
 }
 __device__ __forceinline__ Soft merge(const Soft& a, const Soft& b, float c) {
   const float m = fmaxf(a.m, b.m);
