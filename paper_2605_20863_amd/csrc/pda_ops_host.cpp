@@ -6,7 +6,6 @@
 #include "pda_ops_internal.h"
 
 #include <cmath>
-#include <exception>
 #include <initializer_list>
 #include <new>
 
@@ -375,15 +374,16 @@ int policy_run(const void* logits, const void* targets, const float* old_logprob
 }
 
 // A C entry: what is thrown below it (no memory for the workspace's record, a
-// failed lock) becomes an error code.
+// failed lock) becomes an error code with a text, of at most 15 characters: a
+// std::string holds these without memory of its own.
 template <typename F>
 int entry(F run) {
   try {
     return run();
   } catch (const std::bad_alloc&) {
-    return PDA_ENOMEM;
-  } catch (const std::exception&) {
-    return PDA_EHIP;
+    return host_fail(PDA_ENOMEM, "no host memory");
+  } catch (...) {
+    return host_fail(PDA_EHIP, "host exception");
   }
 }
 
