@@ -80,15 +80,15 @@ __device__ __forceinline__ int odd_of(const Span& s, int V) {
 
 // Vector i from `row` on, all of it in the row. STREAM: what is
 // not read again soon, past the caches (log-probabilities of 8192 x 131072 bf16:
-// 364 - 374 us per call without, 355 - 358 with; policy loss of 4096 x 131072, loads
-// and stores: 427 - 430 and 416 - 417).
+// 364 - 374 us per call without, 355 - 358 with).
 template <bool STREAM, typename T>
 __device__ __forceinline__ u32x4 load_vec(const T* row, int i) {
   const u32x4_any* p = reinterpret_cast<const u32x4_any*>(row + (int64_t)i * kPer<T>);
   return STREAM ? __builtin_nontemporal_load(p) : *p;
 }
 
-template <typename T>
+// STREAM as the launcher says (kStreamBytes).
+template <bool STREAM, typename T>
 __device__ __forceinline__ void store_vec(T* row, int i, const float (&y)[kPer<T>]) {
   u32x4 v;
   if constexpr (sizeof(T) == 2) {
@@ -98,7 +98,9 @@ __device__ __forceinline__ void store_vec(T* row, int i, const float (&y)[kPer<T
 #pragma unroll
     for (int e = 0; e < 4; ++e) v[e] = as_u32(y[e]);
   }
-  __builtin_nontemporal_store(v, reinterpret_cast<u32x4_any*>(row + (int64_t)i * kPer<T>));
+  u32x4_any* p = reinterpret_cast<u32x4_any*>(row + (int64_t)i * kPer<T>);
+  if constexpr (STREAM) __builtin_nontemporal_store(v, p);
+  else *p = v;
 }
 
 template <typename T>
@@ -401,10 +403,10 @@ __global__ __launch_bounds__(kPartThreads) void finish_kernel(LogitsArgs a) {
 }
 
 // Zeros in vectors first .. end - 1, and with `odds` in the elements outside of the vectors.
-template <typename T>
+template <bool STREAM, typename T>
 __device__ __forceinline__ void zero_vectors(T* out, const Span& sp, int first, int end, bool odds, int V) {
   const float z[kPer<T>] = {};
-  for (int i = first + (int)threadIdx.x; i < end; i += (int)blockDim.x) store_vec(out + sp.head, i, z);
+  for (int i = first + (int)threadIdx.x; i < end; i += (int)blockDim.x) store_vec<STREAM>(out + sp.head, i, z);
   const int odd = odd_of<T>(sp, V);
   if (odds && odd >= 0) store1(out + odd, 0.f);
 }
@@ -427,7 +429,7 @@ __device__ __forceinline__ uint64_t write_row(const LogitsArgs& a, int t, const 
 
 // Workgroup (row, part), after sums_kernel: the loss's terms and the gradient.
 // Returns thread 0's arrival.
-template <typename T>
+template <typename T, bool STREAM>
 __device__ __forceinline__ uint64_t policy_part(const LogitsArgs& a) {
   const int t = (int)(blockIdx.x / (uint32_t)a.splits), p = (int)(blockIdx.x - (uint32_t)t * a.splits);
   const int y = target_of(a, t);
@@ -440,7 +442,7 @@ __device__ __forceinline__ uint64_t policy_part(const LogitsArgs& a) {
   uint64_t before = 0;
   if (y < 0) {
     if (p == 0 && threadIdx.x == 0) before = write_row(a, t, RowStats{0.f, 0.f, 0.f}, terms);
-    if (a.dlogits) zero_vectors(out, sp, first, end, odds, a.V);
+    if (a.dlogits) zero_vectors<STREAM>(out, sp, first, end, odds, a.V);
     return before;
   }
   const float c = a.inv_temp * kLog2e, w = a.weight[t], ly = a.part[(int64_t)t * a.splits].w;
@@ -451,7 +453,7 @@ __device__ __forceinline__ uint64_t policy_part(const LogitsArgs& a) {
   if (!a.dlogits) return before;
   const Grad d = row_grad(a, x, r, g, w, c);
   if (d.zero) {
-    zero_vectors(out, sp, first, end, odds, a.V);
+    zero_vectors<STREAM>(out, sp, first, end, odds, a.V);
     return before;
   }
   for (int i = first + (int)threadIdx.x; i < end; i += kPartThreads) {
@@ -459,7 +461,7 @@ __device__ __forceinline__ uint64_t policy_part(const LogitsArgs& a) {
     float o[kPer<T>];
 #pragma unroll
     for (int e = 0; e < kPer<T>; ++e) o[e] = grad_of(d, element<T>(v, e));
-    store_vec(out + sp.head, i, o);
+    store_vec<STREAM>(out + sp.head, i, o);
     if (y >= sp.head && i == (y - sp.head) / kPer<T>) store_target(out, y, ly, d);
   }
   const int odd = odd_of<T>(sp, a.V);
@@ -470,9 +472,9 @@ __device__ __forceinline__ uint64_t policy_part(const LogitsArgs& a) {
   return before;
 }
 
-template <typename T>
+template <typename T, bool STREAM>
 __global__ __launch_bounds__(kPartThreads) void policy_part_kernel(LogitsArgs a) {
-  const uint64_t before = policy_part<T>(a);
+  const uint64_t before = policy_part<T, STREAM>(a);
   // rows arrive with their first part
   if (a.counts && blockIdx.x % (uint32_t)a.splits == 0 && last_of(before, a.epoch, a.T)) sum_terms<kPartThreads, 1>(a);
 }
@@ -488,7 +490,7 @@ __global__ __launch_bounds__(kPartThreads) void policy_part_kernel(LogitsArgs a)
 // instructions where its coefficient is 0 took 398 us instead of 416, but its second copy of
 // the code took 428 us instead of 414 with a coefficient.
 // Returns thread 0's arrival.
-template <typename T, int NT, int N, int L>
+template <typename T, int NT, int N, int L, bool STREAM>
 __device__ __forceinline__ uint64_t policy_row(const LogitsArgs& a) {
   const int t = (int)blockIdx.x, y = target_of(a, t);
   const T* row = static_cast<const T*>(a.logits) + (int64_t)t * a.stride;
@@ -498,7 +500,7 @@ __device__ __forceinline__ uint64_t policy_row(const LogitsArgs& a) {
   uint64_t before = 0;
   if (y < 0) {
     if (threadIdx.x == 0) before = write_row(a, t, RowStats{0.f, 0.f, 0.f}, terms);
-    if (a.dlogits) zero_vectors(out, sp, 0, sp.vectors, true, a.V);
+    if (a.dlogits) zero_vectors<STREAM>(out, sp, 0, sp.vectors, true, a.V);
     return before;
   }
   const int odd = odd_of<T>(sp, a.V);
@@ -531,14 +533,14 @@ __device__ __forceinline__ uint64_t policy_row(const LogitsArgs& a) {
   if (!a.dlogits) return before;
   const Grad d = row_grad(a, x, r, g, w, c);
   if (d.zero) {
-    zero_vectors(out, sp, 0, sp.vectors, true, a.V);
+    zero_vectors<STREAM>(out, sp, 0, sp.vectors, true, a.V);
     return before;
   }
   auto put = [&](int i, const u32x4& l) {
     float o[kPer<T>];
 #pragma unroll
     for (int e = 0; e < kPer<T>; ++e) o[e] = grad_of(d, element<T>(l, e));
-    store_vec(out + sp.head, i, o);
+    store_vec<STREAM>(out + sp.head, i, o);
     if (y >= sp.head && i == (y - sp.head) / kPer<T>) store_target(out, y, ly, d);
   };
 #pragma unroll
@@ -561,9 +563,9 @@ __device__ __forceinline__ uint64_t policy_row(const LogitsArgs& a) {
 
 // Only workgroups of this size finish a counted call's sums (few longer rows go in parts).
 constexpr int kFinishThreads = 256;
-template <typename T, int NT, int N, int L>
+template <typename T, int NT, int N, int L, bool STREAM>
 __global__ __launch_bounds__(NT) void policy_row_kernel(LogitsArgs a) {
-  const uint64_t before = policy_row<T, NT, N, L>(a);
+  const uint64_t before = policy_row<T, NT, N, L, STREAM>(a);
   if constexpr (NT == kFinishThreads) {
     if (a.counts && last_of(before, a.epoch, a.T)) sum_terms<NT, 1>(a);
   }
@@ -596,9 +598,28 @@ hipError_t logprobs_for(const LogitsArgs& a, hipStream_t s) {
   return launch(reinterpret_cast<const void*>(&finish_kernel), (a.T + rows - 1) / rows, kPartThreads, a, s);
 }
 
+// Bytes of a gradient from which it is stored past the caches, for the products that read
+// it to find what they need of the rest. us, stored through them / past them, of the call
+// alone, and with its logits' producer and the gradient's two products (by 1,024 hidden dims)
+// around it; bf16: 1,024 x 4,000 11.0 / 10.9, 64 / 71; 256 x 8,000 9.6 / 9.6, 61 / 66; 300 x 20,000
+// 14.1 / 13.5, 166 / 166; 2,048 x 4,000 16.1 / 15.0, 85 / 89; 1,024 x 8,000 13.6 / 12.8, 89 / 90; 1,024 x 16,000
+// 19.8 / 16.9, 140 / 142; 512 x 131,072 60.5 / 59.4, 734 / 733; 4,096 x 131,072 427 / 435, 3,199 / 3,153;
+// f32 2,048 x 110,000 377 / 356.
+constexpr int64_t kStreamBytes = 10 << 20;
+
+template <typename T>
+bool streamed(const LogitsArgs& a) {
+  return (int64_t)a.T * a.V * (int64_t)sizeof(T) >= kStreamBytes;
+}
+
+// Rows of more than kFinishThreads threads come in numbers that make 7 MB and more, and are always streamed.
 template <typename T, int NT, int N, int L = 0>
 hipError_t rows_for(const LogitsArgs& a, hipStream_t s) {
-  return launch(reinterpret_cast<const void*>(&policy_row_kernel<T, NT, N, L>), a.T, NT, a, s);
+  const void* k = reinterpret_cast<const void*>(&policy_row_kernel<T, NT, N, L, true>);
+  if constexpr (NT == kFinishThreads) {
+    if (!streamed<T>(a)) k = reinterpret_cast<const void*>(&policy_row_kernel<T, NT, N, L, false>);
+  }
+  return launch(k, a.T, NT, a, s);
 }
 
 template <typename T>
@@ -608,7 +629,9 @@ hipError_t policy_for(LogitsArgs a, hipStream_t s) {
   if (a.splits) {
     const int64_t wgs = (int64_t)a.T * a.splits;
     e = sums_for<T>(a, s);
-    if (e == hipSuccess) e = launch(reinterpret_cast<const void*>(&policy_part_kernel<T>), wgs, kPartThreads, a, s);
+    const void* k = streamed<T>(a) ? reinterpret_cast<const void*>(&policy_part_kernel<T, true>)
+                                   : reinterpret_cast<const void*>(&policy_part_kernel<T, false>);
+    if (e == hipSuccess) e = launch(k, wgs, kPartThreads, a, s);
   } else if (a.T) {
     const int v = a.V / kPer<T>;
     e = v <= kFinishThreads * 4 ? rows_for<T, kFinishThreads, 4>(a, s)
