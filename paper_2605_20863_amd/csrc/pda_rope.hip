@@ -48,8 +48,7 @@ template <>
 struct Raw<float> {
   u32x4 a, b;
 };
-// STREAM: past the caches, for calls whose tensors are larger than they are (see
-// `few`).
+// STREAM: past the caches (see `few`).
 template <bool STREAM, typename T>
 __device__ __forceinline__ Raw<T> load8(const void* base, int64_t at) {
   const u32x4* p = reinterpret_cast<const u32x4*>(static_cast<const T*>(base) + at);
@@ -867,7 +866,16 @@ bool by_token(const RopeArgs& a) {
   return a.n == 1 || (KV != KvType::FP8 && a.n > 0 && (a.n <= 3 || (int64_t)a.T * a.Hkv <= 1024));
 }
 
-// Few rows a wave where that gives the compute units more waves than few.
+// Few rows a wave where that gives the compute units more waves than few. Calls of
+// more rows also load and store past the caches (the gradient stores). us through them /
+// past them, alone and between the copy that makes the inputs and what reads the results
+// (append: prefill attention; others: a copy); 32 / 8 heads of 128 dims, bf16:
+//   tokens            2,048                4,096                8,192            16,384          32,768
+//   append     12.6 / 11.6, 71.5 / 70.3 19.0 / 21.7, 112 / 113 34.8 / 39.1, 214 / 212 84 / 75, 447 / 428 162 / 147, 1,079 / 1,055
+//   forward    10.1 / 8.3, 25.8 / 25.5  19.0 / 14.8, 44 / 45   33.1 / 31.1, 93 / 92   69 / 61, 204 / 177 130 / 117, 382 / 361
+//   gradient   19.7 / 19.0, 27.4 / 29.2 29.9 / 28.8, 44 / 47   50.9 / 49.0, 96 / 92   108 / 102, 183 / 187 208 / 201, 358 / 365
+// The append's exceptions, around 30 MB of rotated queries, are larger for other types (f32, 2,048 tokens: 19.1 / 23.9;
+// 16 / 4 heads of 64 dims, 16,384 tokens: 20.9 / 24.7, with the attention 152 / 153).
 bool few(const RopeArgs& a, int heads) { return (int64_t)a.T * heads < 65536; }
 
 template <typename T, KvType KV, int D>
