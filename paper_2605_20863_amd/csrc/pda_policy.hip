@@ -283,6 +283,8 @@ __device__ __forceinline__ void sum_terms(const LogitsArgs& a) {
 }
 
 // dl_v = p_v (base + slope x), x = l_v - m, p_v = exp2(x c - log2 s); + at_y for the target.
+// The exponent is rounded to float32, c and log2 s before it: p_v is off by some 2^-24 |x c|, 1e-6 where p_v
+// is e^-20 (a division of the sums' own exponentials would keep 1e-7, and the exponentials a row long).
 struct Grad {
   float m, c, log2_s, base, slope, at_y;
   bool zero;
@@ -337,10 +339,10 @@ __device__ __forceinline__ Soft merge_parts(const LogitsArgs& a, int t, float c)
 // Workgroup (row, part). A whole row's log-probability and entropy are written;
 // of a part, or for policy_part_kernel, the sums. With counts the last part's
 // workgroup of a row finishes it.
-// 8192 x 131,072 bf16: 335 us, 6.4 TB/s, where the vector ALUs are busy for 92% of
-// the cycles (9 instructions an element, an exponential of twice the cycles among
+// 8192 x 131,072 bf16: 333 us, 6.4 TB/s, where the vector ALUs are busy for 97% of
+// the cycles (9.4 instructions an element, an exponential of twice the cycles among
 // them). Largest values of bf16 pairs by packed integer maxima, 5% fewer instructions, gave
-// nothing (332).
+// nothing.
 template <typename T, int U, bool STREAM>
 __global__ __launch_bounds__(kPartThreads) void sums_kernel(LogitsArgs a) {
   const int t = (int)(blockIdx.x / (uint32_t)a.splits), p = (int)(blockIdx.x - (uint32_t)t * a.splits);
@@ -484,9 +486,9 @@ __global__ __launch_bounds__(kPartThreads) void policy_part_kernel(LogitsArgs a)
 // Workgroup per row, whose vectors stay in its threads' registers (N of a thread)
 // and LDS (L of a thread) between the sums and the gradient: one read and one
 // write of the row.
-// 4096 x 131,072 bf16: 415 us, 5.2 TB/s (a 2 GiB device copy: 5.0). A long row's
+// 4096 x 131,072 bf16: 418 us with the rows' sum, 5.1 TB/s (a 2 GiB device copy: 5.0). A long row's
 // workgroup fills its compute unit, so its reads, sums and writes follow one another; the
-// vector ALUs are busy for 64% of the cycles. The gradient without the entropy's
+// vector ALUs are busy for 69% of the cycles. The gradient without the entropy's
 // instructions where its coefficient is 0 took 398 us instead of 416, but its second copy of
 // the code took 428 us instead of 414 with a coefficient.
 // Returns thread 0's arrival.
