@@ -1,40 +1,11 @@
 // Host side of include/pda_ops.h: argument checks (host code only, before any
 // HIP call), the split of the work, and the launches.
 
-#include "pda_ops.h"
-#include "pda_host.h"
-#include "pda_ops_internal.h"
-
-#include <cmath>
-#include <initializer_list>
-#include <new>
+#include "pda_checks.h"
 
 namespace {
 
-using pda::host_fail;
-
-constexpr int64_t kMaxWaves = 1 << 26;  // a launch has below 2^32 threads
-constexpr int64_t kHeader = 256;        // bytes of the workspace's header
-static_assert(pda::kHdrWords * 4 <= kHeader, "header");
-
-struct Ptr {
-  const void* p;
-  uintptr_t align;
-  const char* name;
-  bool required;
-};
-
-int check_pointers(std::initializer_list<Ptr> ptrs) {
-  for (const Ptr& x : ptrs) {
-    if (x.required && !x.p) return host_fail(PDA_EINVAL, "%s is NULL", x.name);
-    if (reinterpret_cast<uintptr_t>(x.p) % x.align)
-      return host_fail(PDA_EINVAL, "%s is not %d-byte aligned", x.name, (int)x.align);
-  }
-  return PDA_OK;
-}
-
-bool float_type(int t) { return t == PDA_DTYPE_F32 || t == PDA_DTYPE_BF16; }
-int size_of(int t) { return t == PDA_DTYPE_F32 ? 4 : 2; }
+using namespace pda;
 
 // *out: the stride in elements; rows of `heads` heads must not overlap and stay 16-byte aligned.
 int check_stride(const char* name, int64_t stride, int heads, int d, int type, int64_t tokens, int64_t* out) {
@@ -47,7 +18,7 @@ int check_stride(const char* name, int64_t stride, int heads, int d, int type, i
   return PDA_OK;
 }
 
-int check_rope(const pdaops_rope_problem* pr, bool has_q_weight, bool has_k_weight, bool with_v, pda::RopeArgs* a) {
+int check_rope(const pdaops_rope_problem* pr, bool has_q_weight, bool has_k_weight, bool with_v, RopeArgs* a) {
   if (!pr) return host_fail(PDA_EINVAL, "problem is NULL");
   if (pr->num_tokens < 0) return host_fail(PDA_EINVAL, "num_tokens = %d < 0", pr->num_tokens);
   if (pr->num_q_heads < 1 || pr->num_kv_heads < 1)
@@ -94,36 +65,24 @@ int check_rope(const pdaops_rope_problem* pr, bool has_q_weight, bool has_k_weig
   return PDA_OK;
 }
 
-// Arrival counts for the call, unless it is captured.
-template <typename Args>
-int count(hipStream_t s, const pda::HeldWorkspace& ws, Args* a) {
-  pda::Counts c;
-  const int rc = pda::take_counts(s, ws, &c);
-  a->counts = c.words;
-  a->epoch = c.epoch;
-  return rc;
-}
-
-int32_t* status_word(char* base) { return reinterpret_cast<int32_t*>(base) + pda::kHdrStatus; }
-
 int append_run(const void* q, const void* k, const void* v, const void* q_weight, const void* k_weight,
                const float* cos_sin, const int32_t* positions, const int32_t* q_offsets, void* q_out, void* k_cache,
                void* v_cache, float* kv_scales, const int32_t* block_table, const int32_t* seq_lens,
                const pdaops_rope_problem* pr, const pdaops_cache* ca, hipStream_t stream) {
-  pda::host_clear_error();
-  pda::RopeArgs a = {};
+  host_clear_error();
+  RopeArgs a = {};
   int rc = check_rope(pr, q_weight != nullptr, k_weight != nullptr, true, &a);
   if (rc != PDA_OK) return rc;
   if (!ca) return host_fail(PDA_EINVAL, "cache is NULL");
   if (ca->num_seqs < 0) return host_fail(PDA_EINVAL, "num_seqs = %d < 0", ca->num_seqs);
-  if (ca->block_size != pda::kBlockSize) return host_fail(PDA_EUNSUPPORTED, "block_size = %d (supported: 16)", ca->block_size);
+  if (ca->block_size != kBlockSize) return host_fail(PDA_EUNSUPPORTED, "block_size = %d (supported: 16)", ca->block_size);
   if (ca->max_blocks_per_seq < 1) return host_fail(PDA_EINVAL, "max_blocks_per_seq = %d < 1", ca->max_blocks_per_seq);
   if (ca->num_blocks < 1) return host_fail(PDA_EINVAL, "num_blocks = %lld < 1", (long long)ca->num_blocks);
-  const int64_t table_tokens = (int64_t)ca->max_blocks_per_seq * pda::kBlockSize;
+  const int64_t table_tokens = (int64_t)ca->max_blocks_per_seq * kBlockSize;
   if (table_tokens > INT32_MAX) return host_fail(PDA_EINVAL, "max_blocks_per_seq * 16 overflows int32");
   if (ca->max_seq_len < 0 || ca->max_seq_len > table_tokens)
     return host_fail(PDA_EINVAL, "max_seq_len = %d (0 .. max_blocks_per_seq * 16 = %lld)", ca->max_seq_len, (long long)table_tokens);
-  const int64_t tile = (int64_t)pda::kBlockSize * a.D * 4;
+  const int64_t tile = (int64_t)kBlockSize * a.D * 4;
   if (ca->num_blocks > INT64_MAX / a.Hkv / tile) return host_fail(PDA_EINVAL, "num_blocks too large");
   const int kd = ca->kv_dtype;
   if (!float_type(kd) && kd != PDA_DTYPE_FP8_E4M3) return host_fail(PDA_EINVAL, "kv_dtype = %d is not a pda_dtype", kd);
@@ -146,8 +105,8 @@ int append_run(const void* q, const void* k, const void* v, const void* q_weight
                        {block_table, 4, "block_table", true}, {seq_lens, 4, "seq_lens", true}});
   if (rc != PDA_OK) return rc;
 
-  pda::HeldWorkspace ws;
-  if ((rc = pda::hold_workspace(stream, kHeader, &ws)) != PDA_OK) return rc;
+  HeldWorkspace ws;
+  if ((rc = hold_workspace(stream, kHeader, &ws)) != PDA_OK) return rc;
   a.q = q;
   a.k = k;
   a.v = v;
@@ -168,15 +127,15 @@ int append_run(const void* q, const void* k, const void* v, const void* q_weight
   a.len_cap = ca->max_seq_len > 0 ? ca->max_seq_len : (int32_t)table_tokens;
   a.num_blocks = ca->num_blocks;
   a.tiles = (int32_t)tiles;
-  const pda::KvType kv = kd == PDA_DTYPE_F32 ? pda::KvType::F32 : kd == PDA_DTYPE_BF16 ? pda::KvType::BF16 : pda::KvType::FP8;
-  const hipError_t e = pda::launch_rope_append(a, kv, stream);
-  return e == hipSuccess ? PDA_OK : pda::host_fail_hip(e, "norm, rotation and append kernel launch");
+  const KvType kv = kd == PDA_DTYPE_F32 ? KvType::F32 : kd == PDA_DTYPE_BF16 ? KvType::BF16 : KvType::FP8;
+  const hipError_t e = launch_rope_append(a, kv, stream);
+  return e == hipSuccess ? PDA_OK : host_fail_hip(e, "norm, rotation and append kernel launch");
 }
 
 int rope_run(const void* q, const void* k, const void* q_weight, const void* k_weight, const float* cos_sin,
              const int32_t* positions, void* q_out, void* k_out, const pdaops_rope_problem* pr, hipStream_t stream) {
-  pda::host_clear_error();
-  pda::RopeArgs a = {};
+  host_clear_error();
+  RopeArgs a = {};
   int rc = check_rope(pr, q_weight != nullptr, k_weight != nullptr, false, &a);
   if (rc != PDA_OK) return rc;
   if (a.T == 0) return PDA_OK;
@@ -184,8 +143,8 @@ int rope_run(const void* q, const void* k, const void* q_weight, const void* k_w
                        {k_weight, 16, "k_weight", false}, {cos_sin, 16, "cos_sin", true}, {positions, 4, "positions", true},
                        {q_out, 16, "q_out", true}, {k_out, 16, "k_out", true}});
   if (rc != PDA_OK) return rc;
-  pda::HeldWorkspace ws;
-  if ((rc = pda::hold_workspace(stream, kHeader, &ws)) != PDA_OK) return rc;
+  HeldWorkspace ws;
+  if ((rc = hold_workspace(stream, kHeader, &ws)) != PDA_OK) return rc;
   a.q = q;
   a.k = k;
   a.wq = q_weight;
@@ -195,16 +154,16 @@ int rope_run(const void* q, const void* k, const void* q_weight, const void* k_w
   a.q_out = q_out;
   a.k_out = k_out;
   a.status = status_word(ws.base);
-  const hipError_t e = pda::launch_rope(a, stream);
-  return e == hipSuccess ? PDA_OK : pda::host_fail_hip(e, "norm and rotation kernel launch");
+  const hipError_t e = launch_rope(a, stream);
+  return e == hipSuccess ? PDA_OK : host_fail_hip(e, "norm and rotation kernel launch");
 }
 
 int rope_backward_run(const void* q, const void* k, const void* q_weight, const void* k_weight, const float* cos_sin,
                       const int32_t* positions, const void* grad_q_out, const void* grad_k_out, void* grad_q,
                       void* grad_k, float* grad_q_weight, float* grad_k_weight, const pdaops_rope_problem* pr,
                       hipStream_t stream) {
-  pda::host_clear_error();
-  pda::RopeArgs a = {};
+  host_clear_error();
+  RopeArgs a = {};
   int rc = check_rope(pr, q_weight != nullptr, k_weight != nullptr, false, &a);
   if (rc != PDA_OK) return rc;
   if (pr->out_dtype != pr->dtype)
@@ -218,11 +177,11 @@ int rope_backward_run(const void* q, const void* k, const void* q_weight, const 
                        {grad_q, 16, "grad_q", any}, {grad_k, 16, "grad_k", any},
                        {grad_q_weight, 4, "grad_q_weight", norm}, {grad_k_weight, 4, "grad_k_weight", norm}});
   if (rc != PDA_OK) return rc;
-  pda::HeldWorkspace ws;
+  HeldWorkspace ws;
   // parts of the weights' gradients: at most as many workgroups as there are tokens' parts
   constexpr int64_t kWgsPerCu = 4, kMostCus = 1024;
   const int64_t part = 2 * (int64_t)a.D * 4;
-  if ((rc = pda::hold_workspace(stream, kHeader + (norm ? kWgsPerCu * kMostCus * part : 0), &ws)) != PDA_OK) return rc;
+  if ((rc = hold_workspace(stream, kHeader + (norm ? kWgsPerCu * kMostCus * part : 0), &ws)) != PDA_OK) return rc;
   a.q = q;
   a.k = k;
   a.wq = q_weight;
@@ -241,53 +200,14 @@ int rope_backward_run(const void* q, const void* k, const void* q_weight, const 
   a.wgs = (int32_t)kWgsPerCu * (ws.cus < kMostCus ? ws.cus : (int32_t)kMostCus);
   if (norm && (rc = count(stream, ws, &a)) != PDA_OK) return rc;
   a.status = status_word(ws.base);
-  const hipError_t e = pda::launch_rope_backward(a, stream);
-  return e == hipSuccess ? PDA_OK : pda::host_fail_hip(e, "norm and rotation gradient kernel launch");
-}
-
-int check_logits(const pdaops_logits_problem* pr, pda::LogitsArgs* a) {
-  if (!pr) return host_fail(PDA_EINVAL, "problem is NULL");
-  if (pr->num_tokens < 0) return host_fail(PDA_EINVAL, "num_tokens = %d < 0", pr->num_tokens);
-  if (pr->vocab < 1 || pr->vocab > (1 << 30)) return host_fail(PDA_EINVAL, "vocab = %d (1 .. 2^30)", pr->vocab);
-  if (!float_type(pr->dtype)) return host_fail(PDA_EINVAL, "dtype = %d (supported: F32, BF16)", pr->dtype);
-  if (pr->targets_int64 != 0 && pr->targets_int64 != 1) return host_fail(PDA_EINVAL, "targets_int64 = %d (0 or 1)", pr->targets_int64);
-  a->stride = pr->row_stride ? pr->row_stride : pr->vocab;
-  if (a->stride < pr->vocab || a->stride > INT64_MAX / 8 / (pr->num_tokens + 1ll))
-    return host_fail(PDA_EINVAL, "row_stride = %lld", (long long)pr->row_stride);
-  if (!(pr->temperature > 0.f) || !std::isfinite(pr->temperature) || !std::isfinite(1.f / pr->temperature))
-    return host_fail(PDA_EINVAL, "temperature must be positive and finite");
-  a->T = pr->num_tokens;
-  a->V = pr->vocab;
-  a->bf16 = pr->dtype == PDA_DTYPE_BF16;
-  a->targets64 = pr->targets_int64;
-  a->inv_temp = 1.f / pr->temperature;
-  return PDA_OK;
-}
-
-// Whole 16-byte vectors of a row.
-int vectors_of(const pda::LogitsArgs& a) { return a.bf16 ? a.V / 8 : a.V / 4; }
-
-// Parts per row: enough workgroups for the compute units, of at least 512 vectors
-// (two for each thread) each. Half or twice as many workgroups, or least vectors, are
-// within 10% on every size tried (1 to 3,000 rows of 8,000 to 150,000 words) but for
-// rows of 8,000 words, which 256 vectors a part cut in two: 5.3 - 9.3 us per call, 4.2 - 7.1 whole.
-void split_rows(pda::LogitsArgs* a) {
-  constexpr int64_t kWgs = 1024, kLeast = 512;
-  const int64_t v = vectors_of(*a);
-  int64_t s = (kWgs + a->T - 1) / a->T;
-  if (s > v / kLeast) s = v / kLeast;
-  if (s > pda::kMaxSplits) s = pda::kMaxSplits;
-  if (s < 1) s = 1;
-  a->chunk = (int32_t)((v + s - 1) / s);
-  if (a->chunk < 1) a->chunk = 1;
-  a->splits = (int32_t)((v + a->chunk - 1) / a->chunk);
-  if (a->splits < 1) a->splits = 1;
+  const hipError_t e = launch_rope_backward(a, stream);
+  return e == hipSuccess ? PDA_OK : host_fail_hip(e, "norm and rotation gradient kernel launch");
 }
 
 int logprobs_run(const void* logits, const void* targets, float* logprobs, float* entropy,
                  const pdaops_logits_problem* pr, hipStream_t stream) {
-  pda::host_clear_error();
-  pda::LogitsArgs a = {};
+  host_clear_error();
+  LogitsArgs a = {};
   int rc = check_logits(pr, &a);
   if (rc != PDA_OK) return rc;
   if (a.T == 0) return PDA_OK;
@@ -296,24 +216,24 @@ int logprobs_run(const void* logits, const void* targets, float* logprobs, float
   if (rc != PDA_OK) return rc;
   split_rows(&a);
   if ((int64_t)a.T * a.splits > kMaxWaves / 16) return host_fail(PDA_EINVAL, "num_tokens = %d is too much for one call", a.T);
-  pda::HeldWorkspace ws;
-  if ((rc = pda::hold_workspace(stream, kHeader + (a.splits > 1 ? (int64_t)a.T * a.splits * 16 : 0), &ws)) != PDA_OK) return rc;
+  HeldWorkspace ws;
+  if ((rc = hold_workspace(stream, kHeader + (a.splits > 1 ? (int64_t)a.T * a.splits * 16 : 0), &ws)) != PDA_OK) return rc;
   a.logits = logits;
   a.targets = targets;
   a.logp = logprobs;
   a.ent = entropy;
   a.part = reinterpret_cast<float4*>(ws.base + kHeader);
   a.status = status_word(ws.base);
-  if (a.splits > 1 && a.T <= pda::kShortUnits && (rc = count(stream, ws, &a)) != PDA_OK) return rc;
-  const hipError_t e = pda::launch_token_logprobs(a, stream);
-  return e == hipSuccess ? PDA_OK : pda::host_fail_hip(e, "log-probability kernel launch");
+  if (a.splits > 1 && a.T <= kShortUnits && (rc = count(stream, ws, &a)) != PDA_OK) return rc;
+  const hipError_t e = launch_token_logprobs(a, stream);
+  return e == hipSuccess ? PDA_OK : host_fail_hip(e, "log-probability kernel launch");
 }
 
 int policy_run(const void* logits, const void* targets, const float* old_logprobs, const float* ref_logprobs,
                const float* advantages, const float* weights, float* stats, void* dlogits, float* logprobs,
                float* entropy, const pdaops_logits_problem* pr, const pdaops_policy_options* op, hipStream_t stream) {
-  pda::host_clear_error();
-  pda::LogitsArgs a = {};
+  host_clear_error();
+  LogitsArgs a = {};
   int rc = check_logits(pr, &a);
   if (rc != PDA_OK) return rc;
   if (!op) return host_fail(PDA_EINVAL, "options is NULL");
@@ -345,10 +265,10 @@ int policy_run(const void* logits, const void* targets, const float* old_logprob
   // 11.2 / 12.5; f32: 64 of 50,001 14.6 / 12.5, 128 15.5 / 16.1; 128 of 110,000 31 / 34, 2,048 348 / 523).
   constexpr int kManyBf16 = 160, kManyF32 = 112, kShortVectors = 3200;
   const int v = vectors_of(a);
-  if (any && ((a.T < (a.bf16 ? kManyBf16 : kManyF32) && v > kShortVectors) || v > pda::kRowVectors)) split_rows(&a);
-  const int64_t terms = ((int64_t)a.T * pda::kTerms * 4 + 255) / 256 * 256;
-  pda::HeldWorkspace ws;
-  if ((rc = pda::hold_workspace(stream, kHeader + terms + (int64_t)a.T * a.splits * 16, &ws)) != PDA_OK) return rc;
+  if (any && ((a.T < (a.bf16 ? kManyBf16 : kManyF32) && v > kShortVectors) || v > kRowVectors)) split_rows(&a);
+  const int64_t terms = ((int64_t)a.T * kTerms * 4 + 255) / 256 * 256;
+  HeldWorkspace ws;
+  if ((rc = hold_workspace(stream, kHeader + terms + (int64_t)a.T * a.splits * 16, &ws)) != PDA_OK) return rc;
   a.logits = logits;
   a.targets = targets;
   a.logp = logprobs;
@@ -368,23 +288,9 @@ int policy_run(const void* logits, const void* targets, const float* old_logprob
   a.terms = reinterpret_cast<float*>(ws.base + kHeader);
   a.part = reinterpret_cast<float4*>(ws.base + kHeader + terms);
   a.status = status_word(ws.base);
-  if (any && a.T <= pda::kCountedRows && (rc = count(stream, ws, &a)) != PDA_OK) return rc;
-  const hipError_t h = pda::launch_policy_loss(a, stream);
-  return h == hipSuccess ? PDA_OK : pda::host_fail_hip(h, "policy loss kernel launch");
-}
-
-// A C entry: what is thrown below it (no memory for the workspace's record, a
-// failed lock) becomes an error code with a text, of at most 15 characters: a
-// std::string holds these without memory of its own.
-template <typename F>
-int entry(F run) {
-  try {
-    return run();
-  } catch (const std::bad_alloc&) {
-    return host_fail(PDA_ENOMEM, "no host memory");
-  } catch (...) {
-    return host_fail(PDA_EHIP, "host exception");
-  }
+  if (any && a.T <= kCountedRows && (rc = count(stream, ws, &a)) != PDA_OK) return rc;
+  const hipError_t h = launch_policy_loss(a, stream);
+  return h == hipSuccess ? PDA_OK : host_fail_hip(h, "policy loss kernel launch");
 }
 
 }  // namespace
