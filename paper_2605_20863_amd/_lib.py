@@ -1,4 +1,4 @@
-"""ctypes binding of the C interface in include/pda.h and include/pda_ops.h.
+"""ctypes binding of the C interface in include/pda.h, include/pda_ops.h and include/pda_lm.h.
 
 Argument marshalling only: every step of the decode attention, KV append,
 prefill and the operators around them runs in the HIP library ``libpda.so``. Importing this module fails loudly when the
@@ -20,6 +20,7 @@ _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.environ.get("PDA_LIBRARY") or os.path.join(_PKG, "libpda.so")
 HEADER_PATH = os.path.join(os.path.dirname(_PKG), "include", "pda.h")
 OPS_HEADER_PATH = os.path.join(os.path.dirname(_PKG), "include", "pda_ops.h")
+LM_HEADER_PATH = os.path.join(os.path.dirname(_PKG), "include", "pda_lm.h")
 
 if not os.path.exists(LIB_PATH):
     raise ImportError(
@@ -44,8 +45,8 @@ if _torch_rt is not None:
     try:
         from . import _pda_torch
     except ImportError as e:  # not built, or for a torch of another ABI
-        warnings.warn(f"_pda_torch does not load ({e}); calls of include/pda_ops.h take some microseconds more host "
-                      "time each until python -m paper_2605_20863_amd.build has built it", RuntimeWarning)
+        warnings.warn(f"_pda_torch does not load ({e}); calls of include/pda_ops.h and pda_lm.h take some "
+                      "microseconds more host time each until python -m paper_2605_20863_amd.build has built it", RuntimeWarning)
 
 # pda_dtype / pda_status / pda_variant
 F32, BF16, FP8_E4M3 = 0, 1, 2
@@ -54,9 +55,12 @@ VARIANT_AUTO, VARIANT_VECTOR, VARIANT_MFMA = 0, 1, 2
 _VARIANTS = {"auto": VARIANT_AUTO, "vector": VARIANT_VECTOR, "mfma": VARIANT_MFMA}
 STATUS_LEN_CLAMPED, STATUS_BAD_BLOCK, STATUS_PREFIX_SHORTENED, STATUS_BAD_OFFSETS = 1, 2, 4, 8
 STATUS_HALF_RANGE = 16
-STATUS_BAD_POSITION, STATUS_BAD_TARGET = 32, 64
+STATUS_BAD_POSITION, STATUS_BAD_TARGET, STATUS_TWICE = 32, 64, 128
 # "old_kl" is e^-d - 1 + d of the log ratio d: include/pda_ops.h says what its mean estimates.
 POLICY_STATS = ("loss", "policy", "kl", "entropy", "clipped", "ratio", "old_kl", "weight")
+# Sums over rows of weights times these; the masses are the list's under the teacher and under the student.
+DISTILL_STATS = ("loss", "forward", "reverse", "teacher_mass", "student_mass", "weight")
+MAX_TOP = 256   # PDALM_MAX_TOP
 NOALLOC_SCRATCH_BYTES = 32 << 20   # PDA_NOALLOC_SCRATCH_BYTES
 
 
@@ -184,6 +188,32 @@ class PolicyOptions(ctypes.Structure):
     ]
 
 
+class NormProblem(ctypes.Structure):
+    _fields_ = [
+        ("num_tokens", ctypes.c_int32),
+        ("width", ctypes.c_int32),
+        ("dtype", ctypes.c_int32),
+        ("out_dtype", ctypes.c_int32),
+        ("weight_dtype", ctypes.c_int32),
+        ("scale_group", ctypes.c_int32),
+        ("eps", ctypes.c_float),
+        ("x_stride", ctypes.c_int64),
+        ("residual_stride", ctypes.c_int64),
+        ("sum_stride", ctypes.c_int64),
+        ("out_stride", ctypes.c_int64),
+    ]
+
+
+class DistillOptions(ctypes.Structure):
+    _fields_ = [
+        ("num_listed", ctypes.c_int32),
+        ("rest", ctypes.c_int32),
+        ("reverse", ctypes.c_float),
+        ("grad_scale", ctypes.c_float),
+        ("dlogits_stride", ctypes.c_int64),
+    ]
+
+
 _vp = ctypes.c_void_p
 _lib.pda_paged_decode_attention.argtypes = [_vp, _vp, _vp, _vp, _vp, _vp, _vp, ctypes.c_float,
                                             ctypes.POINTER(Problem), ctypes.POINTER(Options), _vp]
@@ -213,22 +243,28 @@ _lib.pda_last_error.argtypes = []
 _lib.pda_last_error.restype = ctypes.c_char_p
 _lib.pda_version.argtypes = []
 _lib.pda_version.restype = ctypes.c_int
-# include/pda_ops.h. PDA_LIBRARY may name a build of the host code behind pda.h
-# alone; a call of one of these then fails for want of its symbol.
-_rope, _logits = ctypes.POINTER(RopeProblem), ctypes.POINTER(LogitsProblem)
+# include/pda_ops.h and include/pda_lm.h. PDA_LIBRARY may name a build of the host code behind
+# pda.h alone; a call of one of these then fails for want of its symbol.
+_rope, _logits, _norm = ctypes.POINTER(RopeProblem), ctypes.POINTER(LogitsProblem), ctypes.POINTER(NormProblem)
 for _name, _args in (
         ("pdaops_paged_qk_norm_rope_append", [_vp] * 14 + [_rope, ctypes.POINTER(Cache), _vp]),
         ("pdaops_qk_norm_rope", [_vp] * 8 + [_rope, _vp]),
         ("pdaops_qk_norm_rope_backward", [_vp] * 12 + [_rope, _vp]),
         ("pdaops_token_logprobs", [_vp] * 4 + [_logits, _vp]),
-        ("pdaops_policy_loss", [_vp] * 10 + [_logits, ctypes.POINTER(PolicyOptions), _vp])):
+        ("pdaops_policy_loss", [_vp] * 10 + [_logits, ctypes.POINTER(PolicyOptions), _vp]),
+        ("pdalm_add_rms_norm", [_vp] * 6 + [_norm, _vp]),
+        ("pdalm_add_rms_norm_backward", [_vp] * 6 + [_norm, _vp]),
+        ("pdalm_top_logprobs", [_vp] * 6 + [_logits, ctypes.c_int32, _vp]),
+        ("pdalm_distill_loss", [_vp] * 7 + [_logits, ctypes.POINTER(DistillOptions), _vp])):
     if hasattr(_lib, _name):
         getattr(_lib, _name).argtypes = _args
         getattr(_lib, _name).restype = ctypes.c_int
 # The torch module's functions with the addresses of their entries.
-_calls = {n: (getattr(_pda_torch, n), ctypes.cast(getattr(_lib, "pdaops_" + n), _vp).value) for n in (
-    "paged_qk_norm_rope_append", "qk_norm_rope", "qk_norm_rope_backward", "token_logprobs", "policy_loss")
-    if _pda_torch is not None and hasattr(_lib, "pdaops_" + n)}
+_calls = {n: (getattr(_pda_torch, n), ctypes.cast(getattr(_lib, p + n), _vp).value) for p, n in (
+    ("pdaops_", "paged_qk_norm_rope_append"), ("pdaops_", "qk_norm_rope"), ("pdaops_", "qk_norm_rope_backward"),
+    ("pdaops_", "token_logprobs"), ("pdaops_", "policy_loss"), ("pdalm_", "add_rms_norm"),
+    ("pdalm_", "add_rms_norm_backward"), ("pdalm_", "top_logprobs"), ("pdalm_", "distill_loss"))
+    if hasattr(_pda_torch, n) and hasattr(_lib, p + n)}
 
 
 class PdaError(RuntimeError):
@@ -254,6 +290,11 @@ def header_symbols():
 def ops_header_symbols():
     """Names of the functions include/pda_ops.h declares."""
     return sorted(set(re.findall(r"^int (pdaops_\w+)\s*\(", open(OPS_HEADER_PATH).read(), re.M)))
+
+
+def lm_header_symbols():
+    """Names of the functions include/pda_lm.h declares."""
+    return sorted(set(re.findall(r"^int (pdalm_\w+)\s*\(", open(LM_HEADER_PATH).read(), re.M)))
 
 
 def _check(rc):
@@ -874,6 +915,162 @@ def policy_loss(logits, targets, old_logprobs, advantages, weights, stats, dlogi
             _ptr(ref_logprobs), advantages.data_ptr(), weights.data_ptr(), stats.data_ptr(), _ptr(dlogits), _ptr(logprobs),
             _ptr(entropy), pr,
             PolicyOptions(clip_low, clip_high, dual_clip, kl_coef, entropy_coef, grad_scale, step))
+    return stats
+
+
+def _wide(t, name, shape=None, dtype=None):
+    """Elements between the rows of t [T, H], whose elements must be contiguous (0: one row)."""
+    s = t.shape
+    if len(s) != 2 or (shape is not None and s != shape):
+        raise ValueError(f"{name} must be {'[tokens, width]' if shape is None else tuple(shape)}, got {tuple(s)}")
+    if dtype is not None and t.dtype is not dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    step, one = t.stride()
+    if one != 1 and s[1] > 1:
+        raise ValueError(f"{name}: rows must be contiguous")
+    if s[0] <= 1:
+        return 0
+    if step < s[1]:
+        raise ValueError(f"{name}: rows must not overlap (an expanded tensor needs .contiguous())")
+    return step
+
+
+def add_rms_norm(x, weight, out, residual=None, residual_out=None, scales=None, eps=1e-6, stream=None):
+    """Enqueue the residual stream's root-mean-square norm.
+
+    x [T, H] (and ``residual`` [T, H], added to it first) float32 or bfloat16; the sum,
+    rounded to x's dtype, goes to ``residual_out`` [T, H] unless None (x or residual
+    itself will do); ``weight`` [H] float32 or bfloat16. ``out`` [T, H] is float32,
+    bfloat16, or float8_e4m3fn (or uint8) with ``scales`` float32 [T, H / 64], [T, H / 128], or
+    [T] or [T, 1]: one scale for each group of neighbours, or each row; out * scales
+    stands for the norm. Rows of all but weight and scales may be apart.
+    """
+    if _direct("add_rms_norm", x, stream, x, weight, out, residual, residual_out, scales, eps) == OK:
+        return out
+    index = x.get_device()
+    strided = {"x": x, "out": out, "residual": residual, "residual_out": residual_out}
+    packed = {"weight": weight, "scales": scales}
+    if _apart(index, strided.values(), packed.values()):
+        _refuse(index, strided, packed)
+    steps = [_wide(x, "x")]
+    T, H = x.shape
+    for name, t in (("residual", residual), ("residual_out", residual_out)):
+        steps.append(0 if t is None else _wide(t, name, x.shape, x.dtype))
+    steps.append(_wide(out, "out", x.shape))
+    if weight.shape != (H,):
+        raise ValueError("weight must be [width]")
+    code, group = _dtype_code(out, "out"), 0
+    if code == FP8_E4M3:
+        if scales is None or scales.dtype is not _FLOAT32 or scales.dim() not in (1, 2) or scales.shape[0] != T:
+            raise ValueError("an fp8 out needs float32 scales [tokens] or [tokens, groups]")
+        n = scales.shape[1] if scales.dim() == 2 else 1
+        if n < 1 or H % n:
+            raise ValueError(f"scales: {n} groups do not divide the width {H}")
+        group = H // n if n > 1 else 0
+    elif scales is not None:
+        raise ValueError("scales are for an fp8 out")
+    _launch(_lib.pdalm_add_rms_norm, index, stream, x.data_ptr(), _ptr(residual), weight.data_ptr(), _ptr(residual_out),
+            out.data_ptr(), _ptr(scales),
+            NormProblem(T, H, _float_code(x, "x"), code, _float_code(weight, "weight"), group, eps, *steps))
+    return out
+
+
+def add_rms_norm_backward(h, weight, grad_out, grad_h, grad_weight=None, grad_residual=None, eps=1e-6, stream=None):
+    """Enqueue the gradient of add_rms_norm at ``h`` [T, H] (its residual_out, or its x
+    without residual): ``grad_h`` (the gradient of x and of residual alike; h's dtype)
+    from ``grad_out`` and, unless None, ``grad_residual``, that of residual_out; and
+    ``grad_weight`` [H] float32 unless None, which is written, not added to."""
+    if _direct("add_rms_norm_backward", h, stream, h, weight, grad_out, grad_h, grad_weight, grad_residual, eps) == OK:
+        return grad_h
+    index = h.get_device()
+    strided = {"h": h, "grad_out": grad_out, "grad_h": grad_h, "grad_residual": grad_residual}
+    packed = {"weight": weight, "grad_weight": grad_weight}
+    if _apart(index, strided.values(), packed.values()):
+        _refuse(index, strided, packed)
+    step = _wide(h, "h")
+    (T, H), dt = h.shape, h.dtype
+    steps = [0 if t is None else _wide(t, name, h.shape, dt) for name, t in
+             (("grad_residual", grad_residual), ("grad_h", grad_h), ("grad_out", grad_out))]
+    if weight.shape != (H,):
+        raise ValueError("weight must be [width]")
+    if grad_weight is not None and (grad_weight.shape != (H,) or grad_weight.dtype is not _FLOAT32):
+        raise ValueError("grad_weight must be float32 [width]")
+    code = _float_code(h, "h")
+    _launch(_lib.pdalm_add_rms_norm_backward, index, stream, h.data_ptr(), weight.data_ptr(), grad_out.data_ptr(),
+            _ptr(grad_residual), grad_h.data_ptr(), _ptr(grad_weight),
+            NormProblem(T, H, code, code, _float_code(weight, "weight"), 0, eps, step, *steps))
+    return grad_h
+
+
+def _lists(ids, logprobs, T, names):
+    """Places of the lists ids int32 and logprobs float32, both [T, K]."""
+    if ids.dim() != 2 or ids.shape[0] != T or ids.dtype is not _INT32:
+        raise ValueError(f"{names[0]} must be int32 [tokens, places]")
+    if logprobs.shape != ids.shape or logprobs.dtype is not _FLOAT32:
+        raise ValueError(f"{names[1]} must be float32, of {names[0]}' shape")
+    return ids.shape[1]
+
+
+def top_logprobs(logits, top_ids, top_logprobs, targets=None, logprobs=None, entropy=None, temperature=1.0, stream=None):
+    """Enqueue the most likely words of every row of logits [T, V] / temperature, the
+    likeliest first: ``top_ids`` int32 [T, K] and ``top_logprobs`` float32 [T, K], K up to
+    MAX_TOP (equal logits in the order of their words; -1 and -inf where no word is
+    left); and as token_logprobs the log-probabilities of ``targets`` [T] (negative: a
+    row that takes no part) and the rows' entropies, float32 [T], each unless None."""
+    if _direct("top_logprobs", logits, stream, logits, top_ids, top_logprobs, targets, logprobs, entropy, temperature) == OK:
+        return top_ids, top_logprobs
+    index = logits.get_device()
+    packed = {"top_ids": top_ids, "top_logprobs": top_logprobs, "targets": targets, "logprobs": logprobs, "entropy": entropy}
+    if _apart(index, (logits,), packed.values()):
+        _refuse(index, {"logits": logits}, packed)
+    if targets is not None:
+        pr = _logits_problem(logits, targets, temperature)
+    elif logprobs is not None:
+        raise ValueError("logprobs are of targets")
+    else:
+        step = _row_step(logits, "logits")
+        pr = LogitsProblem(*logits.shape, step, _float_code(logits, "logits"), 0, temperature)
+    places = _lists(top_ids, top_logprobs, pr.num_tokens, ("top_ids", "top_logprobs"))
+    _rows(pr.num_tokens, (logprobs, entropy))
+    _launch(_lib.pdalm_top_logprobs, index, stream, logits.data_ptr(), _ptr(targets), top_ids.data_ptr(),
+            top_logprobs.data_ptr(), _ptr(logprobs), _ptr(entropy), pr, places)
+    return top_ids, top_logprobs
+
+
+def distill_loss(logits, teacher_ids, teacher_logprobs, weights, stats, dlogits=None, losses=None, reverse=0.0, rest=True,
+                 temperature=1.0, grad_scale=1.0, stream=None):
+    """Enqueue the distillation loss of the student's logits [T, V] from a teacher's
+    lists (as top_logprobs writes them: teacher_ids int32 [T, K], -1 an empty place, and
+    teacher_logprobs float32 [T, K]) and its gradient at the logits.
+
+    A row's loss is (1 - reverse) KL(teacher || student) + reverse KL(student || teacher)
+    over the listed words and, with ``rest``, all others as one outcome; without, the
+    sums are over the listed words alone. ``weights`` float32 [T] carry the mask and the
+    mean; ``stats`` float32 [6] gets the weighted sums named in DISTILL_STATS, the loss
+    first; ``dlogits`` [T, V] of the logits' dtype (may be ``logits``; None: the loss
+    alone) grad_scale times its gradient; ``losses`` float32 [T] the rows'.
+    """
+    if _direct("distill_loss", logits, stream, logits, teacher_ids, teacher_logprobs, weights, stats, dlogits, losses, reverse,
+               rest, temperature, grad_scale) == OK:
+        return stats
+    index = logits.get_device()
+    packed = {"teacher_ids": teacher_ids, "teacher_logprobs": teacher_logprobs, "weights": weights, "stats": stats, "losses": losses}
+    if _apart(index, (logits, dlogits), packed.values()):
+        _refuse(index, {"logits": logits, "dlogits": dlogits}, packed)
+    step = _row_step(logits, "logits")
+    pr = LogitsProblem(*logits.shape, step, _float_code(logits, "logits"), 0, temperature)
+    places = _lists(teacher_ids, teacher_logprobs, pr.num_tokens, ("teacher_ids", "teacher_logprobs"))
+    _rows(pr.num_tokens, (weights, losses))
+    if stats.shape != (6,) or stats.dtype is not _FLOAT32:
+        raise ValueError("stats must be float32 [6]")
+    step = 0
+    if dlogits is not None:
+        if dlogits.shape != logits.shape or dlogits.dtype is not logits.dtype:
+            raise ValueError("dlogits must have the logits' shape and dtype")
+        step = _row_step(dlogits, "dlogits")
+    _launch(_lib.pdalm_distill_loss, index, stream, logits.data_ptr(), teacher_ids.data_ptr(), teacher_logprobs.data_ptr(),
+            weights.data_ptr(), stats.data_ptr(), _ptr(losses), _ptr(dlogits), pr,
+            DistillOptions(places, 1 if rest else 0, reverse, grad_scale, step))
     return stats
 
 

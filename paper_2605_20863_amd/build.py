@@ -21,7 +21,7 @@ LIB = os.path.join(PKG, "libpda.so")
 MODULE = os.path.join(PKG, "_pda_torch.so")
 
 SOURCES = ["pda_kernels.hip", "pda_append.hip", "pda_prefill.hip", "pda_scratch.hip", "pda_rope.hip", "pda_policy.hip",
-           "pda_host.cpp", "pda_ops_host.cpp"]
+           "pda_norm.hip", "pda_top.hip", "pda_distill.hip", "pda_host.cpp", "pda_ops_host.cpp", "pda_lm_host.cpp"]
 ARCH = "gfx950"
 
 # No packed-FP32 instructions: they are kept out of every HIP object.

@@ -1,5 +1,5 @@
 // Element types and wave helpers of the operators around attention
-// (pda_rope.hip, pda_policy.hip).
+// (pda_rope.hip, pda_policy.hip, pda_norm.hip, pda_top.hip, pda_distill.hip).
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -58,6 +58,82 @@ __device__ __forceinline__ float wave_max_f(float x) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) x = fmaxf(x, __shfl_xor(x, o, 64));
   return x;
+}
+
+// fp8 (e4m3) scales: the largest code's value, and the smallest scale.
+constexpr float kE4M3Max = 448.f;
+constexpr float kMinScale = 0x1p-126f;
+
+// Correctly rounded x / s for many x: with y the rounded reciprocal, q = x y and
+// the exact remainder r = x - q s, the quotient is q + r y rounded once
+// (Markstein). Where the remainder could leave float32's range the division is
+// made as such.
+struct Div {
+  float s, y;
+  bool plain;
+};
+__device__ __forceinline__ Div make_div(float s) { return Div{s, 1.f / s, s < 0x1p-90f || s > 0x1p90f}; }
+__device__ __forceinline__ float quotient(float x, const Div& d) {
+  if (d.plain) return __fdiv_rn(x, d.s);
+  const float q = x * d.y, r = fmaf(-q, d.s, x);
+  return r == 0.f ? q : fmaf(r, d.y, q);  // q as it is keeps the sign of a zero
+}
+
+// Eight neighbouring elements, as loaded.
+template <typename T>
+struct Raw;
+template <>
+struct Raw<uint16_t> {
+  u32x4 a;
+};
+template <>
+struct Raw<float> {
+  u32x4 a, b;
+};
+// STREAM: past the caches.
+template <bool STREAM, typename T>
+__device__ __forceinline__ Raw<T> load8(const void* base, int64_t at) {
+  const u32x4* p = reinterpret_cast<const u32x4*>(static_cast<const T*>(base) + at);
+  Raw<T> r;
+  r.a = STREAM ? __builtin_nontemporal_load(p) : *p;
+  if constexpr (sizeof(T) == 4) r.b = STREAM ? __builtin_nontemporal_load(p + 1) : p[1];
+  return r;
+}
+__device__ __forceinline__ void unpack(const Raw<uint16_t>& r, float (&x)[8]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t w = r.a[i];
+    x[2 * i] = as_f32(w << 16);
+    x[2 * i + 1] = as_f32(w & 0xFFFF0000u);
+  }
+}
+__device__ __forceinline__ void unpack(const Raw<float>& r, float (&x)[8]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t u = r.a[i], w = r.b[i];
+    x[i] = as_f32(u);
+    x[4 + i] = as_f32(w);
+  }
+}
+template <bool STREAM>
+__device__ __forceinline__ void put16(void* p, u32x4 v) {
+  if constexpr (STREAM) __builtin_nontemporal_store(v, static_cast<u32x4*>(p));
+  else *static_cast<u32x4*>(p) = v;
+}
+template <bool STREAM>
+__device__ __forceinline__ void store8(void* base, int64_t at, bool bf16, const float (&y)[8]) {
+  u32x4 o[2];
+  if (bf16) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[0][i] = pack_bf16(y[2 * i], y[2 * i + 1]);
+    put16<STREAM>(static_cast<uint16_t*>(base) + at, o[0]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) o[i / 4][i % 4] = as_u32(y[i]);
+    float* p = static_cast<float*>(base) + at;
+    put16<STREAM>(p, o[0]);
+    put16<STREAM>(p + 4, o[1]);
+  }
 }
 
 }  // namespace pda

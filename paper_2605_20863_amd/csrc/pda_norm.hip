@@ -1,0 +1,347 @@
+// HIP kernels for the residual stream's root-mean-square norm and its gradient
+// on MI355X (gfx950).
+//
+// For a token's row x [H], weights w, h = x + residual rounded to the stream's type:
+//     r = 1 / sqrt(mean h^2 + eps),  y = h w r
+// out is y rounded once, or in fp8 y / s with s = max |y| / 448 of a row or of groups
+// of neighbours. With g the gradient of y and q that of h from elsewhere:
+//     dh = q + r (g w - h r^2 mean(g w h)),  dw = sum over rows of g h r.
+//
+// Both sums of a row (squares and, of the gradient, g w h; of a row's fp8 scale the
+// largest |h w|, which is |y| before r) come from one read of it and one merge; the
+// row stays in the registers of its RT threads, N vectors of 8 elements each, until
+// it is written. Sums are float32, the weights' gradient over workgroups float64.
+
+#include "pda_elem.h"
+#include "pda_lm_internal.h"
+
+namespace pda {
+namespace {
+
+constexpr int kThreads = 256;  // of a workgroup, unless a row has more
+
+template <int RT>
+constexpr int kGroup = RT < kThreads ? kThreads : RT;
+
+struct Two {
+  float a, b;
+};
+
+// Sum of x.a and, by MAX, largest or sum of x.b over the 64 lanes, in each of them.
+template <bool MAX>
+__device__ __forceinline__ Two wave_both(Two x) {
+  x.a = group_sum<16>(x.a);
+  x.b = MAX ? group_max<16>(x.b) : group_sum<16>(x.b);
+#pragma unroll
+  for (int o = 16; o < 64; o *= 2) {
+    x.a += __shfl_xor(x.a, o, 64);
+    const float y = __shfl_xor(x.b, o, 64);
+    x.b = MAX ? fmaxf(x.b, y) : x.b + y;
+  }
+  return x;
+}
+
+// The same over a row's RT threads; `turn` alternates between a workgroup's rows, so that
+// one barrier a row does.
+template <int RT, bool MAX>
+__device__ __forceinline__ Two row_both(Two x, int turn) {
+  x = wave_both<MAX>(x);
+  if constexpr (RT > 64) {
+    constexpr int W = RT / 64;
+    __shared__ Two parts[2][W];
+    if ((threadIdx.x & 63) == 0) parts[turn & 1][threadIdx.x / 64] = x;
+    __syncthreads();
+    x = parts[turn & 1][0];
+#pragma unroll
+    for (int w = 1; w < W; ++w) {
+      const Two y = parts[turn & 1][w];
+      x.a += y.a;
+      x.b = MAX ? fmaxf(x.b, y.b) : x.b + y.b;
+    }
+  }
+  return x;
+}
+
+__device__ __forceinline__ void load_weight(const void* w, bool bf16, int at, float (&y)[8]) {
+  if (bf16) unpack(load8<false, uint16_t>(w, at), y);
+  else unpack(load8<false, float>(w, at), y);
+}
+
+// h = x + residual in the stream's type, as kept.
+__device__ __forceinline__ void add_rounded(Raw<uint16_t>& x, const Raw<uint16_t>& r) {
+  float a[8], b[8];
+  unpack(x, a);
+  unpack(r, b);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) x.a[i] = pack_bf16(a[2 * i] + b[2 * i], a[2 * i + 1] + b[2 * i + 1]);
+}
+__device__ __forceinline__ void add_rounded(Raw<float>& x, const Raw<float>& r) {
+  float a[8], b[8];
+  unpack(x, a);
+  unpack(r, b);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    x.a[i] = as_u32(a[i] + b[i]);
+    x.b[i] = as_u32(a[4 + i] + b[4 + i]);
+  }
+}
+template <bool STREAM>
+__device__ __forceinline__ void store_raw(void* base, int64_t at, const Raw<uint16_t>& x) {
+  put16<STREAM>(static_cast<uint16_t*>(base) + at, x.a);
+}
+template <bool STREAM>
+__device__ __forceinline__ void store_raw(void* base, int64_t at, const Raw<float>& x) {
+  float* p = static_cast<float*>(base) + at;
+  put16<STREAM>(p, x.a);
+  put16<STREAM>(p + 4, x.b);
+}
+
+// Codes of y / s; NaN stays NaN (a clamp by min and max would make a number of it).
+__device__ __forceinline__ uint32_t encode4(const float* y, const Div& d) {
+  float z[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    z[i] = quotient(y[i], d);
+    z[i] = z[i] > kE4M3Max ? kE4M3Max : z[i] < -kE4M3Max ? -kE4M3Max : z[i];
+  }
+  const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(z[0], z[1], 0, false);
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(z[2], z[3], lo, true);
+}
+__device__ __forceinline__ float scale_of(float amax) { return fmaxf(__fdiv_rn(amax, kE4M3Max), kMinScale); }
+
+__device__ __forceinline__ float inv_rms(float squares, const NormArgs& a) { return 1.f / sqrtf(squares / (float)a.H + a.eps); }
+
+template <typename T, int RT, int N, bool FP8, bool STREAM>
+__global__ __launch_bounds__(kGroup<RT>) void norm_kernel(NormArgs a) {
+  constexpr int ROWS = kGroup<RT> / RT;
+  const int t = (int)blockIdx.x * ROWS + (int)threadIdx.x / RT, lane = (int)threadIdx.x % RT, vecs = a.H / 8;
+  if (t >= a.T) return;  // whole waves, and only where a row is one wave's
+  Raw<T> x[N] = {}, r[N] = {};
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    const int i = lane + n * RT;
+    if (i >= vecs) continue;
+    x[n] = load8<STREAM, T>(a.x, t * a.x_stride + 8 * i);
+    if (a.res) r[n] = load8<STREAM, T>(a.res, t * a.res_stride + 8 * i);
+  }
+  Two s = {0.f, 0.f};
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    const int i = lane + n * RT;
+    if (i >= vecs) continue;
+    if (a.res) {
+      add_rounded(x[n], r[n]);
+      if (a.sum) store_raw<STREAM>(a.sum, t * a.sum_stride + 8 * i, x[n]);
+    }
+    float h[8];
+    unpack(x[n], h);
+    float q = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) q = fmaf(h[e], h[e], q);
+    s.a += q;
+    if (FP8 && !a.group) {
+      float w[8];
+      load_weight(a.w, a.w_bf16, 8 * i, w);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s.b = fmaxf(s.b, fabsf(h[e] * w[e]));
+    }
+  }
+  s = row_both<RT, true>(s, 0);
+  const float rms = inv_rms(s.a, a);
+  if (FP8 && !a.group) {
+    s.b = scale_of(s.b * rms);
+    if (lane == 0) a.scales[t] = s.b;
+  }
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    const int i = lane + n * RT;
+    if (!FP8 && i >= vecs) continue;  // an fp8 group's lanes stay together
+    float h[8], w[8] = {};
+    unpack(x[n], h);
+    if (i < vecs) load_weight(a.w, a.w_bf16, 8 * i, w);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) h[e] = h[e] * w[e] * rms;
+    if constexpr (FP8) {
+      float scale = s.b;
+      if (a.group) {
+        float m = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) m = fmaxf(m, fabsf(h[e]));
+        scale = scale_of(a.group == 64 ? group_max<8>(m) : group_max<16>(m));
+      }
+      if (i >= vecs) continue;
+      if (a.group && 8 * i % a.group == 0) a.scales[(int64_t)t * (a.H / a.group) + 8 * i / a.group] = scale;
+      const Div d = make_div(scale);
+      const u32x2 codes = {encode4(h, d), encode4(h + 4, d)};
+      u32x2* p = reinterpret_cast<u32x2*>(static_cast<uint8_t*>(a.out) + t * a.out_stride + 8 * i);
+      if constexpr (STREAM) __builtin_nontemporal_store(codes, p);
+      else *p = codes;
+    } else {
+      store8<STREAM>(a.out, t * a.out_stride + 8 * i, a.type == OutType::BF16, h);
+    }
+  }
+}
+
+// Every workgroup takes rows in turn and keeps their part of the weights' gradient
+// in registers.
+template <typename T, int RT, int N, bool STREAM>
+__global__ __launch_bounds__(kGroup<RT>) void norm_backward_kernel(NormArgs a) {
+  constexpr int ROWS = kGroup<RT> / RT;
+  const int sub = (int)threadIdx.x / RT, lane = (int)threadIdx.x % RT, vecs = a.H / 8;
+  float acc[N][8] = {};
+  int turn = 0;
+  for (int t = (int)blockIdx.x * ROWS + sub; t < a.T; t += a.wgs * ROWS, ++turn) {
+    Raw<T> x[N] = {}, g[N] = {}, q[N] = {};
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      const int i = lane + n * RT;
+      if (i >= vecs) continue;
+      x[n] = load8<STREAM, T>(a.x, t * a.x_stride + 8 * i);
+      g[n] = load8<STREAM, T>(a.out, t * a.out_stride + 8 * i);
+      if (a.res) q[n] = load8<STREAM, T>(a.res, t * a.res_stride + 8 * i);
+    }
+    Two s = {0.f, 0.f};
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      const int i = lane + n * RT;
+      if (i >= vecs) continue;
+      float h[8], y[8], w[8];
+      unpack(x[n], h);
+      unpack(g[n], y);
+      load_weight(a.w, a.w_bf16, 8 * i, w);
+      float b = 0.f, c = 0.f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        b = fmaf(h[e], h[e], b);
+        c = fmaf(y[e] * w[e], h[e], c);
+      }
+      s.a += b;
+      s.b += c;
+    }
+    s = row_both<RT, false>(s, turn);
+    const float rms = inv_rms(s.a, a), back = s.b / (float)a.H * rms * rms;
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      const int i = lane + n * RT;
+      if (i >= vecs) continue;
+      float h[8], y[8], w[8], o[8];
+      unpack(x[n], h);
+      unpack(g[n], y);
+      load_weight(a.w, a.w_bf16, 8 * i, w);
+      unpack(q[n], o);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        acc[n][e] = fmaf(y[e], h[e] * rms, acc[n][e]);
+        o[e] = fmaf(rms, fmaf(-h[e], back, y[e] * w[e]), o[e]);
+      }
+      store8<STREAM>(a.sum, t * a.sum_stride + 8 * i, a.bf16, o);
+    }
+  }
+  if (!a.dw) return;
+  // waves of one row each: their parts to the first one's
+  if constexpr (ROWS > 1) {
+    __shared__ float sums[ROWS - 1][N][8][RT];
+    if (sub > 0) {
+#pragma unroll
+      for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sums[sub - 1][n][e][lane] = acc[n][e];
+    }
+    __syncthreads();
+    if (sub > 0) return;
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+#pragma unroll
+        for (int r = 0; r < ROWS - 1; ++r) acc[n][e] += sums[r][n][e][lane];
+  }
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    const int i = lane + n * RT;
+    if (i < vecs) store8<false>(a.dw_part, (int64_t)blockIdx.x * a.H + 8 * i, false, acc[n]);
+  }
+}
+
+// Sums the workgroups' parts in a fixed order: a workgroup per 16 weights, a row of
+// parts for each 16 of its threads, four loads of a thread in flight.
+constexpr int kSumRows = 64;
+__global__ __launch_bounds__(16 * kSumRows) void norm_weight_grad_kernel(NormArgs a) {
+  __shared__ double sums[kSumRows][16];
+  const int i = (int)threadIdx.x % 16, r = (int)threadIdx.x / 16, at = (int)blockIdx.x * 16 + i;
+  const float* part = a.dw_part + min(at, a.H - 1);
+  double x = 0.;
+  int g = r;
+  for (; g + 3 * kSumRows < a.wgs; g += 4 * kSumRows) {
+    float v[4];
+#pragma unroll
+    for (int n = 0; n < 4; ++n) v[n] = part[(int64_t)(g + n * kSumRows) * a.H];
+    x += ((double)v[0] + (double)v[1]) + ((double)v[2] + (double)v[3]);
+  }
+  for (; g < a.wgs; g += kSumRows) x += (double)part[(int64_t)g * a.H];
+  sums[r][i] = x;
+  __syncthreads();
+  for (int n = kSumRows / 2; n > 0; n /= 2) {
+    if (r < n) sums[r][i] += sums[r + n][i];
+    __syncthreads();
+  }
+  if (r == 0 && at < a.H) a.dw[at] = (float)sums[0][i];
+}
+
+// ------------------------------------------------------------- launches
+
+template <typename K>
+hipError_t launch(K kernel, int64_t wgs, int threads, const NormArgs& a, hipStream_t s) {
+  NormArgs args = a;
+  void* params[] = {&args};
+  return hipLaunchKernel(reinterpret_cast<const void*>(kernel), dim3((unsigned)wgs), dim3((unsigned)threads), params, 0, s);
+}
+
+template <typename T, bool FP8, int RT, int N>
+hipError_t norm_rows(const NormArgs& a, hipStream_t s) {
+  constexpr int rows = kGroup<RT> / RT;
+  return launch(&norm_kernel<T, RT, N, FP8, false>, (a.T + rows - 1) / rows, kGroup<RT>, a, s);
+}
+
+template <typename T, bool FP8>
+hipError_t norm_for(const NormArgs& a, hipStream_t s) {
+  const int v = a.H / 8;
+  return v <= 64 ? norm_rows<T, FP8, 64, 1>(a, s)
+         : v <= 256 ? norm_rows<T, FP8, 256, 1>(a, s)
+         : v <= 512 ? norm_rows<T, FP8, 256, 2>(a, s)
+         : v <= 1024 ? norm_rows<T, FP8, 256, 4>(a, s)
+         : v <= 2048 ? norm_rows<T, FP8, 512, 4>(a, s) : norm_rows<T, FP8, 1024, 4>(a, s);
+}
+
+template <typename T, int RT, int N>
+hipError_t backward_rows(const NormArgs& a, hipStream_t s) {
+  return launch(&norm_backward_kernel<T, RT, N, false>, a.wgs, kGroup<RT>, a, s);
+}
+
+template <typename T>
+hipError_t backward_for(NormArgs a, hipStream_t s) {
+  const int v = a.H / 8, rows = v <= 64 ? 4 : 1;
+  const int64_t wgs = ((int64_t)a.T + rows - 1) / rows;
+  if (wgs < a.wgs) a.wgs = (int32_t)wgs;
+  hipError_t e = hipSuccess;
+  if (a.wgs) e = v <= 64 ? backward_rows<T, 64, 1>(a, s)
+                 : v <= 256 ? backward_rows<T, 256, 1>(a, s)
+                 : v <= 512 ? backward_rows<T, 256, 2>(a, s)
+                 : v <= 1024 ? backward_rows<T, 256, 4>(a, s)
+                 : v <= 2048 ? backward_rows<T, 512, 4>(a, s) : backward_rows<T, 1024, 4>(a, s);
+  if (e != hipSuccess || !a.dw) return e;
+  return launch(&norm_weight_grad_kernel, (a.H + 15) / 16, 16 * kSumRows, a, s);
+}
+
+}  // namespace
+
+hipError_t launch_norm(const NormArgs& a, hipStream_t s) {
+  if (a.type == OutType::FP8) return a.bf16 ? norm_for<uint16_t, true>(a, s) : norm_for<float, true>(a, s);
+  return a.bf16 ? norm_for<uint16_t, false>(a, s) : norm_for<float, false>(a, s);
+}
+
+hipError_t launch_norm_backward(const NormArgs& a, hipStream_t s) {
+  return a.bf16 ? backward_for<uint16_t>(a, s) : backward_for<float>(a, s);
+}
+
+}  // namespace pda

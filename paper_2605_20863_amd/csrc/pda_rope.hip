@@ -25,8 +25,6 @@ namespace {
 
 constexpr int kWaves = 4;  // waves per workgroup
 constexpr int kManyRows = 8, kFewRows = 2;  // rows of a lane group that a wave takes
-constexpr float kE4M3Max = 448.f;
-constexpr float kMinScale = 0x1p-126f;
 
 __device__ __forceinline__ int lane_id() { return (int)(threadIdx.x & 63); }
 __device__ __forceinline__ int wave_id() { return __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)); }
@@ -36,63 +34,6 @@ struct Row {
   static constexpr int LPR = D / 8;     // lanes of a row
   static constexpr int RPI = 64 / LPR;  // rows of a wave at a time
 };
-
-// Eight neighbouring elements, as loaded.
-template <typename T>
-struct Raw;
-template <>
-struct Raw<uint16_t> {
-  u32x4 a;
-};
-template <>
-struct Raw<float> {
-  u32x4 a, b;
-};
-// STREAM: past the caches (see `few`).
-template <bool STREAM, typename T>
-__device__ __forceinline__ Raw<T> load8(const void* base, int64_t at) {
-  const u32x4* p = reinterpret_cast<const u32x4*>(static_cast<const T*>(base) + at);
-  Raw<T> r;
-  r.a = STREAM ? __builtin_nontemporal_load(p) : *p;
-  if constexpr (sizeof(T) == 4) r.b = STREAM ? __builtin_nontemporal_load(p + 1) : p[1];
-  return r;
-}
-__device__ __forceinline__ void unpack(const Raw<uint16_t>& r, float (&x)[8]) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const uint32_t w = r.a[i];
-    x[2 * i] = as_f32(w << 16);
-    x[2 * i + 1] = as_f32(w & 0xFFFF0000u);
-  }
-}
-__device__ __forceinline__ void unpack(const Raw<float>& r, float (&x)[8]) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const uint32_t u = r.a[i], w = r.b[i];
-    x[i] = as_f32(u);
-    x[4 + i] = as_f32(w);
-  }
-}
-template <bool STREAM>
-__device__ __forceinline__ void put16(void* p, u32x4 v) {
-  if constexpr (STREAM) __builtin_nontemporal_store(v, static_cast<u32x4*>(p));
-  else *static_cast<u32x4*>(p) = v;
-}
-template <bool STREAM>
-__device__ __forceinline__ void store8(void* base, int64_t at, bool bf16, const float (&y)[8]) {
-  u32x4 o[2];
-  if (bf16) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) o[0][i] = pack_bf16(y[2 * i], y[2 * i + 1]);
-    put16<STREAM>(static_cast<uint16_t*>(base) + at, o[0]);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) o[i / 4][i % 4] = as_u32(y[i]);
-    float* p = static_cast<float*>(base) + at;
-    put16<STREAM>(p, o[0]);
-    put16<STREAM>(p + 4, o[1]);
-  }
-}
 
 // A lane's part of the rotation: y_i = n_i c_i + partner_i s_i, where dim i's
 // partner is the other member of its pair and s carries the sign.
@@ -288,20 +229,6 @@ __device__ __forceinline__ uint32_t enc4(const float (&z)[4]) {
   for (int i = 0; i < 4; ++i) y[i] = fminf(fmaxf(z[i], -kE4M3Max), kE4M3Max);
   const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
   return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], lo, true);
-}
-// Correctly rounded x / s for many x: with y the rounded reciprocal, q = x y and
-// the exact remainder r = x - q s, the quotient is q + r y rounded once
-// (Markstein). Where the remainder could leave float32's range the division is
-// made as such.
-struct Div {
-  float s, y;
-  bool plain;
-};
-__device__ __forceinline__ Div make_div(float s) { return Div{s, 1.f / s, s < 0x1p-90f || s > 0x1p90f}; }
-__device__ __forceinline__ float quotient(float x, const Div& d) {
-  if (d.plain) return __fdiv_rn(x, d.s);
-  const float q = x * d.y, r = fmaf(-q, d.s, x);
-  return r == 0.f ? q : fmaf(r, d.y, q);  // q as it is keeps the sign of a zero
 }
 __device__ __forceinline__ uint32_t reencode4(uint32_t w, float old, const Div& d) {
   const float z[4] = {

@@ -1,4 +1,5 @@
-// Python module _pda_torch: the calls of include/pda_ops.h from torch tensors.
+// Python module _pda_torch: the calls of include/pda_ops.h and include/pda_lm.h from
+// torch tensors.
 //
 // A small call's kernels take 3 - 8 us, and reading the shapes, strides and
 // pointers of up to 14 tensors from Python took 5 - 7 us of host time before each
@@ -14,7 +15,7 @@
 #include <cstdint>
 #include <initializer_list>
 
-#include "pda_ops.h"
+#include "pda_lm.h"
 
 namespace {
 
@@ -232,13 +233,16 @@ struct Logits {
   int64_t T, V;
   Pointer z, y;
 
-  Logits(Args& a, int iz, int iy) {
+  // iy < 0, or None where that may be: no targets
+  Logits(Args& a, int iz, int iy, bool may_lack = false) {
     const auto n = a.tensor(iz).sizes();
     Args::need(n.size() == 2);
     T = n[0], V = n[1];
     z = a.rows(iz, n, &pr.row_stride);
-    y = a.contiguous(iy, {T});
-    Args::need(y.type == c10::kLong || y.type == c10::kInt);
+    if (iy >= 0 && !(may_lack && a.none(iy))) {
+      y = a.contiguous(iy, {T});
+      Args::need(y.type == c10::kLong || y.type == c10::kInt);
+    }
     pr.num_tokens = Args::int32(T);
     pr.vocab = Args::int32(V);
     pr.dtype = float_code(z.type);
@@ -280,6 +284,101 @@ int policy(PyObject* const* args, Py_ssize_t n) {
                                               static_cast<hipStream_t>(a.address(STREAM)));
 }
 
+// [T, H] of type `dt` (null where None may be given).
+Pointer stream_rows(Args& a, int i, c10::IntArrayRef shape, c10::ScalarType dt, int64_t* stride, bool may_lack) {
+  if (may_lack && a.none(i)) return {};
+  const Pointer p = a.rows(i, shape, stride);
+  Args::need(p.type == dt);
+  return p;
+}
+
+int norm(PyObject* const* args, Py_ssize_t n) {
+  Args a(args, n, 9);
+  enum { ENTRY, STREAM, X, WEIGHT, OUT, RES, SUM, SCALES, EPS };
+  pdalm_norm_problem pr = {};
+  const auto s = a.tensor(X).sizes();
+  Args::need(s.size() == 2);
+  const int64_t T = s[0], H = s[1];
+  const Pointer x = a.rows(X, s, &pr.x_stride), out = a.rows(OUT, s, &pr.out_stride), w = a.contiguous(WEIGHT, {H});
+  const Pointer res = stream_rows(a, RES, s, x.type, &pr.residual_stride, true);
+  const Pointer sum = stream_rows(a, SUM, s, x.type, &pr.sum_stride, true);
+  pr.num_tokens = Args::int32(T);
+  pr.width = Args::int32(H);
+  pr.dtype = float_code(x.type);
+  pr.out_dtype = cache_code(out.type);
+  pr.weight_dtype = float_code(w.type);
+  pr.eps = a.number(EPS);
+  float* scales = nullptr;
+  Args::need((pr.out_dtype == PDA_DTYPE_FP8_E4M3) != a.none(SCALES));
+  if (!a.none(SCALES)) {
+    const auto g = a.tensor(SCALES).sizes();
+    Args::need(g.size() == 1 || (g.size() == 2 && g[1] >= 1 && H % g[1] == 0));
+    if (g.size() == 1) scales = a.array<float>(SCALES, c10::kFloat, {T});
+    else scales = a.array<float>(SCALES, c10::kFloat, {T, g[1]});
+    pr.scale_group = g.size() == 1 || g[1] == 1 ? 0 : Args::int32(H / g[1]);
+  }
+  return enter<decltype(&pdalm_add_rms_norm)>(a.address(ENTRY), x.p, res.p, w.p, sum.p, out.p, scales, &pr,
+                                              static_cast<hipStream_t>(a.address(STREAM)));
+}
+
+int norm_backward(PyObject* const* args, Py_ssize_t n) {
+  Args a(args, n, 9);
+  enum { ENTRY, STREAM, X, WEIGHT, GOUT, GH, GW, GRES, EPS };
+  pdalm_norm_problem pr = {};
+  const auto s = a.tensor(X).sizes();
+  Args::need(s.size() == 2);
+  const Pointer h = a.rows(X, s, &pr.x_stride), w = a.contiguous(WEIGHT, {s[1]});
+  const Pointer g = stream_rows(a, GOUT, s, h.type, &pr.out_stride, false);
+  const Pointer d = stream_rows(a, GH, s, h.type, &pr.sum_stride, false);
+  const Pointer q = stream_rows(a, GRES, s, h.type, &pr.residual_stride, true);
+  float* dw = a.optional<float>(GW, c10::kFloat, {s[1]});
+  pr.num_tokens = Args::int32(s[0]);
+  pr.width = Args::int32(s[1]);
+  pr.dtype = pr.out_dtype = float_code(h.type);
+  pr.weight_dtype = float_code(w.type);
+  pr.eps = a.number(EPS);
+  return enter<decltype(&pdalm_add_rms_norm_backward)>(a.address(ENTRY), h.p, w.p, g.p, q.p, d.p, dw, &pr,
+                                                       static_cast<hipStream_t>(a.address(STREAM)));
+}
+
+int top(PyObject* const* args, Py_ssize_t n) {
+  Args a(args, n, 9);
+  enum { ENTRY, STREAM, LOGITS, IDS, TOPS, TARGETS, LOGP, ENT, TEMP };
+  Logits l(a, LOGITS, TARGETS, true);
+  l.pr.temperature = a.number(TEMP);
+  const auto s = a.tensor(IDS).sizes();
+  Args::need(s.size() == 2 && s[0] == l.T && (l.y.p || a.none(TARGETS) || l.T == 0) && (!a.none(TARGETS) || a.none(LOGP)));
+  auto* ids = a.array<int32_t>(IDS, c10::kInt, {l.T, s[1]});
+  float* tops = a.array<float>(TOPS, c10::kFloat, {l.T, s[1]});
+  float* lp = a.optional<float>(LOGP, c10::kFloat, {l.T});
+  float* ent = a.optional<float>(ENT, c10::kFloat, {l.T});
+  return enter<decltype(&pdalm_top_logprobs)>(a.address(ENTRY), l.z.p, l.y.p, ids, tops, lp, ent, &l.pr, Args::int32(s[1]),
+                                              static_cast<hipStream_t>(a.address(STREAM)));
+}
+
+int distill(PyObject* const* args, Py_ssize_t n) {
+  Args a(args, n, 13);
+  enum { ENTRY, STREAM, LOGITS, IDS, TAU, WEIGHT, STATS, GRAD, LOSSES, REVERSE, REST, TEMP, SCALE };
+  Logits l(a, LOGITS, -1);
+  l.pr.temperature = a.number(TEMP);
+  const auto s = a.tensor(IDS).sizes();
+  Args::need(s.size() == 2 && s[0] == l.T);
+  pdalm_distill_options op = {Args::int32(s[1]), a.truth(REST), a.number(REVERSE), a.number(SCALE), 0};
+  const auto f = c10::kFloat;
+  const auto* ids = a.array<int32_t>(IDS, c10::kInt, {l.T, s[1]});
+  const float* tau = a.array<float>(TAU, f, {l.T, s[1]});
+  const float* w = a.array<float>(WEIGHT, f, {l.T});
+  float* stats = a.array<float>(STATS, f, {6});
+  Pointer g;
+  if (!a.none(GRAD)) {
+    g = a.rows(GRAD, {l.T, l.V}, &op.dlogits_stride);
+    Args::need(g.type == l.z.type);
+  }
+  float* losses = a.optional<float>(LOSSES, f, {l.T});
+  return enter<decltype(&pdalm_distill_loss)>(a.address(ENTRY), l.z.p, ids, tau, w, stats, losses, g.p, &l.pr, &op,
+                                              static_cast<hipStream_t>(a.address(STREAM)));
+}
+
 template <int (*F)(PyObject* const*, Py_ssize_t)>
 PyObject* call(PyObject*, PyObject* const* args, Py_ssize_t n) {
   int rc;
@@ -298,7 +397,9 @@ PyMethodDef method(const char* name) {
 
 PyMethodDef methods[] = {method<append>("paged_qk_norm_rope_append"), method<forward>("qk_norm_rope"),
                          method<backward>("qk_norm_rope_backward"), method<logprobs>("token_logprobs"),
-                         method<policy>("policy_loss"), {}};
+                         method<policy>("policy_loss"), method<norm>("add_rms_norm"),
+                         method<norm_backward>("add_rms_norm_backward"), method<top>("top_logprobs"),
+                         method<distill>("distill_loss"), {}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_pda_torch", nullptr, -1, methods};
 
 }  // namespace
