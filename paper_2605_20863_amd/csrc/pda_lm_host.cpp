@@ -121,15 +121,19 @@ int top_run(const void* logits, const void* targets, int32_t* top_ids, float* to
                        {top_ids, 4, "top_ids", true}, {top_logprobs, 4, "top_logprobs", true}, {logprobs, 4, "logprobs", false},
                        {entropy, 4, "entropy", false}});
   if (rc != PDA_OK) return rc;
-  a.splits = 1;
+  split_rows(&a);
   if ((int64_t)a.T * a.splits > kMaxWaves / 16) return host_fail(PDA_EINVAL, "num_tokens = %d is too much for one call", a.T);
+  const int64_t parts = a.splits > 1 ? (int64_t)a.T * a.splits : 0;
   HeldWorkspace ws;
-  if ((rc = hold_workspace(stream, kHeader, &ws)) != PDA_OK) return rc;
+  if ((rc = hold_workspace(stream, kHeader + parts * (16 + 8 * (int64_t)num_top), &ws)) != PDA_OK) return rc;
   a.logits = logits;
   a.targets = targets;
   a.logp = logprobs;
   a.ent = entropy;
   a.status = status_word(ws.base);
+  a.part = reinterpret_cast<float4*>(ws.base + kHeader);
+  g.keys = reinterpret_cast<uint64_t*>(ws.base + kHeader + parts * 16);
+  if (a.splits > 1 && a.T <= kShortUnits && (rc = count(stream, ws, &a)) != PDA_OK) return rc;
   g.K = num_top;
   g.ids = top_ids;
   g.tops = top_logprobs;

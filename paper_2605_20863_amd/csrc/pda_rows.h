@@ -178,6 +178,12 @@ __device__ __forceinline__ Soft group_merge(Soft x, float c) {
   return lanes_merge<W>(parts[threadIdx.x % W], c);
 }
 
+// The first lane's sums: a merge's roundings depend on the order of its two sides, so that lanes may differ by one.
+__device__ __forceinline__ Soft first_lane(const Soft& x) {
+  const auto first = [](float y) { return as_f32((uint32_t)__builtin_amdgcn_readfirstlane((int)as_u32(y))); };
+  return Soft{first(x.m), first(x.s), first(x.u)};
+}
+
 // Row t's target, or -1 for a row that takes no part.
 __device__ __forceinline__ int target_of(const LogitsArgs& a, int t) {
   const int64_t y = a.targets64 ? static_cast<const int64_t*>(a.targets)[t] : static_cast<const int32_t*>(a.targets)[t];

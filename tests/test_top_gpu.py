@@ -75,7 +75,7 @@ def orders(V):
     return {"rising": i / V * 30, "falling": -i / V * 30, "equal": torch.zeros(V), "rising steps": (i // 37) / V * 300, "saw": saw,
             "blocks": (i // 2048) % 3, "late": torch.where(i > V - 700, 5.0 + i / V, torch.zeros(V)),
             "one thread's": torch.where(i % 2048 < 16, 9.0 + i / V, i / V), "zeros": torch.where(i % 2 == 0, 0.0, -0.0),
-            "lowest": torch.full((V,), -3.3e38), "two": torch.where((i == 5) | (i == V - 1), 1.0, -math.inf)}
+            "zero bar": torch.where(i % 3 == 0, 0.0, -1.0 - i / V), "lowest": torch.full((V,), -3.3e38), "two": torch.where((i == 5) | (i == V - 1), 1.0, -math.inf)}
 
 
 @pytest.mark.parametrize("t", ["f32", "bf16"])
@@ -126,6 +126,25 @@ def test_masks_and_special_values(lib, t, V, T):
     R.near(lp[rest], wl[rest], bl[rest], torch.float32, "targets'")
     if T > 7:
         R.near(H[rest], wh[rest], bh[rest], torch.float32, "entropies")
+
+
+@pytest.mark.parametrize("V", [3000, 70_001])
+def test_infinities_and_nan_among_each_other(lib, V):
+    """More of +inf than places, and NaN before, among and after them; more NaN than places."""
+    z = torch.randn((4, V), generator=torch.Generator().manual_seed(V))
+    z[0, 5:500] = math.inf
+    z[0, V - 3] = math.nan
+    z[1, 100:2900:7] = math.nan
+    z[1, 0] = math.inf
+    z[2, V // 2] = math.inf
+    z[3, 40], z[3, 41], z[3, V - 1] = math.inf, -math.nan, math.nan
+    for K in (1, 2, 20, 256):
+        for x in (z, z.to(torch.bfloat16)):
+            rank = torch.where(x.isnan(), 3e38, torch.where(x == math.inf, 2e38, x.double()))
+            want = rank.sort(dim=1, descending=True, stable=True).indices[:, :K]
+            for r in (x, x.repeat(300, 1)):
+                ids, tops, _, _ = run(lib, r.to(DEV), K, 1.0)
+                assert torch.equal(ids.cpu().long(), want.repeat(r.shape[0] // 4, 1)) and tops.isnan().all()
 
 
 def test_options_change_nothing_else(lib):
