@@ -175,7 +175,7 @@ typedef struct pdalm_distill_options {
  *
  * The sums are in a fixed order. Errors as for pdaops_policy_loss (targets_int64 is not used), and
  * PDA_EINVAL for options out of range. Uses the stream's workspace (32 bytes per row, and where
- * few rows are cut into parts 16 per part and 4 K per row).
+ * few or very long rows are cut into parts 16 per part and 8 K per row).
  */
 int pdalm_distill_loss(const void* logits,
                        const int32_t* teacher_ids,

@@ -165,9 +165,14 @@ int distill_run(const void* logits, const int32_t* teacher_ids, const float* tea
                        {losses, 4, "losses", false}, {dlogits, e, "dlogits", false}});
   if (rc != PDA_OK) return rc;
   if (a.T > kMaxWaves / 64) return host_fail(PDA_EINVAL, "num_tokens = %d is too much for one call", a.T);
-  const int64_t terms = ((int64_t)a.T * kTerms * 4 + 255) / 256 * 256;
+  // Rows in registers (and LDS) where they fit and either there are enough of them for the
+  // compute units or they are short; otherwise in parts, read twice (as the policy loss).
+  constexpr int kManyBf16 = 160, kManyF32 = 112, kShortVectors = 3200;
+  const int v = vectors_of(a);
+  if (any && ((a.T < (a.bf16 ? kManyBf16 : kManyF32) && v > kShortVectors) || v > kListedVectors)) split_rows(&a);
+  const int64_t terms = ((int64_t)a.T * kTerms * 4 + 255) / 256 * 256, parts = (int64_t)a.T * a.splits * 16;
   HeldWorkspace ws;
-  if ((rc = hold_workspace(stream, kHeader + terms, &ws)) != PDA_OK) return rc;
+  if ((rc = hold_workspace(stream, kHeader + terms + parts + (parts ? (int64_t)a.T * op->num_listed * 8 : 0), &ws)) != PDA_OK) return rc;
   a.logits = logits;
   a.weight = weights;
   a.stats = stats;
@@ -181,6 +186,9 @@ int distill_run(const void* logits, const int32_t* teacher_ids, const float* tea
   g.rest = op->rest;
   g.rev = op->reverse;
   g.losses = losses;
+  a.part = reinterpret_cast<float4*>(ws.base + kHeader + terms);
+  g.listed = reinterpret_cast<float*>(ws.base + kHeader + terms + parts);
+  if (any && a.T <= kCountedRows && (rc = count(stream, ws, &a)) != PDA_OK) return rc;
   const hipError_t h = launch_distill_loss(g, stream);
   return h == hipSuccess ? PDA_OK : host_fail_hip(h, "distillation kernel launch");
 }

@@ -39,6 +39,7 @@ struct TopArgs {
 
 // Distillation from a teacher's lists (pda_distill.hip).
 constexpr int kDistillStats = 6;
+constexpr int kListedVectors = 1024 * (19 + 6);  // of a row in registers and LDS, beside its words' bits
 struct DistillArgs {
   LogitsArgs z;     // no targets; weight, terms, stats, dlogits as for the policy loss
   const int32_t* ids;  // [T, K]
@@ -46,7 +47,7 @@ struct DistillArgs {
   int32_t K, rest;
   float rev;
   float* losses;    // [T], or null
-  float* listed;    // [T, K] listed words' logits, of rows in parts
+  float* listed;    // [T, K] of rows in parts: {a place's word's logit, 1, or 0 if the word has an earlier place}
 };
 
 hipError_t launch_norm(const NormArgs& a, hipStream_t s);
