@@ -12,8 +12,8 @@
 //
 // The words outside of the list are summed by themselves, against their own largest logit,
 // so that a small p_r is as exact as a large one (1 - P would not be); the gradient outside is
-// one factor a row times a word's share of the rest. A bit in LDS for each of a row's words says which are listed: one
-// LDS read for a vector of 16 bytes, whose listed words are made -inf as it is loaded. Their gradients are written
+// one factor a row times a word's share of the rest. A byte in LDS for each of a row's vectors says which of its words are
+// listed; these are made -inf when the vector has come. Their gradients are written
 // over the vectors' by the threads that wrote these, after them.
 //
 // With rest, sum p + p_r = 1 turns the divergences into sums of terms that are not
@@ -74,27 +74,42 @@ __device__ __forceinline__ void add(Mass& x, u32x4 (&v)[N], float c, int live = 
     for (int e = 0; e < kPer<T>; ++e) m = fmaxf(m, element<T>(v[n], e));
   }
   x = rebase(x, m, c);
-#pragma unroll
-  for (int n = 0; n < N; ++n) again(v[n]);
   float s = 0.f;
 #pragma unroll
   for (int n = 0; n < N; ++n) {
     if (n >= live) continue;
+    again(v[n]);
 #pragma unroll
     for (int e = 0; e < kPer<T>; ++e) s += __builtin_amdgcn_exp2f((element<T>(v[n], e) - m) * c);
+    asm volatile("" : "+v"(s));  // one vector's elements after another's
   }
   x.s += s;
 }
-__device__ __forceinline__ Mass wave_merge(Mass x, float c) {
-#pragma unroll
-  for (int o = 1; o < 64; o *= 2) x = merge(x, Mass{__shfl_xor(x.m, o, 64), __shfl_xor(x.s, o, 64)}, c);
-  return x;
+// Over the 64 lanes, in each of them (in one order of additions for all).
+__device__ __forceinline__ float wave_total(float x) {
+  x = group_sum<16>(x);
+  x += __shfl_xor(x, 16, 64);
+  return x + __shfl_xor(x, 32, 64);
 }
-template <typename X>
-__device__ __forceinline__ X wave_total(X x) {
+__device__ __forceinline__ double wave_total(double x) {
 #pragma unroll
   for (int o = 1; o < 64; o *= 2) x += __shfl_xor(x, o, 64);
   return x;
+}
+__device__ __forceinline__ Mass wave_merge(const Mass& x, float c) {
+  float m = group_max<16>(x.m);
+  m = fmaxf(m, __shfl_xor(m, 16, 64));
+  m = fmaxf(m, __shfl_xor(m, 32, 64));
+  return Mass{m, wave_total(rebase(x, m, c).s)};
+}
+// Over W waves' sums, in every thread.
+template <int W>
+__device__ __forceinline__ Mass waves_merge(const Mass* parts, float c) {
+  static_assert(W <= 16, "a lane each");
+  const int i = (int)threadIdx.x & 15;
+  const Mass x = i < W ? parts[i] : no_mass();
+  const float m = group_max<16>(x.m);
+  return Mass{m, group_sum<16>(rebase(x, m, c).s)};
 }
 
 // ------------------------------------------------------------- the list
@@ -124,89 +139,87 @@ struct Range {
   bool odds;
 };
 
-// For a range of V vectors: which of its words are listed, and the places whose words each of NT threads writes.
+// For a range of up to V vectors of each of NT threads: which of its words are listed, and the places whose words each
+// thread writes. Vector n of the range is thread n % NT's.
 template <typename T, int NT, int V>
 struct Listed {
-  static constexpr int kOdd = V * kPer<T>;  // bits of the elements outside of all vectors, from here on
-  uint32_t bits[kOdd / 32 + 1];
+  uint32_t bits[(V + 3) / 4][NT];  // a byte for each of a thread's vectors
+  uint32_t odd;                    // of the elements outside of all vectors
   int head[NT], next[kListThreads];  // a thread's places, -1: no more
   int id[kListThreads];
-  float d[kListThreads];  // gradients
+  float p[kListThreads], t[kListThreads], pa[kListThreads];  // see Row
   int twice;
 
   __device__ __forceinline__ void clear() {
-    for (int i = (int)threadIdx.x; i < kOdd / 32 + 1; i += NT) bits[i] = 0;
+#pragma unroll
+    for (int i = 0; i < (V + 3) / 4; ++i) bits[i][threadIdx.x] = 0;
     head[threadIdx.x] = -1;
-    if (threadIdx.x == 0) twice = 0;
+    if (threadIdx.x == 0) odd = twice = 0;
   }
 
-  // Between two barriers, after clear(): this thread's place goes to the thread that writes its word, if that is in
-  // the range. Returns the word's bit, or -1.
-  __device__ __forceinline__ int chain(const Place& p, const Span& sp, const Range& r) {
+  // After clear() and a barrier: this thread's place goes to the thread that writes its word, and the word's bit is set,
+  // if that is in the range. A barrier later all can be read. MASK: the bits are wanted.
+  template <bool MASK>
+  __device__ __forceinline__ bool enter(const Place& place, const Span& sp, const Range& r) {
     const int k = (int)threadIdx.x;
-    if (k >= kListThreads) return -1;
-    id[k] = p.id;
-    if (p.id < 0) return -1;
-    const int at = p.id - sp.head, in = sp.vectors * kPer<T>, i = at / kPer<T>;
-    const bool odd = at < 0 || at >= in;
-    if (odd ? !r.odds : i < r.first || i >= r.end) return -1;
-    const int owner = odd ? (at < 0 ? p.id : p.id - in) : (i - r.first) % NT;
+    if (k >= kListThreads) return false;
+    id[k] = place.id;
+    if (place.id < 0) return false;
+    const int at = place.id - sp.head, in = sp.vectors * kPer<T>, n = at / kPer<T> - r.first;
+    const bool outer = at < 0 || at >= in;
+    if (outer ? !r.odds : n < 0 || n >= r.end - r.first) return false;
+    const int owner = outer ? (at < 0 ? place.id : place.id - in) : n % NT;
     next[k] = atomicExch(&head[owner], k);
-    return odd ? kOdd + owner : at - r.first * kPer<T>;
-  }
-  // The same, and its bit is set.
-  __device__ __forceinline__ bool enter(const Place& p, const Span& sp, const Range& r) {
-    const int bit = chain(p, sp, r);
-    if (bit < 0) return false;
-    if (atomicOr(&bits[bit / 32], 1u << (bit % 32)) >> (bit % 32) & 1) twice = 1;
+    if constexpr (MASK) {
+      uint32_t* word = outer ? &odd : &bits[n / NT / 4][owner];
+      const int bit = outer ? owner : n / NT % 4 * 8 + at % kPer<T>;
+      if (atomicOr(word, 1u << bit) >> bit & 1) twice = 1;
+    }
     return true;
   }
-  // After the barrier behind enter(): a word's further places leave the list.
-  __device__ __forceinline__ void drop_further(Place& p, int K, int32_t* status) {
+  // After that barrier: a word's further places leave the list.
+  __device__ __forceinline__ void drop_further(Place& place, int32_t* status) {
     if (!twice) return;
     const int k = (int)threadIdx.x;
     bool further = false;
     if (k < kListThreads)
-      for (int j = 0; j < k; ++j) further |= p.id >= 0 && id[j] == p.id;
+      for (int j = 0; j < k; ++j) further |= place.id >= 0 && id[j] == place.id;
     __syncthreads();
     if (further) {
       atomicOr(status, kStatusTwice);
-      p.id = id[k] = -1;
+      place.id = id[k] = -1;
     }
   }
 
-  // Vector n (counted from the range's first) with its listed words made -inf.
-  __device__ __forceinline__ void leave_out(u32x4& v, int n) const {
-    const uint32_t byte = reinterpret_cast<const uint8_t*>(bits)[n * kPer<T> / 8];
-    const uint32_t mask = kPer<T> == 8 ? byte : byte >> (4 * (n & 1)) & 15;
-    if (mask) {
+  // Vectors first .. first + N - 1 of this thread's, with their listed words made -inf.
+  template <int N>
+  __device__ __forceinline__ void leave_out(u32x4 (&v)[N], int first) const {
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      const uint32_t mask = bits[(first + n) / 4][threadIdx.x] >> (first + n) % 4 * 8 & 255;
+      if (!mask) continue;
 #pragma unroll
       for (int w = 0; w < 4; ++w) {
         if constexpr (kPer<T> == 8) {
-          v[w] = mask >> (2 * w) & 1 ? (v[w] & 0xFFFF0000u) | 0xFF80u : v[w];
-          v[w] = mask >> (2 * w + 1) & 1 ? (v[w] & 0xFFFFu) | 0xFF800000u : v[w];
+          v[n][w] = mask >> (2 * w) & 1 ? (v[n][w] & 0xFFFF0000u) | 0xFF80u : v[n][w];
+          v[n][w] = mask >> (2 * w + 1) & 1 ? (v[n][w] & 0xFFFFu) | 0xFF800000u : v[n][w];
         } else {
-          v[w] = mask >> w & 1 ? 0xFF800000u : v[w];
+          v[n][w] = mask >> w & 1 ? 0xFF800000u : v[n][w];
         }
       }
     }
   }
-  __device__ __forceinline__ bool odd_listed() const { return bits[kOdd / 32] >> (kOdd % 32 + threadIdx.x) & 1; }
-
-  // This thread's places' gradients, over what it wrote before.
-  __device__ __forceinline__ void write(T* out) const {
-    for (int k = head[threadIdx.x]; k >= 0; k = next[k])
-      if (id[k] >= 0) store1(out + id[k], d[k]);
-  }
+  __device__ __forceinline__ bool odd_listed() const { return odd >> threadIdx.x & 1; }
 };
 
 // ------------------------------------------------------------- a row's results
 
+// A row's gradient, by the word's logit: outside of the list exp2((l - m) c - log2_s) outside, of a place's word
+// f (p total - t) + b (pa - p R).
 struct Row {
-  float loss;
-  float terms[kTerms];
-  float m, c, log2_s, outside;  // gradient outside of the list: exp2((l - m) c - log2_s) outside
-  bool zero;                    // no gradient, whatever the logits
+  float m, c, log2_s, outside;
+  float total, R, f, b;
+  bool zero;  // no gradient, whatever the logits
 };
 
 // What the waves of a workgroup hand each other.
@@ -214,112 +227,125 @@ template <int NT>
 struct Parts {
   Mass rest[NT / 64], list[kListThreads / 64];
   double S[kListThreads / 64];
-  float P[kListThreads / 64], f[kListThreads / 64], r[kListThreads / 64];
+  float P[kListThreads / 64], F[kListThreads / 64], R[kListThreads / 64];
 };
 
-// From the sums of the words outside of the list (`all`: the row's, otherwise this thread's part) and the
-// places; *d: the gradient by this thread's place's logit. Two barriers.
+constexpr int kListWaves = kListThreads / 64;
+__device__ __forceinline__ int wave_id() { return __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)); }
+
+// The list's own sums, by its waves: for the barrier before finish_row. Returns this thread's t.
 template <int NT>
-__device__ __forceinline__ Row finish_row(const DistillArgs& g, int t, Mass rest, bool all, const Place& place, Parts<NT>& s, float* d) {
-  constexpr int LW = kListThreads / 64;
-  const LogitsArgs& a = g.z;
-  const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
-  const bool first = (threadIdx.x & 63) == 0, in = place.id >= 0;
-  const float c = a.inv_temp * kLog2e, w = a.weight[t];
-  double t64 = 0.;
-  if (!all) {
-    rest = wave_merge(rest, c);
-    if (first) s.rest[wave] = rest;
+__device__ __forceinline__ double sum_list(const Place& place, float c, Parts<NT>& s) {
+  const int wave = wave_id();
+  if (wave >= kListWaves) return 0.;
+  const bool in = place.id >= 0;
+  Mass x = no_mass();
+  if (in) add1(x, place.l, c);
+  x = wave_merge(x, c);
+  const double t = in ? exp((double)place.tau) : 0., S = wave_total(t);
+  if ((threadIdx.x & 63) == 0) {
+    s.list[wave] = x;
+    s.S[wave] = S;
   }
-  if (wave < LW) {
-    Mass x = no_mass();
-    if (in) add1(x, place.l, c);
-    x = wave_merge(x, c);
-    t64 = in ? exp((double)place.tau) : 0.;
-    const double S = wave_total(t64);
-    if (first) {
-      s.list[wave] = x;
-      s.S[wave] = S;
-    }
-  }
-  __syncthreads();
-  if (!all) {
-    rest = s.rest[0];
+  return t;
+}
+
+// A row's quantities, from the sums of the words outside of the list, in every thread.
+struct Known {
+  Mass x;     // of all words
+  bool some;  // a distribution: some logit is above -inf (or NaN)
+  float log_s, pr, tr, ar, total, over;
+  double S;
+};
+template <int NT>
+__device__ __forceinline__ Known know_row(const DistillArgs& g, const Mass& rest, const Parts<NT>& s, float c) {
+  Known q;
+  q.x = rest;
+  q.S = 0.;
 #pragma unroll
-    for (int i = 1; i < NT / 64; ++i) rest = merge(rest, s.rest[i], c);
+  for (int i = 0; i < kListWaves; ++i) {
+    q.x = merge(q.x, s.list[i], c);
+    q.S += s.S[i];
   }
-  Mass x = rest;
-  double S64 = 0.;
-#pragma unroll
-  for (int i = 0; i < LW; ++i) {
-    x = merge(x, s.list[i], c);
-    S64 += s.S[i];
-  }
-  const bool some = x.s != 0.f;  // NaN too; else every logit is -inf: no distribution
+  q.some = q.x.s != 0.f;
+  q.log_s = logf(q.x.s);
+  const float lpr = (rest.m - q.x.m) * g.z.inv_temp + (logf(rest.s) - q.log_s);
+  q.pr = rest.s != 0.f ? expf(lpr) : 0.f;
   const bool others = g.rest && rest.s != 0.f;
-  const float log_s = logf(x.s), b = g.rev;
-  const float lpr = (rest.m - x.m) * a.inv_temp + (logf(rest.s) - log_s), pr = rest.s != 0.f ? expf(lpr) : 0.f;
-  const double t_rest = others ? fmax(1. - S64, kLeastRest) : 0.;
-  const float tr = (float)t_rest, ar = others ? lpr - (float)log(t_rest) : 0.f;
-  const float total = (float)(S64 + t_rest), over = (float)(S64 + t_rest - 1.);
-  // this thread's place
-  float tk = 0.f, p = 0.f, ta = 0.f, pa = 0.f;
-  if (wave < LW) {
-    const float lp = some ? (place.l - x.m) * a.inv_temp - log_s : -__builtin_huge_valf();
-    const float ak = in ? lp - place.tau : 0.f;
-    tk = (float)t64;
-    p = in ? expf(lp) : 0.f;
-    ta = tk == 0.f ? 0.f : tk * ak;
-    pa = p == 0.f ? 0.f : p * ak;
-    float f = -ta, r = pa;
-    if (g.rest) {  // squares where a is near to 0
-      const bool near = fabsf(ak) <= 1.f;
-      f = near ? tk * phi(ak) : p - tk - ta;
-      r = near ? p * phi(-ak) : tk - p + pa;
-    }
-    const float P = wave_total(p), F = wave_total(f), R = wave_total(r);
-    if (first) {
-      s.P[wave] = P;
-      s.f[wave] = F;
-      s.r[wave] = R;
-    }
+  const double t_rest = others ? fmax(1. - q.S, kLeastRest) : 0.;
+  q.tr = (float)t_rest;
+  q.ar = others ? lpr - (float)log(t_rest) : 0.f;
+  q.total = (float)(q.S + t_rest);
+  q.over = (float)(q.S + t_rest - 1.);
+  return q;
+}
+
+// This thread's place's part of the divergences, by the list's waves; what its gradient takes goes to `list`.
+template <int NT, typename List>
+__device__ __forceinline__ void sum_places(const DistillArgs& g, const Known& q, const Place& place, double t64, List& list, Parts<NT>& s) {
+  const int wave = wave_id(), k = (int)threadIdx.x;
+  if (wave >= kListWaves) return;
+  const bool in = place.id >= 0;
+  const float lp = q.some ? (place.l - q.x.m) * g.z.inv_temp - q.log_s : -__builtin_huge_valf();
+  const float a = in ? lp - place.tau : 0.f, t = (float)t64, p = in ? expf(lp) : 0.f;
+  const float ta = t == 0.f ? 0.f : t * a, pa = p == 0.f ? 0.f : p * a;
+  float f = -ta, r = pa;
+  if (g.rest) {  // squares where a is near to 0
+    const bool near = fabsf(a) <= 1.f;
+    f = near ? t * phi(a) : p - t - ta;
+    r = near ? p * phi(-a) : t - p + pa;
   }
-  __syncthreads();
-  float P = 0.f, F = 0.f, R = 0.f;
+  list.p[k] = p;
+  list.t[k] = t;
+  list.pa[k] = pa;
+  const float P = wave_total(p), F = wave_total(f), R = wave_total(r);
+  if ((threadIdx.x & 63) == 0) {
+    s.P[wave] = P;
+    s.F[wave] = F;
+    s.R[wave] = R;
+  }
+}
+
+// The divergences, a barrier after sum_places.
+struct Sums {
+  float P, F, R;
+};
+template <int NT>
+__device__ __forceinline__ Sums sum_row(const DistillArgs& g, const Known& q, const Parts<NT>& s) {
+  Sums o = {0.f, 0.f, 0.f};
 #pragma unroll
-  for (int i = 0; i < LW; ++i) {
-    P += s.P[i];
-    F += s.f[i];
-    R += s.r[i];
+  for (int i = 0; i < kListWaves; ++i) {
+    o.P += s.P[i];
+    o.F += s.F[i];
+    o.R += s.R[i];
   }
-  const float k = w * a.grad_scale * a.inv_temp;
-  Row o;
-  o.zero = k == 0.f || !some;
   if (g.rest) {
-    const float par = pr == 0.f ? 0.f : pr * ar;
-    const bool near = fabsf(ar) <= 1.f;
-    F += (near ? tr * phi(ar) : pr - tr - tr * ar) + over;
-    R += (near ? pr * phi(-ar) : tr - pr + par) - over;
-    *d = (1.f - b) * (p * total - tk) + b * (pa - p * R);
-    o.outside = (1.f - b) * (pr * total - tr) + b * (par - pr * R);
-  } else {
-    *d = (1.f - b) * (p * total - tk) + b * (pa + p - p * (R + P));
-    o.outside = pr * ((1.f - b) * total - b * (R + P));
+    const bool near = fabsf(q.ar) <= 1.f;
+    o.F += (near ? q.tr * phi(q.ar) : q.pr - q.tr - q.tr * q.ar) + q.over;
+    o.R += (near ? q.pr * phi(-q.ar) : q.tr - q.pr + (q.pr == 0.f ? 0.f : q.pr * q.ar)) - q.over;
   }
-  *d *= k;
-  o.outside *= k;
-  if (!some) {
-    F = S64 > 0. ? __builtin_huge_valf() : 0.f;
-    R = 0.f;
+  if (!q.some) {
+    o.F = q.S > 0. ? __builtin_huge_valf() : 0.f;
+    o.R = 0.f;
   }
-  o.loss = (b < 1.f ? (1.f - b) * F : 0.f) + (b > 0.f ? b * R : 0.f);
-  const float v[kTerms] = {o.loss, F, R, (float)S64, P, 1.f, 0.f, 0.f};
-#pragma unroll
-  for (int i = 0; i < kTerms; ++i) o.terms[i] = w != 0.f ? w * v[i] : 0.f;
-  o.m = rest.m;
-  o.c = c;
-  o.log2_s = rest.s == 0.f ? 0.f : logf(rest.s) * kLog2e;
   return o;
+}
+
+// With b = 0 the gradient takes none of the sums.
+__device__ __forceinline__ Row row_grad(const DistillArgs& g, int t, const Mass& rest, const Known& q, const Sums& o, float c) {
+  const float k = g.z.weight[t] * g.z.grad_scale * g.z.inv_temp, b = g.rev;
+  Row r;
+  r.zero = k == 0.f || !q.some;
+  r.m = rest.m;
+  r.c = c;
+  r.log2_s = rest.s == 0.f ? 0.f : logf(rest.s) * kLog2e;
+  r.total = q.total;
+  r.R = b == 0.f ? 0.f : g.rest ? o.R : o.R + o.P - 1.f;
+  r.f = k * (1.f - b);
+  r.b = k * b;
+  const float away = g.rest ? (q.pr == 0.f ? 0.f : q.pr * q.ar) - q.pr * r.R : -q.pr * (r.R + 1.f);
+  r.outside = r.f * (q.pr * q.total - q.tr) + (b == 0.f ? 0.f : r.b * away);
+  return r;
 }
 
 template <typename T>
@@ -327,10 +353,23 @@ __device__ __forceinline__ float outside_of(const Row& o, float l) {
   return __builtin_amdgcn_exp2f(fmaf(l - o.m, o.c, -o.log2_s)) * o.outside;
 }
 
+// This thread's places' gradients, over what it wrote before.
+template <typename T, typename List>
+__device__ __forceinline__ void write_places(const List& s, const Row& r, T* out) {
+  for (int k = s.head[threadIdx.x]; k >= 0; k = s.next[k])
+    if (s.id[k] >= 0) store1(out + s.id[k], r.f * (s.p[k] * r.total - s.t[k]) + (r.b == 0.f ? 0.f : r.b * (s.pa[k] - s.p[k] * r.R)));
+}
+
 // What thread 0 of a row writes beside the gradient; with counts also its arrival.
-__device__ __forceinline__ uint64_t write_result(const DistillArgs& g, int t, const Row& o) {
-  write_terms(g.z, t, o.terms);
-  if (g.losses) g.losses[t] = o.loss;
+__device__ __forceinline__ uint64_t write_result(const DistillArgs& g, int t, const Sums& o, double S, bool idle) {
+  const float w = g.z.weight[t], b = g.rev;
+  const float loss = (b < 1.f ? (1.f - b) * o.F : 0.f) + (b > 0.f ? b * o.R : 0.f);
+  const float v[kTerms] = {loss, o.F, o.R, (float)S, o.P, 1.f, 0.f, 0.f};
+  float terms[kTerms];
+#pragma unroll
+  for (int i = 0; i < kTerms; ++i) terms[i] = w != 0.f && !idle ? w * v[i] : 0.f;
+  write_terms(g.z, t, terms);
+  if (g.losses) g.losses[t] = loss;
   if (!g.z.counts) return 0;
   parts_written();
   return arrive(g.z.counts, g.z.epoch);
@@ -338,10 +377,6 @@ __device__ __forceinline__ uint64_t write_result(const DistillArgs& g, int t, co
 
 // Whether row t takes no part at all: of weight 0, and its loss not wanted.
 __device__ __forceinline__ bool idle(const DistillArgs& g, int t) { return g.z.weight[t] == 0.f && !g.losses; }
-__device__ __forceinline__ uint64_t write_idle(const DistillArgs& g, int t) {
-  Row o = {};
-  return write_result(g, t, o);
-}
 
 // ------------------------------------------------------------- rows in registers
 
@@ -357,17 +392,18 @@ __device__ __forceinline__ uint64_t distill_row(const DistillArgs& g) {
   T* out = static_cast<T*>(a.dlogits) + (int64_t)t * a.d_stride;
   uint64_t before = 0;
   if (idle(g, t)) {
-    if (threadIdx.x == 0) before = write_idle(g, t);
+    if (threadIdx.x == 0) before = write_result(g, t, Sums{}, 0., true);
     if (a.dlogits) zero_vectors<STREAM>(out, sp, 0, sp.vectors, true, a.V);
     return before;
   }
-  __shared__ Listed<T, NT, NT * (N + L)> list;
+  __shared__ Listed<T, NT, N + L> list;
   __shared__ Parts<NT> parts;
   __shared__ u32x4 more[L ? L : 1][L ? NT : 1];
   static_assert(L % 3 == 0, "three at a time");
   const float c = a.inv_temp * kLog2e;
+  // a list's waves ask for its words' logits before the row's vectors, and wait for no vector to have them
   Place place = load_place(g, t);
-  list.clear();
+  if (place.id >= 0) place.l = load1(row + place.id);
   u32x4 v[N];
 #pragma unroll
   for (int n = 0; n < N; ++n) {
@@ -376,18 +412,16 @@ __device__ __forceinline__ uint64_t distill_row(const DistillArgs& g) {
   }
   const int odd = odd_of<T>(sp, a.V);
   float lodd = odd >= 0 ? load1(row + odd) : -__builtin_huge_valf();
-  if (place.id >= 0) place.l = load1(row + place.id);
+  list.clear();
   __syncthreads();
-  list.enter(place, sp, Range{0, sp.vectors, true});
+  list.template enter<true>(place, sp, Range{0, sp.vectors, true});
   __syncthreads();
-  list.drop_further(place, g.K, a.status);
-  const int live = (sp.vectors - __builtin_amdgcn_readfirstlane((int)threadIdx.x) + NT - 1) / NT;
-#pragma unroll
-  for (int n = 0; n < N; ++n)
-    if (n < live) list.leave_out(v[n], (int)threadIdx.x + n * NT);
+  list.drop_further(place, a.status);
+  const double t64 = sum_list(place, c, parts);
+  list.leave_out(v, 0);
   if (odd >= 0 && list.odd_listed()) lodd = -__builtin_huge_valf();
   Mass x = no_mass();
-  add<T>(x, v, c, live);
+  add<T>(x, v, c, (sp.vectors - __builtin_amdgcn_readfirstlane((int)threadIdx.x) + NT - 1) / NT);
   for (int l = 0; l < L; l += 3) {
     u32x4 m[3];
 #pragma unroll
@@ -395,43 +429,56 @@ __device__ __forceinline__ uint64_t distill_row(const DistillArgs& g) {
       const int i = (int)threadIdx.x + (N + l + j) * NT;
       m[j] = i < sp.vectors ? load_vec<true>(row + sp.head, i) : nothing<T>();
     }
+    list.leave_out(m, N + l);
 #pragma unroll
-    for (int j = 0; j < 3; ++j) {
-      list.leave_out(m[j], (int)threadIdx.x + (N + l + j) * NT);
-      more[l + j][threadIdx.x] = m[j];
-    }
+    for (int j = 0; j < 3; ++j) more[l + j][threadIdx.x] = m[j];
     add<T>(x, m, c);
   }
   add1(x, lodd, c);
-  float d;
-  const Row o = finish_row<NT>(g, t, x, false, place, parts, &d);
-  if (threadIdx.x == 0) before = write_result(g, t, o);
-  if (!a.dlogits) return before;
-  if (o.zero) {
-    zero_vectors<STREAM>(out, sp, 0, sp.vectors, true, a.V);
-    return before;
-  }
-  if (threadIdx.x < kListThreads) list.d[threadIdx.x] = d;
+  x = wave_merge(x, c);
+  if ((threadIdx.x & 63) == 0) parts.rest[wave_id()] = x;
   __syncthreads();
-  auto put = [&](int i, const u32x4& l) {
-    float y[kPer<T>];
-#pragma unroll
-    for (int e = 0; e < kPer<T>; ++e) y[e] = outside_of<T>(o, element<T>(l, e));
-    store_vec<STREAM>(out + sp.head, i, y);
-  };
-#pragma unroll
-  for (int n = 0; n < N; ++n) {
-    const int i = (int)threadIdx.x + n * NT;
-    if (i >= sp.vectors) break;
-    again(v[n]);
-    put(i, v[n]);
+  const Mass rest = waves_merge<NT / 64>(parts.rest, c);
+  const Known q = know_row(g, rest, parts, c);
+  sum_places(g, q, place, t64, list, parts);
+  // without a reverse part the gradient needs no more than this
+  const bool late = g.rev == 0.f;
+  Sums sums = {};
+  if (!late) {
+    __syncthreads();
+    sums = sum_row(g, q, parts);
   }
-  for (int l = 0; l < L; ++l) {
-    const int i = (int)threadIdx.x + (N + l) * NT;
-    if (i < sp.vectors) put(i, more[l][threadIdx.x]);
+  const Row o = row_grad(g, t, rest, q, sums, c);
+  if (a.dlogits) {
+    if (o.zero) {
+      zero_vectors<STREAM>(out, sp, 0, sp.vectors, true, a.V);
+    } else {
+      auto put = [&](int i, const u32x4& l) {
+        float y[kPer<T>];
+#pragma unroll
+        for (int e = 0; e < kPer<T>; ++e) y[e] = outside_of<T>(o, element<T>(l, e));
+        store_vec<STREAM>(out + sp.head, i, y);
+      };
+#pragma unroll
+      for (int n = 0; n < N; ++n) {
+        const int i = (int)threadIdx.x + n * NT;
+        if (i >= sp.vectors) break;
+        again(v[n]);
+        put(i, v[n]);
+      }
+      for (int l = 0; l < L; ++l) {
+        const int i = (int)threadIdx.x + (N + l) * NT;
+        if (i < sp.vectors) put(i, more[l][threadIdx.x]);
+      }
+      if (odd >= 0) store1(out + odd, outside_of<T>(o, lodd));
+    }
   }
-  if (odd >= 0) store1(out + odd, outside_of<T>(o, lodd));
-  list.write(out);
+  if (late) {
+    __syncthreads();
+    if (threadIdx.x == 0) sums = sum_row(g, q, parts);
+  }
+  if (threadIdx.x == 0) before = write_result(g, t, sums, q.S, false);
+  if (a.dlogits && !o.zero) write_places(list, o, out);
   return before;
 }
 
@@ -447,14 +494,15 @@ __global__ __launch_bounds__(NT) void distill_row_kernel(DistillArgs g) {
 
 // ------------------------------------------------------------- parts of rows
 
-constexpr int kWindow = 4096;  // vectors whose bits LDS holds at a time
+constexpr int kWindow = 16;  // vectors of a thread whose bits LDS holds at a time
 
 // Workgroup (row, part): the sums of its words that are not listed, and the listed words' logits.
-template <typename T, int U, bool STREAM>
+template <typename T, int U>
 __global__ __launch_bounds__(kPartThreads) void distill_sums_kernel(DistillArgs g) {
   const LogitsArgs& a = g.z;
   const int t = (int)(blockIdx.x / (uint32_t)a.splits), p = (int)(blockIdx.x - (uint32_t)t * a.splits);
   if (idle(g, t)) return;
+  static_assert(kWindow % U == 0 && U % 4 == 0, "whole batches, of whole words of bits");
   __shared__ Listed<T, kPartThreads, kWindow> list;
   __shared__ Mass parts[kPartThreads / 64];
   const T* row = static_cast<const T*>(a.logits) + (int64_t)t * a.stride;
@@ -462,43 +510,44 @@ __global__ __launch_bounds__(kPartThreads) void distill_sums_kernel(DistillArgs 
   const int first = p * a.chunk, end = min(first + a.chunk, sp.vectors), odd = odd_of<T>(sp, a.V);
   const bool odds = p == a.splits - 1;
   const float c = a.inv_temp * kLog2e;
-  Place place = load_place(g, t);
+  const Place place = load_place(g, t);
   Mass x = no_mass();
-  for (int w0 = first; w0 == first || w0 < end; w0 += kWindow) {
-    const int w1 = min(w0 + kWindow, end);
+  int w0 = first;
+  do {
+    const int w1 = min(w0 + kWindow * kPartThreads, end);
     const bool last = w1 >= end;
+    u32x4 v[U];
+    auto load = [&](int i0) {
+#pragma unroll
+      for (int n = 0; n < U; ++n) {
+        const int i = i0 + n * kPartThreads + (int)threadIdx.x;
+        v[n] = i < w1 ? load_vec<false>(row + sp.head, i) : nothing<T>();
+      }
+    };
+    load(w0);  // on its way while the list is entered
     list.clear();
     __syncthreads();
-    const bool mine = list.enter(place, sp, Range{w0, w1, odds && last});
-    if (mine) place.l = load1(row + place.id);
+    const bool mine = list.template enter<true>(place, sp, Range{w0, w1, odds && last});
+    const float l = mine ? load1(row + place.id) : 0.f;
     __syncthreads();
     Place kept = place;
-    list.drop_further(kept, g.K, a.status);
-    if (mine) reinterpret_cast<float2*>(g.listed)[(int64_t)t * g.K + threadIdx.x] = make_float2(place.l, kept.id >= 0 ? 1.f : 0.f);
-    int i = w0 + (int)threadIdx.x;
-    for (; i + (U - 1) * kPartThreads < w1; i += kPartThreads * U) {
-      u32x4 v[U];
-#pragma unroll
-      for (int n = 0; n < U; ++n) v[n] = load_vec<STREAM>(row + sp.head, i + n * kPartThreads);
-#pragma unroll
-      for (int n = 0; n < U; ++n) list.leave_out(v[n], i + n * kPartThreads - w0);
+    list.drop_further(kept, a.status);
+    for (int n = 0;; n += U) {
+      list.leave_out(v, n);
       add<T>(x, v, c);
+      if (w0 + (n + U) * kPartThreads >= w1) break;
+      load(w0 + (n + U) * kPartThreads);
     }
-    for (; i < w1; i += kPartThreads) {
-      u32x4 v[1] = {load_vec<STREAM>(row + sp.head, i)};
-      list.leave_out(v[0], i - w0);
-      add<T>(x, v, c);
-    }
+    if (mine) reinterpret_cast<float2*>(g.listed)[(int64_t)t * g.K + threadIdx.x] = make_float2(l, kept.id >= 0 ? 1.f : 0.f);
     if (odds && last && odd >= 0 && !list.odd_listed()) add1(x, load1(row + odd), c);
     __syncthreads();
-  }
+    w0 = w1;
+  } while (w0 < end);
   x = wave_merge(x, c);
   if ((threadIdx.x & 63) == 0) parts[threadIdx.x >> 6] = x;
   __syncthreads();
-  if (threadIdx.x) return;
-#pragma unroll
-  for (int i = 1; i < kPartThreads / 64; ++i) x = merge(x, parts[i], c);
-  a.part[(int64_t)t * a.splits + p] = make_float4(x.m, x.s, 0.f, 0.f);
+  x = waves_merge<kPartThreads / 64>(parts, c);
+  if (threadIdx.x == 0) a.part[(int64_t)t * a.splits + p] = make_float4(x.m, x.s, 0.f, 0.f);
 }
 
 // Workgroup (row, part), after distill_sums_kernel: the row's results and the part's gradient.
@@ -514,49 +563,69 @@ __device__ __forceinline__ uint64_t distill_part(const DistillArgs& g) {
   T* out = static_cast<T*>(a.dlogits) + (int64_t)t * a.d_stride;
   uint64_t before = 0;
   if (idle(g, t)) {
-    if (p == 0 && threadIdx.x == 0) before = write_idle(g, t);
+    if (p == 0 && threadIdx.x == 0) before = write_result(g, t, Sums{}, 0., true);
     if (a.dlogits) zero_vectors<STREAM>(out, sp, first, end, odds, a.V);
     return before;
   }
   if (p > 0 && !a.dlogits) return before;
-  __shared__ Listed<T, kPartThreads, 1> list;  // its bits are not needed
+  __shared__ Listed<T, kPartThreads, 1> list;  // its bits are not used
   __shared__ Parts<kPartThreads> parts;
   const float c = a.inv_temp * kLog2e;
   Place place = load_place(g, t);
-  if (place.id >= 0) {
-    const float2 x = reinterpret_cast<const float2*>(g.listed)[(int64_t)t * g.K + threadIdx.x];
-    place.l = x.x;
-    if (x.y == 0.f) place.id = -1;
-  }
   const int lane = (int)(threadIdx.x & 63);
   Mass x = no_mass();
   if (lane < a.splits) {
     const float4 q = a.part[(int64_t)t * a.splits + lane];
     x = Mass{q.x, q.y};
   }
+  if (place.id >= 0) {
+    const float2 q = reinterpret_cast<const float2*>(g.listed)[(int64_t)t * g.K + threadIdx.x];
+    place.l = q.x;
+    if (q.y == 0.f) place.id = -1;
+  }
+  // the part's first vectors are on their way meanwhile
+  constexpr int U = 4;
+  u32x4 v[U];
+  auto load = [&](int i0) {
+#pragma unroll
+    for (int n = 0; n < U; ++n) {
+      const int i = i0 + n * kPartThreads + (int)threadIdx.x;
+      if (i < end) v[n] = load_vec<false>(row + sp.head, i);
+    }
+  };
+  if (a.dlogits) load(first);
   list.head[threadIdx.x] = -1;
+  const double t64 = sum_list(place, c, parts);
   __syncthreads();
-  list.chain(place, sp, Range{first, end, odds});
-  float d;
-  const Row o = finish_row<kPartThreads>(g, t, wave_merge(x, c), true, place, parts, &d);
-  if (p == 0 && threadIdx.x == 0) before = write_result(g, t, o);
+  list.template enter<false>(place, sp, Range{first, end, odds});
+  const Mass rest = wave_merge(x, c);
+  const Known q = know_row(g, rest, parts, c);
+  sum_places(g, q, place, t64, list, parts);
+  __syncthreads();
+  const Sums sums = sum_row(g, q, parts);
+  const Row o = row_grad(g, t, rest, q, sums, c);
+  if (p == 0 && threadIdx.x == 0) before = write_result(g, t, sums, q.S, false);
   if (!a.dlogits) return before;
   if (o.zero) {
     zero_vectors<STREAM>(out, sp, first, end, odds, a.V);
     return before;
   }
-  list.d[threadIdx.x] = d;
-  __syncthreads();
-  for (int i = first + (int)threadIdx.x; i < end; i += kPartThreads) {
-    const u32x4 v = load_vec<false>(row + sp.head, i);
-    float y[kPer<T>];
+  for (int i0 = first; i0 < end;) {
 #pragma unroll
-    for (int e = 0; e < kPer<T>; ++e) y[e] = outside_of<T>(o, element<T>(v, e));
-    store_vec<STREAM>(out + sp.head, i, y);
+    for (int n = 0; n < U; ++n) {
+      const int i = i0 + n * kPartThreads + (int)threadIdx.x;
+      if (i >= end) break;
+      float y[kPer<T>];
+#pragma unroll
+      for (int e = 0; e < kPer<T>; ++e) y[e] = outside_of<T>(o, element<T>(v[n], e));
+      store_vec<STREAM>(out + sp.head, i, y);
+    }
+    i0 += U * kPartThreads;
+    if (i0 < end) load(i0);
   }
   const int odd = odd_of<T>(sp, a.V);
   if (odds && odd >= 0) store1(out + odd, outside_of<T>(o, load1(row + odd)));
-  list.write(out);
+  write_places(list, o, out);
   return before;
 }
 
@@ -603,8 +672,8 @@ hipError_t distill_for(DistillArgs g, hipStream_t s) {
   if (!a.splits && a.V / kPer<T> > kFinishThreads * 16) a.counts = nullptr;  // the sums take a launch of their own
   if (a.splits) {
     const int64_t wgs = (int64_t)a.T * a.splits;
-    const void* k = a.chunk < 8 * kPartThreads ? reinterpret_cast<const void*>(&distill_sums_kernel<T, 4, false>)
-                                               : reinterpret_cast<const void*>(&distill_sums_kernel<T, 8, false>);
+    const void* k = a.chunk <= 4 * kPartThreads ? reinterpret_cast<const void*>(&distill_sums_kernel<T, 4>)
+                                                : reinterpret_cast<const void*>(&distill_sums_kernel<T, 8>);
     e = launch(k, wgs, kPartThreads, g, s);
     k = streamed<T>(a) ? reinterpret_cast<const void*>(&distill_part_kernel<T, true>)
                        : reinterpret_cast<const void*>(&distill_part_kernel<T, false>);
