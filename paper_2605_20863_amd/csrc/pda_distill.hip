@@ -63,21 +63,18 @@ __device__ __forceinline__ void add1(Mass& x, float l, float c) {
   x = rebase(x, m, c);
   x.s += __builtin_amdgcn_exp2f((l - m) * c);
 }
-// The first `live` of N vectors' elements (as for Soft).
+// N vectors' elements (as for Soft).
 template <typename T, int N>
-__device__ __forceinline__ void add(Mass& x, u32x4 (&v)[N], float c, int live = N) {
+__device__ __forceinline__ void add(Mass& x, u32x4* v, float c) {
   float m = x.m;
 #pragma unroll
-  for (int n = 0; n < N; ++n) {
-    if (n >= live) continue;
+  for (int n = 0; n < N; ++n)
 #pragma unroll
     for (int e = 0; e < kPer<T>; ++e) m = fmaxf(m, element<T>(v[n], e));
-  }
   x = rebase(x, m, c);
   float s = 0.f;
 #pragma unroll
   for (int n = 0; n < N; ++n) {
-    if (n >= live) continue;
     again(v[n]);
 #pragma unroll
     for (int e = 0; e < kPer<T>; ++e) s += __builtin_amdgcn_exp2f((element<T>(v[n], e) - m) * c);
@@ -193,7 +190,7 @@ struct Listed {
 
   // Vectors first .. first + N - 1 of this thread's, with their listed words made -inf.
   template <int N>
-  __device__ __forceinline__ void leave_out(u32x4 (&v)[N], int first) const {
+  __device__ __forceinline__ void leave_out(u32x4* v, int first) const {
 #pragma unroll
     for (int n = 0; n < N; ++n) {
       const uint32_t mask = bits[(first + n) / 4][threadIdx.x] >> (first + n) % 4 * 8 & 255;
@@ -380,6 +377,8 @@ __device__ __forceinline__ bool idle(const DistillArgs& g, int t) { return g.z.w
 
 // ------------------------------------------------------------- rows in registers
 
+constexpr int kBatch = 4;  // vectors of a thread whose sums are made at a time
+
 // Workgroup per row, whose vectors stay in its threads' registers (N of a thread)
 // and LDS (L of a thread) between the sums and the gradient: one read and one
 // write of the row. Returns thread 0's arrival.
@@ -399,17 +398,20 @@ __device__ __forceinline__ uint64_t distill_row(const DistillArgs& g) {
   __shared__ Listed<T, NT, N + L> list;
   __shared__ Parts<NT> parts;
   __shared__ u32x4 more[L ? L : 1][L ? NT : 1];
-  static_assert(L % 3 == 0, "three at a time");
+  static_assert(L % kBatch == 0 && N % kBatch == 0, "whole batches");
   const float c = a.inv_temp * kLog2e;
   // a list's waves ask for its words' logits before the row's vectors, and wait for no vector to have them
   Place place = load_place(g, t);
   if (place.id >= 0) place.l = load1(row + place.id);
+  auto load = [&](int n) {
+    const int i = (int)threadIdx.x + n * NT;
+    return i < sp.vectors ? load_vec<true>(row + sp.head, i) : nothing<T>();
+  };
+#pragma unroll
+  for (int l = 0; l < L; ++l) more[l][threadIdx.x] = load(N + l);
   u32x4 v[N];
 #pragma unroll
-  for (int n = 0; n < N; ++n) {
-    const int i = (int)threadIdx.x + n * NT;
-    v[n] = i < sp.vectors ? load_vec<true>(row + sp.head, i) : nothing<T>();
-  }
+  for (int n = 0; n < N; ++n) v[n] = load(n);
   const int odd = odd_of<T>(sp, a.V);
   float lodd = odd >= 0 ? load1(row + odd) : -__builtin_huge_valf();
   list.clear();
@@ -418,21 +420,25 @@ __device__ __forceinline__ uint64_t distill_row(const DistillArgs& g) {
   __syncthreads();
   list.drop_further(place, a.status);
   const double t64 = sum_list(place, c, parts);
-  list.leave_out(v, 0);
   if (odd >= 0 && list.odd_listed()) lodd = -__builtin_huge_valf();
   Mass x = no_mass();
-  add<T>(x, v, c, (sp.vectors - __builtin_amdgcn_readfirstlane((int)threadIdx.x) + NT - 1) / NT);
-  for (int l = 0; l < L; l += 3) {
-    u32x4 m[3];
 #pragma unroll
-    for (int j = 0; j < 3; ++j) {
-      const int i = (int)threadIdx.x + (N + l + j) * NT;
-      m[j] = i < sp.vectors ? load_vec<true>(row + sp.head, i) : nothing<T>();
-    }
-    list.leave_out(m, N + l);
+  for (int l = 0; l < L; l += kBatch) {
+    u32x4 m[kBatch];
 #pragma unroll
-    for (int j = 0; j < 3; ++j) more[l + j][threadIdx.x] = m[j];
-    add<T>(x, m, c);
+    for (int j = 0; j < kBatch; ++j) m[j] = more[l + j][threadIdx.x];
+    list.template leave_out<kBatch>(m, N + l);
+#pragma unroll
+    for (int j = 0; j < kBatch; ++j) more[l + j][threadIdx.x] = m[j];
+    add<T, kBatch>(x, m, c);
+  }
+  // a few vectors at a time, as they come
+  const int live = (sp.vectors - __builtin_amdgcn_readfirstlane((int)threadIdx.x) + NT - 1) / NT;
+#pragma unroll
+  for (int n = 0; n < N; n += kBatch) {
+    if (n >= live) continue;
+    list.template leave_out<kBatch>(v + n, n);
+    add<T, kBatch>(x, v + n, c);
   }
   add1(x, lodd, c);
   x = wave_merge(x, c);
@@ -533,8 +539,8 @@ __global__ __launch_bounds__(kPartThreads) void distill_sums_kernel(DistillArgs 
     Place kept = place;
     list.drop_further(kept, a.status);
     for (int n = 0;; n += U) {
-      list.leave_out(v, n);
-      add<T>(x, v, c);
+      list.template leave_out<U>(v, n);
+      add<T, U>(x, v, c);
       if (w0 + (n + U) * kPartThreads >= w1) break;
       load(w0 + (n + U) * kPartThreads);
     }
@@ -685,7 +691,7 @@ hipError_t distill_for(DistillArgs g, hipStream_t s) {
         : v <= kFinishThreads * 16 ? rows_for<T, kFinishThreads, 16>(g, s)
         : v <= 512 * 16 ? rows_for<T, 512, 16>(g, s)
         : v <= 1024 * 16 ? rows_for<T, 1024, 16>(g, s)
-        : v <= 1024 * 20 ? rows_for<T, 1024, 20>(g, s) : rows_for<T, 1024, 19, 6>(g, s);
+        : v <= 1024 * 20 ? rows_for<T, 1024, 20>(g, s) : rows_for<T, 1024, 20, 4>(g, s);
   }
   if (e != hipSuccess || a.counts) return e;
   return launch(reinterpret_cast<const void*>(&distill_stats_kernel), 1, 1024, a, s);

@@ -39,7 +39,7 @@ struct TopArgs {
 
 // Distillation from a teacher's lists (pda_distill.hip).
 constexpr int kDistillStats = 6;
-constexpr int kListedVectors = 1024 * (19 + 6);  // of a row in registers and LDS, beside its words' bits
+constexpr int kListedVectors = 1024 * (20 + 4);  // of a row in registers and LDS, beside its words' bits
 struct DistillArgs {
   LogitsArgs z;     // no targets; weight, terms, stats, dlogits as for the policy loss
   const int32_t* ids;  // [T, K]
