@@ -27,9 +27,12 @@ namespace pda {
 namespace {
 
 constexpr double kLeastRest = 0x1p-24;  // half a step of float32 below 1: what a sum of t can tell from it
-constexpr int kListThreads = 256;       // the first threads of a workgroup hold a list's places
-static_assert(kMaxTop <= kListThreads, "a place a thread");
-static_assert(kPartThreads >= kListThreads, "in every workgroup");
+
+// A list's places are the first threads' of a workgroup of NT, one each up to 256, or all threads' in turn.
+template <int NT>
+constexpr int kPlaces = NT < kMaxTop ? kMaxTop / NT : 1;
+template <int NT>
+constexpr int kListWaves = (NT < kMaxTop ? NT : kMaxTop) / 64;
 
 // e^x - 1 - x
 __device__ __forceinline__ float phi(float x) {
@@ -111,23 +114,26 @@ __device__ __forceinline__ Mass waves_merge(const Mass* parts, float c) {
 
 // ------------------------------------------------------------- the list
 
-// A place of a row's list, thread k's the k-th.
+// A place of a row's list: thread t's n-th is the (t + n NT)-th.
 struct Place {
   int id;  // -1: no word
-  float tau, l;
+  float tau, l, t;
 };
-__device__ __forceinline__ Place load_place(const DistillArgs& g, int t) {
-  Place p = {-1, 0.f, kLowest};
-  const int k = (int)threadIdx.x;
-  if (k >= g.K) return p;
-  p.id = g.ids[(int64_t)t * g.K + k];
-  p.tau = g.tau[(int64_t)t * g.K + k];
-  if (p.id >= g.z.V) {
-    atomicOr(g.z.status, kStatusBadTarget);
-    p.id = -1;
+template <int NT>
+__device__ __forceinline__ void load_places(const DistillArgs& g, int t, Place (&p)[kPlaces<NT>]) {
+#pragma unroll
+  for (int n = 0; n < kPlaces<NT>; ++n) {
+    p[n] = Place{-1, 0.f, kLowest, 0.f};
+    const int k = (int)threadIdx.x + n * NT;
+    if (k >= g.K) continue;
+    p[n].id = g.ids[(int64_t)t * g.K + k];
+    p[n].tau = g.tau[(int64_t)t * g.K + k];
+    if (p[n].id >= g.z.V) {
+      atomicOr(g.z.status, kStatusBadTarget);
+      p[n].id = -1;
+    }
+    if (p[n].id < 0 || p[n].tau == -__builtin_huge_valf()) p[n].id = -1;
   }
-  if (p.id < 0 || p.tau == -__builtin_huge_valf()) p.id = -1;
-  return p;
 }
 
 // Vectors first .. end - 1 of a row, and with `odds` the elements outside of all vectors.
@@ -142,9 +148,9 @@ template <typename T, int NT, int V>
 struct Listed {
   uint32_t bits[(V + 3) / 4][NT];  // a byte for each of a thread's vectors
   uint32_t odd;                    // of the elements outside of all vectors
-  int head[NT], next[kListThreads];  // a thread's places, -1: no more
-  int id[kListThreads];
-  float p[kListThreads], t[kListThreads], pa[kListThreads];  // see Row
+  int head[NT], next[kMaxTop];  // a thread's places, -1: no more
+  int id[kMaxTop];
+  float p[kMaxTop], t[kMaxTop], pa[kMaxTop];  // see Row
   int twice;
 
   __device__ __forceinline__ void clear() {
@@ -154,12 +160,11 @@ struct Listed {
     if (threadIdx.x == 0) odd = twice = 0;
   }
 
-  // After clear() and a barrier: this thread's place goes to the thread that writes its word, and the word's bit is set,
-  // if that is in the range. A barrier later all can be read. MASK: the bits are wanted.
+  // After clear() and a barrier: place k goes to the thread that writes its word, and the word's bit is set, if that is
+  // in the range. A barrier later all can be read. MASK: the bits are wanted.
   template <bool MASK>
-  __device__ __forceinline__ bool enter(const Place& place, const Span& sp, const Range& r) {
-    const int k = (int)threadIdx.x;
-    if (k >= kListThreads) return false;
+  __device__ __forceinline__ bool enter(const Place& place, int k, const Span& sp, const Range& r) {
+    if (k >= kMaxTop) return false;
     id[k] = place.id;
     if (place.id < 0) return false;
     const int at = place.id - sp.head, in = sp.vectors * kPer<T>, n = at / kPer<T> - r.first;
@@ -175,17 +180,23 @@ struct Listed {
     return true;
   }
   // After that barrier: a word's further places leave the list.
-  __device__ __forceinline__ void drop_further(Place& place, int32_t* status) {
+  __device__ __forceinline__ void drop_further(Place (&place)[kPlaces<NT>], int32_t* status) {
     if (!twice) return;
-    const int k = (int)threadIdx.x;
-    bool further = false;
-    if (k < kListThreads)
-      for (int j = 0; j < k; ++j) further |= place.id >= 0 && id[j] == place.id;
-    __syncthreads();
-    if (further) {
-      atomicOr(status, kStatusTwice);
-      place.id = id[k] = -1;
+    bool further[kPlaces<NT>];
+#pragma unroll
+    for (int n = 0; n < kPlaces<NT>; ++n) {
+      const int k = (int)threadIdx.x + n * NT;
+      further[n] = false;
+      if (k < kMaxTop)
+        for (int j = 0; j < k; ++j) further[n] |= place[n].id >= 0 && id[j] == place[n].id;
     }
+    __syncthreads();
+#pragma unroll
+    for (int n = 0; n < kPlaces<NT>; ++n)
+      if (further[n]) {
+        atomicOr(status, kStatusTwice);
+        place[n].id = id[(int)threadIdx.x + n * NT] = -1;
+      }
   }
 
   // Vectors first .. first + N - 1 of this thread's, with their listed words made -inf.
@@ -222,29 +233,34 @@ struct Row {
 // What the waves of a workgroup hand each other.
 template <int NT>
 struct Parts {
-  Mass rest[NT / 64], list[kListThreads / 64];
-  double S[kListThreads / 64];
-  float P[kListThreads / 64], F[kListThreads / 64], R[kListThreads / 64];
+  Mass rest[NT / 64], list[kListWaves<NT>];
+  double S[kListWaves<NT>];
+  float P[kListWaves<NT>], F[kListWaves<NT>], R[kListWaves<NT>];
 };
 
-constexpr int kListWaves = kListThreads / 64;
 __device__ __forceinline__ int wave_id() { return __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)); }
 
-// The list's own sums, by its waves: for the barrier before finish_row. Returns this thread's t.
+// The list's own sums, by its waves: before the barrier in front of know_row.
 template <int NT>
-__device__ __forceinline__ double sum_list(const Place& place, float c, Parts<NT>& s) {
+__device__ __forceinline__ void sum_list(Place (&place)[kPlaces<NT>], float c, Parts<NT>& s) {
   const int wave = wave_id();
-  if (wave >= kListWaves) return 0.;
-  const bool in = place.id >= 0;
+  if (wave >= kListWaves<NT>) return;
   Mass x = no_mass();
-  if (in) add1(x, place.l, c);
+  double S = 0.;
+#pragma unroll
+  for (int n = 0; n < kPlaces<NT>; ++n)
+    if (place[n].id >= 0) {
+      add1(x, place[n].l, c);
+      const double t = exp((double)place[n].tau);
+      place[n].t = (float)t;
+      S += t;
+    }
   x = wave_merge(x, c);
-  const double t = in ? exp((double)place.tau) : 0., S = wave_total(t);
+  S = wave_total(S);
   if ((threadIdx.x & 63) == 0) {
     s.list[wave] = x;
     s.S[wave] = S;
   }
-  return t;
 }
 
 // A row's quantities, from the sums of the words outside of the list, in every thread.
@@ -260,7 +276,7 @@ __device__ __forceinline__ Known know_row(const DistillArgs& g, const Mass& rest
   q.x = rest;
   q.S = 0.;
 #pragma unroll
-  for (int i = 0; i < kListWaves; ++i) {
+  for (int i = 0; i < kListWaves<NT>; ++i) {
     q.x = merge(q.x, s.list[i], c);
     q.S += s.S[i];
   }
@@ -277,25 +293,35 @@ __device__ __forceinline__ Known know_row(const DistillArgs& g, const Mass& rest
   return q;
 }
 
-// This thread's place's part of the divergences, by the list's waves; what its gradient takes goes to `list`.
+// This thread's places' part of the divergences, by the list's waves; what their gradients take goes to `list`.
 template <int NT, typename List>
-__device__ __forceinline__ void sum_places(const DistillArgs& g, const Known& q, const Place& place, double t64, List& list, Parts<NT>& s) {
-  const int wave = wave_id(), k = (int)threadIdx.x;
-  if (wave >= kListWaves) return;
-  const bool in = place.id >= 0;
-  const float lp = q.some ? (place.l - q.x.m) * g.z.inv_temp - q.log_s : -__builtin_huge_valf();
-  const float a = in ? lp - place.tau : 0.f, t = (float)t64, p = in ? expf(lp) : 0.f;
-  const float ta = t == 0.f ? 0.f : t * a, pa = p == 0.f ? 0.f : p * a;
-  float f = -ta, r = pa;
-  if (g.rest) {  // squares where a is near to 0
-    const bool near = fabsf(a) <= 1.f;
-    f = near ? t * phi(a) : p - t - ta;
-    r = near ? p * phi(-a) : t - p + pa;
+__device__ __forceinline__ void sum_places(const DistillArgs& g, const Known& q, const Place (&place)[kPlaces<NT>], List& list, Parts<NT>& s) {
+  const int wave = wave_id();
+  if (wave >= kListWaves<NT>) return;
+  float P = 0.f, F = 0.f, R = 0.f;
+#pragma unroll
+  for (int n = 0; n < kPlaces<NT>; ++n) {
+    const int k = (int)threadIdx.x + n * NT;
+    if (place[n].id < 0) continue;
+    const float lp = q.some ? (place[n].l - q.x.m) * g.z.inv_temp - q.log_s : -__builtin_huge_valf();
+    const float a = lp - place[n].tau, t = place[n].t, p = expf(lp);
+    const float ta = t == 0.f ? 0.f : t * a, pa = p == 0.f ? 0.f : p * a;
+    if (g.rest) {  // squares where a is near to 0
+      const bool near = fabsf(a) <= 1.f;
+      F += near ? t * phi(a) : p - t - ta;
+      R += near ? p * phi(-a) : t - p + pa;
+    } else {
+      F -= ta;
+      R += pa;
+    }
+    P += p;
+    list.p[k] = p;
+    list.t[k] = t;
+    list.pa[k] = pa;
   }
-  list.p[k] = p;
-  list.t[k] = t;
-  list.pa[k] = pa;
-  const float P = wave_total(p), F = wave_total(f), R = wave_total(r);
+  P = wave_total(P);
+  F = wave_total(F);
+  R = wave_total(R);
   if ((threadIdx.x & 63) == 0) {
     s.P[wave] = P;
     s.F[wave] = F;
@@ -311,7 +337,7 @@ template <int NT>
 __device__ __forceinline__ Sums sum_row(const DistillArgs& g, const Known& q, const Parts<NT>& s) {
   Sums o = {0.f, 0.f, 0.f};
 #pragma unroll
-  for (int i = 0; i < kListWaves; ++i) {
+  for (int i = 0; i < kListWaves<NT>; ++i) {
     o.P += s.P[i];
     o.F += s.F[i];
     o.R += s.R[i];
@@ -401,8 +427,11 @@ __device__ __forceinline__ uint64_t distill_row(const DistillArgs& g) {
   static_assert(L % kBatch == 0 && N % kBatch == 0, "whole batches");
   const float c = a.inv_temp * kLog2e;
   // a list's waves ask for its words' logits before the row's vectors, and wait for no vector to have them
-  Place place = load_place(g, t);
-  if (place.id >= 0) place.l = load1(row + place.id);
+  Place place[kPlaces<NT>];
+  load_places<NT>(g, t, place);
+#pragma unroll
+  for (int n = 0; n < kPlaces<NT>; ++n)
+    if (place[n].id >= 0) place[n].l = load1(row + place[n].id);
   auto load = [&](int n) {
     const int i = (int)threadIdx.x + n * NT;
     return i < sp.vectors ? load_vec<true>(row + sp.head, i) : nothing<T>();
@@ -416,10 +445,12 @@ __device__ __forceinline__ uint64_t distill_row(const DistillArgs& g) {
   float lodd = odd >= 0 ? load1(row + odd) : -__builtin_huge_valf();
   list.clear();
   __syncthreads();
-  list.template enter<true>(place, sp, Range{0, sp.vectors, true});
+#pragma unroll
+  for (int n = 0; n < kPlaces<NT>; ++n)
+    list.template enter<true>(place[n], (int)threadIdx.x + n * NT, sp, Range{0, sp.vectors, true});
   __syncthreads();
   list.drop_further(place, a.status);
-  const double t64 = sum_list(place, c, parts);
+  sum_list<NT>(place, c, parts);
   if (odd >= 0 && list.odd_listed()) lodd = -__builtin_huge_valf();
   Mass x = no_mass();
 #pragma unroll
@@ -446,7 +477,7 @@ __device__ __forceinline__ uint64_t distill_row(const DistillArgs& g) {
   __syncthreads();
   const Mass rest = waves_merge<NT / 64>(parts.rest, c);
   const Known q = know_row(g, rest, parts, c);
-  sum_places(g, q, place, t64, list, parts);
+  sum_places<NT>(g, q, place, list, parts);
   // without a reverse part the gradient needs no more than this
   const bool late = g.rev == 0.f;
   Sums sums = {};
@@ -516,7 +547,8 @@ __global__ __launch_bounds__(kPartThreads) void distill_sums_kernel(DistillArgs 
   const int first = p * a.chunk, end = min(first + a.chunk, sp.vectors), odd = odd_of<T>(sp, a.V);
   const bool odds = p == a.splits - 1;
   const float c = a.inv_temp * kLog2e;
-  const Place place = load_place(g, t);
+  Place place[1];
+  load_places<kPartThreads>(g, t, place);
   Mass x = no_mass();
   int w0 = first;
   do {
@@ -533,10 +565,10 @@ __global__ __launch_bounds__(kPartThreads) void distill_sums_kernel(DistillArgs 
     load(w0);  // on its way while the list is entered
     list.clear();
     __syncthreads();
-    const bool mine = list.template enter<true>(place, sp, Range{w0, w1, odds && last});
-    const float l = mine ? load1(row + place.id) : 0.f;
+    const bool mine = list.template enter<true>(place[0], (int)threadIdx.x, sp, Range{w0, w1, odds && last});
+    const float l = mine ? load1(row + place[0].id) : 0.f;
     __syncthreads();
-    Place kept = place;
+    Place kept[1] = {place[0]};
     list.drop_further(kept, a.status);
     for (int n = 0;; n += U) {
       list.template leave_out<U>(v, n);
@@ -544,7 +576,7 @@ __global__ __launch_bounds__(kPartThreads) void distill_sums_kernel(DistillArgs 
       if (w0 + (n + U) * kPartThreads >= w1) break;
       load(w0 + (n + U) * kPartThreads);
     }
-    if (mine) reinterpret_cast<float2*>(g.listed)[(int64_t)t * g.K + threadIdx.x] = make_float2(l, kept.id >= 0 ? 1.f : 0.f);
+    if (mine) reinterpret_cast<float2*>(g.listed)[(int64_t)t * g.K + threadIdx.x] = make_float2(l, kept[0].id >= 0 ? 1.f : 0.f);
     if (odds && last && odd >= 0 && !list.odd_listed()) add1(x, load1(row + odd), c);
     __syncthreads();
     w0 = w1;
@@ -577,17 +609,18 @@ __device__ __forceinline__ uint64_t distill_part(const DistillArgs& g) {
   __shared__ Listed<T, kPartThreads, 1> list;  // its bits are not used
   __shared__ Parts<kPartThreads> parts;
   const float c = a.inv_temp * kLog2e;
-  Place place = load_place(g, t);
+  Place place[1];
+  load_places<kPartThreads>(g, t, place);
   const int lane = (int)(threadIdx.x & 63);
   Mass x = no_mass();
   if (lane < a.splits) {
     const float4 q = a.part[(int64_t)t * a.splits + lane];
     x = Mass{q.x, q.y};
   }
-  if (place.id >= 0) {
+  if (place[0].id >= 0) {
     const float2 q = reinterpret_cast<const float2*>(g.listed)[(int64_t)t * g.K + threadIdx.x];
-    place.l = q.x;
-    if (q.y == 0.f) place.id = -1;
+    place[0].l = q.x;
+    if (q.y == 0.f) place[0].id = -1;
   }
   // the part's first vectors are on their way meanwhile
   constexpr int U = 4;
@@ -601,12 +634,12 @@ __device__ __forceinline__ uint64_t distill_part(const DistillArgs& g) {
   };
   if (a.dlogits) load(first);
   list.head[threadIdx.x] = -1;
-  const double t64 = sum_list(place, c, parts);
+  sum_list<kPartThreads>(place, c, parts);
   __syncthreads();
-  list.template enter<false>(place, sp, Range{first, end, odds});
+  list.template enter<false>(place[0], (int)threadIdx.x, sp, Range{first, end, odds});
   const Mass rest = wave_merge(x, c);
   const Known q = know_row(g, rest, parts, c);
-  sum_places(g, q, place, t64, list, parts);
+  sum_places<kPartThreads>(g, q, place, list, parts);
   __syncthreads();
   const Sums sums = sum_row(g, q, parts);
   const Row o = row_grad(g, t, rest, q, sums, c);
@@ -643,7 +676,11 @@ __global__ __launch_bounds__(kPartThreads) void distill_part_kernel(DistillArgs 
     sum_terms<kPartThreads, 1, kDistillStats>(g.z);
 }
 
-__global__ __launch_bounds__(1024) void distill_stats_kernel(LogitsArgs a) { sum_terms<1024, 8, kDistillStats>(a); }
+// U: rows' terms of a thread on their way at once.
+template <int U>
+__global__ __launch_bounds__(1024) void distill_stats_kernel(LogitsArgs a) {
+  sum_terms<1024, U, kDistillStats>(a);
+}
 
 // ------------------------------------------------------------- launches
 
@@ -665,11 +702,18 @@ bool streamed(const LogitsArgs& a) {
 template <typename T, int NT, int N, int L = 0>
 hipError_t rows_for(const DistillArgs& g, hipStream_t s) {
   const void* k = reinterpret_cast<const void*>(&distill_row_kernel<T, NT, N, L, true>);
-  if constexpr (NT == kFinishThreads) {
+  if constexpr (NT <= kFinishThreads) {
     if (!streamed<T>(g.z)) k = reinterpret_cast<const void*>(&distill_row_kernel<T, NT, N, L, false>);
   }
   return launch(k, g.z.T, NT, g, s);
 }
+
+// Rows from which short ones take a wave or two each: a workgroup's chain (places, listed logits, two barriers, sums,
+// stores) is the same length for them, and more rows are on their way at once. us per call, 256 / 128 / 64 threads
+// a row, 64 places, bf16: 8,192 x 1,000 51 / 38 / 30, x 2,000 57 / 41 / 34, x 4,000 62 / 48 / 45, x 8,000 78 / 68 / 73; 2,000 x 2,000 19.8 /
+// 15.9 / 14.6; 1,000 x 4,000 15.0 / 13.4 / 13.6, x 8,000 17.8 / 17.3 / 17.9; 500 x 2,000 11.4 / 12.0 / 11.4; 300 x 4,000 11.3 / 11.6 / 13.2;
+// f32 4,000 x 4,000 36.3 / 35.6 / 38.5.
+constexpr int kManyRows = 600;
 
 template <typename T>
 hipError_t distill_for(DistillArgs g, hipStream_t s) {
@@ -686,7 +730,10 @@ hipError_t distill_for(DistillArgs g, hipStream_t s) {
     if (e == hipSuccess) e = launch(k, wgs, kPartThreads, g, s);
   } else if (a.T) {
     const int v = a.V / kPer<T>;
-    e = v <= kFinishThreads * 4 ? rows_for<T, kFinishThreads, 4>(g, s)
+    e = a.T >= kManyRows && v <= 64 * 4 ? rows_for<T, 64, 4>(g, s)
+        : a.T >= kManyRows && v <= 64 * 8 ? rows_for<T, 64, 8>(g, s)
+        : a.T >= kManyRows && v <= 128 * 8 ? rows_for<T, 128, 8>(g, s)
+        : v <= kFinishThreads * 4 ? rows_for<T, kFinishThreads, 4>(g, s)
         : v <= kFinishThreads * 8 ? rows_for<T, kFinishThreads, 8>(g, s)
         : v <= kFinishThreads * 16 ? rows_for<T, kFinishThreads, 16>(g, s)
         : v <= 512 * 16 ? rows_for<T, 512, 16>(g, s)
@@ -694,7 +741,9 @@ hipError_t distill_for(DistillArgs g, hipStream_t s) {
         : v <= 1024 * 20 ? rows_for<T, 1024, 20>(g, s) : rows_for<T, 1024, 20, 4>(g, s);
   }
   if (e != hipSuccess || a.counts) return e;
-  return launch(reinterpret_cast<const void*>(&distill_stats_kernel), 1, 1024, a, s);
+  const void* k = a.T <= 8 * kSums ? reinterpret_cast<const void*>(&distill_stats_kernel<8>)
+                                   : reinterpret_cast<const void*>(&distill_stats_kernel<32>);
+  return launch(k, 1, 1024, a, s);
 }
 
 }  // namespace

@@ -95,6 +95,9 @@ def test_distill(lib, t, V):
 
 @pytest.mark.parametrize("t,V,T", [("bf16", 1003, 700), ("f32", 4001, 300), ("bf16", 16_391, 170), ("f32", 8193, 170),
                                    ("bf16", 65_537, 165), ("f32", 40_000, 165), ("bf16", 131_073, 161), ("f32", 70_001, 161),
+                                   ("bf16", 2047, 600), ("bf16", 2056, 601),
+                                   ("f32", 1023, 777), ("f32", 2050, 650), ("bf16", 4096, 640), ("bf16", 8191, 610), ("bf16", 8200, 602),
+                                   ("f32", 4100, 603), ("bf16", 40, 1000), ("f32", 3, 5000),
                                    ("bf16", 170_001, 161), ("bf16", 204_801, 161), ("f32", 102_401, 161), ("bf16", 300_001, 5)])
 def test_many_rows(lib, t, V, T):
     n = 4_000_000 // V + 1
@@ -118,7 +121,7 @@ def base(T, V, K, seed=3, dtype=torch.float32):
     return z, ids, tau, torch.full((T,), 1.0 / T)
 
 
-@pytest.mark.parametrize("T,V", [(6, 500), (6, 40_000), (200, 20_000)])
+@pytest.mark.parametrize("T,V", [(6, 500), (6, 40_000), (200, 20_000), (700, 300), (700, 3000), (610, 8000)])
 def test_lists_out_of_the_ordinary(lib, T, V):
     """No entry, every word listed, the same word twice, words past the vocabulary, masked words."""
     K = 12
@@ -146,7 +149,7 @@ def test_every_word_listed(lib, V, b, rest):
     check(lib, z, ids, tau, w, b, rest, 1.0, 1.0)
 
 
-@pytest.mark.parametrize("T,V", [(9, 700), (9, 40_000), (170, 20_000)])
+@pytest.mark.parametrize("T,V", [(9, 700), (9, 40_000), (170, 20_000), (700, 700), (640, 5000)])
 @pytest.mark.parametrize("b,rest", [(0.0, True), (0.5, True), (1.0, True), (0.0, False), (1.0, False)])
 def test_masks_and_special_values(lib, T, V, b, rest):
     """Masked words in and out of the list, rows of -inf, NaN and infinities in their own rows, rows of weight 0."""
