@@ -25,13 +25,25 @@ __device__ __forceinline__ float logit_of(uint32_t rank) {
 }
 __device__ __forceinline__ uint64_t key_of(float l, int word) { return ((uint64_t)rank_of(l) << 32) | (uint32_t)~word; }
 
-// Keys that may be among the K largest; n of them, in no order.
+constexpr int kWaves = kPartThreads / 64;
+constexpr int kRegion = kRoom / kWaves;  // keys that a wave holds by itself
+constexpr int kRoomy = kRegion - 16;     // of them the vectors', the rest for the elements outside of all vectors
+
+// Keys that may be among the K largest, in no order: while a row is read, each wave's in its own region, afterwards
+// side by side.
 struct Pool {
   uint64_t keys[kRoom];
-  uint64_t bar;      // after keep(): the K-th largest, 0 where there are fewer
-  int count[3];      // of the keys that a batch adds, in turn
+  uint64_t bar;          // after keep(): the K-th largest, 0 where there are fewer
+  int held[2][kWaves];   // of each wave's region, in turn
+  int count;
   uint32_t tops[2 * kPartThreads];
 };
+
+__device__ __forceinline__ int wave_id() { return __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)); }
+// Bits of `mask` below this lane's.
+__device__ __forceinline__ int lanes_before(uint64_t mask) {
+  return (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
+}
 
 // This thread's number, for code that is seldom reached: the compiler works out what follows from it there, rather than
 // once for all at the kernel's start and in registers of its own.
@@ -41,36 +53,55 @@ __device__ __forceinline__ int thread_here() {
   return t;
 }
 
-// A value that at least K of the n ranks are not below, and that is their K-th largest in its upper 16 bits (0 where there
-// are fewer), the same in every lane: a wave settles bit after bit by counting. rank(i): the i-th; N * 64 >= n.
-template <int N, typename F>
-__device__ __forceinline__ uint32_t kth_of(int n, int K, F rank) {
-  uint32_t v[N], c = 0;
-  const int lane = thread_here() & 63;
+// Over the 64 lanes, in each of them.
+__device__ __forceinline__ uint32_t wave_max(uint32_t x) {
 #pragma unroll
-  for (int j = 0; j < N; ++j) v[j] = lane + 64 * j < n ? rank(lane + 64 * j) : 0;
-#pragma unroll 1
-  for (uint32_t bit = 0x80000000u; bit >= 0x10000u; bit >>= 1) {
-    int above = 0;
-#pragma unroll
-    for (int j = 0; j < N; ++j) above += (int)__popcll(__ballot(v[j] >= (c | bit)));
-    if (above >= K) c |= bit;
-  }
-  return c;
+  for (int o = 32; o > 0; o >>= 1) x = max(x, (uint32_t)__shfl_xor((int)x, o, 64));
+  return (uint32_t)__builtin_amdgcn_readfirstlane((int)x);
 }
-__device__ __forceinline__ uint32_t kth_in(const Pool& b, int n, int K) {
-  const auto rank = [&](int i) { return (uint32_t)(b.keys[i] >> 32); };
-  if (n <= 512) return kth_of<8>(n, K, rank);
-  uint32_t c = 0;
-  const int lane = thread_here() & 63;
+
+// Of the ranks that the wave's lanes hold N each of (0: none): one that at least K are not below, and that is their K-th
+// largest in its upper 16 bits, 0 where there are fewer; the same in every lane. Halves what is between `from`, which the
+// K-th largest is not below, and the largest, by counting.
+template <int N>
+__device__ __forceinline__ uint32_t kth_of(const uint32_t (&v)[N], int K, uint32_t from) {
+  uint32_t top = v[0];
+#pragma unroll
+  for (int j = 1; j < N; ++j) top = max(top, v[j]);
+  uint32_t lo = from >> 16, hi = wave_max(top) >> 16;
 #pragma unroll 1
-  for (uint32_t bit = 0x80000000u; bit >= 0x10000u; bit >>= 1) {
-    int above = 0;
-#pragma unroll 4
-    for (int i = 0; i < n; i += 64) above += (int)__popcll(__ballot(i + lane < n && rank(i + lane) >= (c | bit)));
-    if (above >= K) c |= bit;
+  while (lo < hi) {
+    const uint32_t mid = (lo + hi + 1) / 2, least = mid << 16;
+    int n = 0;
+#pragma unroll
+    for (int j = 0; j < N; ++j) n += (int)__popcll(__ballot(v[j] >= least));
+    if (n >= K) lo = mid;
+    else hi = mid - 1;
   }
-  return c;
+  return lo << 16;
+}
+// What the waves hold.
+struct Held {
+  int n[kWaves];
+  __device__ __forceinline__ int all() const { return n[0] + n[1] + n[2] + n[3]; }
+  __device__ __forceinline__ int most() const { return max(max(n[0], n[1]), max(n[2], n[3])); }
+};
+static_assert(kWaves == 4, "Held");
+// Of the keys in the waves' regions, N in each lane from each region.
+template <int N>
+__device__ __forceinline__ uint32_t kth_held(const Pool& b, const Held& h, int K, uint32_t from) {
+  const int lane = thread_here() & 63;
+  uint32_t v[kWaves * N];
+#pragma unroll
+  for (int j = 0; j < kWaves * N; ++j) {
+    const int w = j / N, i = lane + 64 * (j % N);
+    v[j] = i < h.n[w] ? (uint32_t)(b.keys[w * kRegion + i] >> 32) : 0;
+  }
+  return kth_of(v, K, from);
+}
+__device__ __forceinline__ uint32_t kth_held(const Pool& b, const Held& h, int K, uint32_t from) {
+  const int most = h.most();
+  return most <= 128 ? kth_held<2>(b, h, K, from) : most <= 256 ? kth_held<4>(b, h, K, from) : kth_held<kRegion / 64>(b, h, K, from);
 }
 
 // Sorts the first `size` (a power of two) keys, the largest first.
@@ -106,46 +137,84 @@ __device__ __forceinline__ int keep(Pool& b, int n, int K) {
   return min(n, K);
 }
 
-// A logit that words of further batches have to pass: with key `bar` the K-th largest of earlier words, an equal one loses.
-__device__ __forceinline__ float bar_of(uint64_t bar) { return bar ? logit_of((uint32_t)(bar >> 32)) : -__builtin_huge_valf(); }
-
-// Leaves the keys whose rank is not below `least`; returns their number.
-__device__ __forceinline__ int filter(Pool& b, int n, uint32_t least) {
-  constexpr int N = kRoom / kPartThreads;
-  uint64_t v[N];
-  const int tid = thread_here();
-  __syncthreads();
-#pragma unroll
-  for (int j = 0; j < N; ++j) {
-    const int i = tid + j * kPartThreads;
-    v[j] = i < n ? b.keys[i] : 0;
+// This wave's keys of rank `least` and above to the front of its region; returns their number.
+__device__ __forceinline__ int thin(Pool& b, int n, uint32_t least) {
+  uint64_t* keys = b.keys + wave_id() * kRegion;
+  const int lane = thread_here() & 63;
+  int kept = 0;
+#pragma unroll 1
+  for (int i = 0; i < n; i += 64) {  // writes stay behind what has been read
+    const uint64_t key = i + lane < n ? keys[i + lane] : 0;
+    const bool stays = key && (uint32_t)(key >> 32) >= least;
+    const uint64_t mask = __ballot(stays);
+    if (stays) keys[kept + lanes_before(mask)] = key;
+    kept += (int)__popcll(mask);
   }
-  if (threadIdx.x == 0) b.count[0] = 0;
-  __syncthreads();
-#pragma unroll
-  for (int j = 0; j < N; ++j)
-    if (v[j] && (uint32_t)(v[j] >> 32) >= least) b.keys[atomicAdd(&b.count[0], 1)] = v[j];
-  __syncthreads();
-  return b.count[0];
+  return kept;
 }
 
-// The K largest of n keys, put(place, key) for each by some thread, 0 for places without.
+// The waves' keys of rank `least` and above, side by side; returns their number. n: what this wave holds.
+__device__ __forceinline__ int gather(Pool& b, int n, uint32_t least) {
+  constexpr int N = kRegion / 64;
+  const int wave = wave_id(), lane = thread_here() & 63;
+  uint64_t v[N];
+  int kept = 0;
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    v[j] = lane + 64 * j < n ? b.keys[wave * kRegion + lane + 64 * j] : 0;
+    if ((uint32_t)(v[j] >> 32) < least) v[j] = 0;
+    kept += (int)__popcll(__ballot(v[j] != 0));
+  }
+  __syncthreads();  // earlier counts have been read
+  if (lane == 0) b.held[0][wave] = kept;
+  __syncthreads();
+  int at = 0, all = 0;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    at += w < wave ? b.held[0][w] : 0;
+    all += b.held[0][w];
+  }
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    const uint64_t mask = __ballot(v[j] != 0);
+    if (v[j]) b.keys[at + lanes_before(mask)] = v[j];
+    at += (int)__popcll(mask);
+  }
+  __syncthreads();
+  return all;
+}
+
+// The K largest of n keys that lie side by side, put(place, key) for each by some thread, 0 for places without. A key's
+// place is the number of larger ones: counted by several threads for each key, or by one for two.
 template <typename F>
 __device__ __forceinline__ void put_best(Pool& b, int n, int K, F put) {
-  constexpr int kFew = 128, kRanked = 512;
   __syncthreads();
-  if (n > kFew && n > K) n = filter(b, n, kth_in(b, n, K));
-  if (n > kRanked) n = keep(b, n, K);
-#pragma unroll 1
-  for (int i = thread_here(); i < n; i += kPartThreads) {
-    const uint64_t key = b.keys[i];
-    int place = 0;
-#pragma unroll 4
-    for (int j = 0; j < n; ++j) place += b.keys[j] > key;
+  if (n > 2 * kPartThreads) n = keep(b, n, K);
+  const int tid = thread_here();
+  if (n > kPartThreads) {
+    const uint64_t key = b.keys[tid], more = tid + kPartThreads < n ? b.keys[tid + kPartThreads] : 0;
+    int place = 0, after = 0;
+#pragma unroll 8
+    for (int j = 0; j < n; ++j) {
+      const uint64_t other = b.keys[j];
+      place += other > key;
+      after += other > more;
+    }
     if (place < K) put(place, key);
+    if (more && after < K) put(after, more);
+  } else {
+    int each = 1;
+    while (each < 16 && 2 * each * n <= kPartThreads) each *= 2;
+    const int i = tid / each;
+    const uint64_t key = i < n ? b.keys[i] : 0;
+    int place = 0;
+#pragma unroll 8
+    for (int j = tid & (each - 1); j < n; j += each) place += b.keys[j] > key;
+    for (int o = 1; o < each; o *= 2) place += __shfl_xor(place, o, 64);
+    if (key && !(tid & (each - 1)) && place < K) put(place, key);
   }
 #pragma unroll 1
-  for (int k = n + thread_here(); k < K; k += kPartThreads) put(k, (uint64_t)0);
+  for (int k = n + tid; k < K; k += kPartThreads) put(k, (uint64_t)0);
 }
 
 // Offers vectors first .. end - 1 a few words of a thread at a time, looking at the room left in between; the n keys
@@ -159,7 +228,7 @@ __device__ __forceinline__ int offer_slowly(Pool& b, int n, int K, const T* row,
     if (n > kRoom - kStep * kPartThreads || i0 >= stop) n = keep(b, n, K);
     if (i0 >= stop) return n;
     __syncthreads();
-    if (threadIdx.x == 0) b.count[0] = 0;
+    if (threadIdx.x == 0) b.count = 0;
     __syncthreads();
     if (i0 + tid < stop) {
       const int word = sp.head + (i0 + tid) * kStep;
@@ -167,35 +236,63 @@ __device__ __forceinline__ int offer_slowly(Pool& b, int n, int K, const T* row,
       for (int e = 0; e < kStep; ++e) {
         const float l = load1(row + word + e);
         const uint64_t key = key_of(l, word + e);
-        if (l != -__builtin_huge_valf() && key > b.bar) b.keys[n + atomicAdd(&b.count[0], 1)] = key;
+        if (l != -__builtin_huge_valf() && key > b.bar) b.keys[n + atomicAdd(&b.count, 1)] = key;
       }
     }
     __syncthreads();
-    n += b.count[0];
+    n += b.count;
   }
 }
 
-// The K largest words' keys of vectors first .. end - 1 of a row (and of the elements outside of the vectors, with `odds`),
-// and the sums of these. A batch is U vectors of each thread; a word of it is taken if it passes the bar, a lower
-// bound on the K-th largest so far: after the first batch from the largest of each thread's two halves of it, later, when
-// the words seen have doubled, from the keys themselves. Batches go through the words in their order, so that an
-// equal word of a later one loses.
+// What the words of further batches have to pass.
+struct Bar {
+  float least;  // words above it pass; NaN does
+  bool closed;  // none does
+};
+__device__ __forceinline__ Bar bar_at(uint32_t rank) {
+  const float l = logit_of(rank);
+  return l != l ? Bar{__builtin_huge_valf(), true} : Bar{l, false};
+}
+
+// The keys, side by side, of words among which the K largest of vectors first .. end - 1 of a row (and of the elements outside of
+// the vectors, with `odds`) are, their number, and these words' sums. A batch is U vectors of each thread; a word of it is
+// taken if it passes the bar, a lower bound on the K-th largest so far: in the first batch from the largest of
+// each thread's two halves of it, later, when the batches read have doubled, from the keys themselves.
+// Between these points the waves go on by themselves. Batches go through the words in their order, so that an equal word
+// of a later one loses.
 template <typename T, int U, bool STREAM>
 __device__ __forceinline__ int select_part(const T* row, const Span& sp, int V, int first, int end, bool odds, int K, float c,
                                            Pool& b, Soft& x) {
   const float low = -__builtin_huge_valf();
-  const int odd = odds ? odd_of<T>(sp, V) : -1;
+  const int odd = odds ? odd_of<T>(sp, V) : -1, wave = wave_id(), lane = (int)(threadIdx.x & 63);
   const float lodd = odd >= 0 ? load1(row + odd) : low;
   x = none();
   if (odd >= 0) add1(x, lodd, c);
-  if (threadIdx.x < 3) b.count[threadIdx.x] = 0;
-  if (threadIdx.x == 0) b.bar = 0;
-  __syncthreads();
-  if (odd >= 0 && odd < sp.head && lodd != low) b.keys[atomicAdd(&b.count[2], 1)] = key_of(lodd, odd);
-  __syncthreads();
-  int n = b.count[2], turn = 0, batch = 0;
-  float bar = low;
-  for (int i0 = first; i0 < end; i0 += U * kPartThreads, ++batch) {
+  if (threadIdx.x == 0) b.bar = 0;  // read some barriers later
+  uint64_t* keys = b.keys + wave * kRegion;
+  int n = 0, turn = 0;  // n: of this wave's keys
+  Held held = {};
+  const auto take = [&](bool hit, float l, int word) {  // all lanes together
+    const uint64_t mask = __ballot(hit);
+    if (!mask) return;
+    const int at = n + lanes_before(mask);
+    if (hit && at < kRegion) keys[at] = key_of(l, word);
+    n += (int)__popcll(mask);
+  };
+  take(odd >= 0 && odd < sp.head && lodd != low, lodd, odd);
+  const auto share = [&](int n) {
+    if (lane == 0) b.held[turn][wave] = n;
+    __syncthreads();
+    Held h;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) h.n[w] = __builtin_amdgcn_readfirstlane(b.held[turn][w]);
+    turn ^= 1;
+    return h;
+  };
+  Bar bar = {low, false};
+  uint32_t floor = 0;  // the K-th largest rank so far is not below it
+  int since = first, mine = n;  // the vectors that came after the last look at all keys; what this wave held then
+  for (int i0 = first, batch = 0; i0 < end; i0 += U * kPartThreads, ++batch) {
     u32x4 v[U];
     float vm[U];
     const int i = i0 + (int)threadIdx.x;
@@ -235,55 +332,51 @@ __device__ __forceinline__ int select_part(const T* row, const Span& sp, int V, 
       b.tops[threadIdx.x] = rank_of(lo);
       b.tops[kPartThreads + threadIdx.x] = rank_of(hi);
       __syncthreads();
-      const uint32_t r = kth_of<2 * kPartThreads / 64>(2 * kPartThreads, K, [&](int j) { return b.tops[j]; });
+      uint32_t t[2 * kPartThreads / 64];
+#pragma unroll
+      for (int j = 0; j < 2 * kPartThreads / 64; ++j) t[j] = b.tops[lane + 64 * j];
+      const uint32_t r = kth_of(t, K, 0);
       // words of rank r pass (the rank below 0's is no number's)
-      bar = r <= rank_of(low) ? low : r == rank_of(0.f) ? -1e-30f : logit_of(r - 1);
+      bar.least = r <= rank_of(low) ? low : r == rank_of(0.f) ? -1e-30f : logit_of(r - 1);
     }
-    const bool all = x.s != x.s;  // a NaN, which the maxima pass over, or +inf
+    const bool all = x.s != x.s && !bar.closed;  // a NaN, which the maxima pass over, or +inf
 #pragma unroll
     for (int u = 0; u < U; ++u)
-      if (vm[u] > bar || all) {
+      if (__ballot(vm[u] > bar.least || all)) {
         again(v[u]);
 #pragma unroll
         for (int e = 0; e < kPer<T>; ++e) {
           const float l = element<T>(v[u], e);
-          if (!(l <= bar)) {
-            const int at = n + atomicAdd(&b.count[turn], 1);
-            if (at < kRoom) b.keys[at] = key_of(l, sp.head + (i + u * kPartThreads) * kPer<T> + e);
-          }
+          take(!(l <= bar.least), l, sp.head + (i + u * kPartThreads) * kPer<T> + e);
         }
       }
-    __syncthreads();
-    const int more = b.count[turn];
-    const int next = turn == 2 ? 0 : turn + 1, last = turn == 0 ? 2 : turn - 1;
-    if (threadIdx.x == 0) b.count[last] = 0;  // read before this barrier, added to after the next
-    turn = next;
-    if (n + more > kRoom) {
-      n = offer_slowly(b, n, K, row, sp, i0, min(i0 + U * kPartThreads, end));
-      bar = bar_of(b.bar);
+    const int next = i0 + U * kPartThreads;
+    const bool last = next >= end;
+    if (!last && (batch & 63) != 63 && ((batch & (batch + 1)) != 0 || (batch == 0 && K <= kPartThreads / 2))) continue;
+    Held now = share(n);
+    if (now.most() > kRoomy) {  // some are lost: from the last look on again
+      const int total = offer_slowly(b, gather(b, mine, 0), K, row, sp, since, min(next, end));
+      floor = (uint32_t)(b.bar >> 32);
+      bar = b.bar ? bar_at(floor) : Bar{low, false};
+      now = Held{{total, 0, 0, 0}};
+      n = wave == 0 ? total : 0;
       __syncthreads();
-      if (threadIdx.x < 3) b.count[threadIdx.x] = 0;
-      __syncthreads();
-      continue;
+    } else if (!last && now.all() >= K) {
+      floor = kth_held(b, now, K, floor);
+      bar = bar_at(floor);
+      if (now.most() > kRegion / 2) {
+        __syncthreads();
+        n = thin(b, n, floor);
+        now = share(n);
+      }
     }
-    n += more;
-    if (n > kRoom / 2) {
-      n = filter(b, n, kth_in(b, n, K));
-      if (n > kRoom / 2) n = keep(b, n, K);
-      if (n >= K) bar = logit_of(kth_in(b, n, K));
-      __syncthreads();
-      if (threadIdx.x < 3) b.count[threadIdx.x] = 0;
-      __syncthreads();
-    } else if (n >= K && (batch == 0 || (batch & (batch + 1)) == 0)) {
-      bar = logit_of(kth_in(b, n, K));
-    }
+    held = now;
+    mine = n;
+    since = next;
   }
-  __syncthreads();
-  if (threadIdx.x == 0) b.count[0] = 0;
-  __syncthreads();
-  if (odd >= sp.head && lodd != low) b.keys[n + atomicAdd(&b.count[0], 1)] = key_of(lodd, odd);
-  __syncthreads();
-  return n + b.count[0];
+  take(odd >= sp.head && lodd != low, lodd, odd);
+  const uint32_t least = held.all() > kPartThreads / 2 && held.all() > K ? kth_held(b, held, K, floor) : 0;
+  return gather(b, n, least);
 }
 
 // A row's results from its sums, its target's logit and its words' keys.
@@ -307,47 +400,61 @@ __device__ __forceinline__ uint64_t load_key(const uint64_t* p) {
 }
 
 // Joins row t's parts, whose lists are sorted: as each of S lists has K / S keys that are not below its own K / S-th, the
-// smallest of these is a lower bound.
+// smallest of these is a lower bound. What is read is asked for at once.
 __device__ __forceinline__ void join_parts(const TopArgs& g, int t, Pool& b) {
+  constexpr int U = 4;
   const LogitsArgs& a = g.z;
-  const float c = a.inv_temp * kLog2e;
-  const Soft x = first_lane(merge_parts(a, t, c));
-  const RowStats r = row_stats(a, x, load_part(reinterpret_cast<const float*>(a.part + (int64_t)t * a.splits) + 3));
-  if (threadIdx.x == 0) write_stats(g, t, r);
   const uint64_t* lists = g.keys + (int64_t)t * a.splits * g.K;
   const int each = (g.K + a.splits - 1) / a.splits, all = a.splits * g.K;
+  uint64_t keys[U];
+  const auto load = [&](int i0) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int i = i0 + u * kPartThreads + (int)threadIdx.x;
+      keys[u] = i < all ? load_key(lists + i) : 0;
+    }
+  };
+  load(0);
   uint64_t bar = ~(uint64_t)0;
-  for (int s = (int)(threadIdx.x & 63); s < a.splits; s += 64) {
-    const uint64_t key = load_key(lists + s * g.K + each - 1);
-    bar = key < bar ? key : bar;
-  }
+  static_assert(kMaxSplits <= 64, "a lane each");
+  const int s = (int)(threadIdx.x & 63);
+  if (s < a.splits) bar = load_key(lists + s * g.K + each - 1);
+  const float ly = load_part(reinterpret_cast<const float*>(a.part + (int64_t)t * a.splits) + 3);
+  const Soft x = first_lane(merge_parts(a, t, a.inv_temp * kLog2e));
+  const RowStats r = row_stats(a, x, ly);
+  if (threadIdx.x == 0) write_stats(g, t, r);
 #pragma unroll
   for (int o = 1; o < 64; o *= 2) {
     const uint64_t y = __shfl_xor(bar, o, 64);
     bar = y < bar ? y : bar;
   }
-  if (threadIdx.x == 0) b.count[0] = 0, b.count[1] = 0, b.bar = 0;
+  if (threadIdx.x == 0) b.count = 0, b.bar = 0;
   __syncthreads();
-  for (int i = (int)threadIdx.x; i < all; i += kPartThreads) {
-    const uint64_t key = load_key(lists + i);
-    if (!key || key < bar) continue;
-    const int at = atomicAdd(&b.count[0], 1);
-    if (at < kRoom) b.keys[at] = key;
+  for (int i0 = 0;;) {
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (keys[u] && keys[u] >= bar) {
+        const int at = atomicAdd(&b.count, 1);
+        if (at < kRoom) b.keys[at] = keys[u];
+      }
+    i0 += U * kPartThreads;
+    if (i0 >= all) break;
+    load(i0);
   }
   __syncthreads();
-  int n = b.count[0];
-  if (n > kRoom) {
+  int n = b.count;
+  if (n > kRoom) {  // as many at a time as fit behind the K largest
     n = 0;
     for (int i0 = 0; i0 < all; i0 += kPartThreads) {
       if (n > kRoom - kPartThreads) n = keep(b, n, g.K);
       __syncthreads();
-      if (threadIdx.x == 0) b.count[1] = 0;
+      if (threadIdx.x == 0) b.count = 0;
       __syncthreads();
       const int i = i0 + (int)threadIdx.x;
       const uint64_t key = i < all ? load_key(lists + i) : 0;
-      if (key && key > b.bar) b.keys[n + atomicAdd(&b.count[1], 1)] = key;
+      if (key && key > b.bar) b.keys[n + atomicAdd(&b.count, 1)] = key;
       __syncthreads();
-      n += b.count[1];
+      n += b.count;
     }
   }
   put_best(b, n, g.K, [&](int k, uint64_t key) { write_top(g, t, k, key, x, r); });
