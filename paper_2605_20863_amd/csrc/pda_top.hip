@@ -33,9 +33,12 @@ constexpr int kRoomy = kRegion - 16;     // of them the vectors', the rest for t
 // side by side.
 struct Pool {
   uint64_t keys[kRoom];
+  u32x4 queue[kWaves][64];  // vectors that hold a word above the bar, each wave's, to be looked through together
+  int first[kWaves][64];    // their first words
   uint64_t bar;          // after keep(): the K-th largest, 0 where there are fewer
   int held[2][kWaves];   // of each wave's region, in turn
   int count;
+  uint32_t floor;        // a bar on its way from the wave that settled it
   uint32_t tops[2 * kPartThreads];
 };
 
@@ -63,8 +66,8 @@ __device__ __forceinline__ uint32_t wave_max(uint32_t x) {
 // Of the ranks that the wave's lanes hold N each of (0: none): one that at least K are not below, and that is their K-th
 // largest in its upper 16 bits, 0 where there are fewer; the same in every lane. Halves what is between `from`, which the
 // K-th largest is not below, and the largest, by counting.
-template <int N>
-__device__ __forceinline__ uint32_t kth_of(const uint32_t (&v)[N], int K, uint32_t from) {
+template <int N, int M>
+__device__ __forceinline__ uint32_t kth_of(const uint32_t (&v)[M], int K, uint32_t from) {
   uint32_t top = v[0];
 #pragma unroll
   for (int j = 1; j < N; ++j) top = max(top, v[j]);
@@ -97,7 +100,7 @@ __device__ __forceinline__ uint32_t kth_held(const Pool& b, const Held& h, int K
     const int w = j / N, i = lane + 64 * (j % N);
     v[j] = i < h.n[w] ? (uint32_t)(b.keys[w * kRegion + i] >> 32) : 0;
   }
-  return kth_of(v, K, from);
+  return kth_of<kWaves * N>(v, K, from);
 }
 __device__ __forceinline__ uint32_t kth_held(const Pool& b, const Held& h, int K, uint32_t from) {
   const int most = h.most();
@@ -257,7 +260,7 @@ __device__ __forceinline__ Bar bar_at(uint32_t rank) {
 // The keys, side by side, of words among which the K largest of vectors first .. end - 1 of a row (and of the elements outside of
 // the vectors, with `odds`) are, their number, and these words' sums. A batch is U vectors of each thread; a word of it is
 // taken if it passes the bar, a lower bound on the K-th largest so far: in the first batch from the largest of
-// each thread's two halves of it, later, when the batches read have doubled, from the keys themselves.
+// each thread's words of it (or, for many places, of its even and odd vectors), later, when the batches read have doubled, from the keys themselves.
 // Between these points the waves go on by themselves. Batches go through the words in their order, so that an equal word
 // of a later one loses.
 template <typename T, int U, bool STREAM>
@@ -279,6 +282,17 @@ __device__ __forceinline__ int select_part(const T* row, const Span& sp, int V, 
     if (hit && at < kRegion) keys[at] = key_of(l, word);
     n += (int)__popcll(mask);
   };
+  int queued = 0;
+  const auto look_through = [&](const float least) {
+    const u32x4 w = b.queue[wave][lane];
+    const int word = b.first[wave][lane];
+#pragma unroll
+    for (int e = 0; e < kPer<T>; ++e) {
+      const float l = element<T>(w, e);
+      take(lane < queued && !(l <= least), l, word + e);
+    }
+    queued = 0;
+  };
   take(odd >= 0 && odd < sp.head && lodd != low, lodd, odd);
   const auto share = [&](int n) {
     if (lane == 0) b.held[turn][wave] = n;
@@ -290,6 +304,9 @@ __device__ __forceinline__ int select_part(const T* row, const Span& sp, int V, 
     return h;
   };
   Bar bar = {low, false};
+  // one wave of the workgroup, not always the same, settles the bars: the vector ALUs have no time for four
+  const int judge = (int)blockIdx.x % kWaves;
+  const bool few = K <= kPartThreads / 4;
   uint32_t floor = 0;  // the K-th largest rank so far is not below it
   int since = first, mine = n;  // the vectors that came after the last look at all keys; what this wave held then
   for (int i0 = first, batch = 0; i0 < end; i0 += U * kPartThreads, ++batch) {
@@ -323,36 +340,53 @@ __device__ __forceinline__ int select_part(const T* row, const Span& sp, int V, 
     x.s += s;
     x.u += w;
     if (batch == 0) {
-      float lo = vm[0], hi = vm[U / 2];
+      float lo = vm[0], hi = vm[1];
 #pragma unroll
-      for (int u = 1; u < U / 2; ++u) {
+      for (int u = 2; u < U; u += 2) {
         lo = fmaxf(lo, vm[u]);
-        hi = fmaxf(hi, vm[U / 2 + u]);
+        hi = fmaxf(hi, vm[u + 1]);
       }
+      if (few) lo = fmaxf(lo, hi);
       b.tops[threadIdx.x] = rank_of(lo);
-      b.tops[kPartThreads + threadIdx.x] = rank_of(hi);
+      if (!few) b.tops[kPartThreads + threadIdx.x] = rank_of(hi);
       __syncthreads();
-      uint32_t t[2 * kPartThreads / 64];
+      if (wave == judge) {
+        uint32_t t[2 * kWaves], r;
 #pragma unroll
-      for (int j = 0; j < 2 * kPartThreads / 64; ++j) t[j] = b.tops[lane + 64 * j];
-      const uint32_t r = kth_of(t, K, 0);
+        for (int j = 0; j < kWaves; ++j) t[j] = b.tops[lane + 64 * j];
+        if (few) {
+          r = kth_of<kWaves>(t, K, 0);
+        } else {
+#pragma unroll
+          for (int j = kWaves; j < 2 * kWaves; ++j) t[j] = b.tops[lane + 64 * j];
+          r = kth_of<2 * kWaves>(t, K, 0);
+        }
+        if (lane == 0) b.floor = r;
+      }
+      __syncthreads();
+      const uint32_t r = b.floor;
       // words of rank r pass (the rank below 0's is no number's)
       bar.least = r <= rank_of(low) ? low : r == rank_of(0.f) ? -1e-30f : logit_of(r - 1);
     }
     const bool all = x.s != x.s && !bar.closed;  // a NaN, which the maxima pass over, or +inf
 #pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (__ballot(vm[u] > bar.least || all)) {
-        again(v[u]);
-#pragma unroll
-        for (int e = 0; e < kPer<T>; ++e) {
-          const float l = element<T>(v[u], e);
-          take(!(l <= bar.least), l, sp.head + (i + u * kPartThreads) * kPer<T> + e);
-        }
+    for (int u = 0; u < U; ++u) {
+      const bool hit = vm[u] > bar.least || all;
+      const uint64_t mask = __ballot(hit);
+      if (!mask) continue;
+      const int more = (int)__popcll(mask);
+      if (queued + more > 64) look_through(bar.least);
+      if (hit) {
+        const int at = queued + lanes_before(mask);
+        b.queue[wave][at] = v[u];
+        b.first[wave][at] = sp.head + (i + u * kPartThreads) * kPer<T>;
       }
+      queued += more;
+    }
     const int next = i0 + U * kPartThreads;
     const bool last = next >= end;
     if (!last && (batch & 63) != 63 && ((batch & (batch + 1)) != 0 || (batch == 0 && K <= kPartThreads / 2))) continue;
+    if (queued) look_through(bar.least);
     Held now = share(n);
     if (now.most() > kRoomy) {  // some are lost: from the last look on again
       const int total = offer_slowly(b, gather(b, mine, 0), K, row, sp, since, min(next, end));
@@ -362,10 +396,14 @@ __device__ __forceinline__ int select_part(const T* row, const Span& sp, int V, 
       n = wave == 0 ? total : 0;
       __syncthreads();
     } else if (!last && now.all() >= K) {
-      floor = kth_held(b, now, K, floor);
+      if (wave == judge) {
+        floor = kth_held(b, now, K, floor);
+        if (lane == 0) b.floor = floor;
+      }
+      __syncthreads();
+      floor = b.floor;
       bar = bar_at(floor);
       if (now.most() > kRegion / 2) {
-        __syncthreads();
         n = thin(b, n, floor);
         now = share(n);
       }
@@ -375,7 +413,15 @@ __device__ __forceinline__ int select_part(const T* row, const Span& sp, int V, 
     since = next;
   }
   take(odd >= sp.head && lodd != low, lodd, odd);
-  const uint32_t least = held.all() > kPartThreads / 2 && held.all() > K ? kth_held(b, held, K, floor) : 0;
+  uint32_t least = 0;
+  if (held.all() > kPartThreads / 2 && held.all() > K) {
+    if (wave == judge) {
+      least = kth_held(b, held, K, floor);
+      if (lane == 0) b.floor = least;
+    }
+    __syncthreads();
+    least = b.floor;
+  }
   return gather(b, n, least);
 }
 
