@@ -48,13 +48,13 @@ __device__ __forceinline__ float phi(float x) {
   return y * x * x;
 }
 
-// Largest logit and sum of exponentials below it.
+// Largest logit and sum of exponentials below it, as base2 has them.
 struct Mass {
   float m, s;
 };
 __device__ __forceinline__ Mass no_mass() { return Mass{kLowest, 0.f}; }
 __device__ __forceinline__ Mass rebase(const Mass& x, float m, float c) {
-  return Mass{m, x.s * __builtin_amdgcn_exp2f((x.m - m) * c)};
+  return Mass{m, x.s * rescale(x.m, m, c)};
 }
 __device__ __forceinline__ Mass merge(const Mass& a, const Mass& b, float c) {
 #pragma clang fp contract(off)  // the same whichever side is which, so that all lanes agree
@@ -64,7 +64,7 @@ __device__ __forceinline__ Mass merge(const Mass& a, const Mass& b, float c) {
 __device__ __forceinline__ void add1(Mass& x, float l, float c) {
   const float m = fmaxf(x.m, l);
   x = rebase(x, m, c);
-  x.s += __builtin_amdgcn_exp2f((l - m) * c);
+  x.s += __builtin_amdgcn_exp2f(base2(m, c).of(l));
 }
 // N vectors' elements (as for Soft).
 template <typename T, int N>
@@ -75,12 +75,13 @@ __device__ __forceinline__ void add(Mass& x, u32x4* v, float c) {
 #pragma unroll
     for (int e = 0; e < kPer<T>; ++e) m = fmaxf(m, element<T>(v[n], e));
   x = rebase(x, m, c);
+  const Base2 below = base2(m, c);
   float s = 0.f;
 #pragma unroll
   for (int n = 0; n < N; ++n) {
     again(v[n]);
 #pragma unroll
-    for (int e = 0; e < kPer<T>; ++e) s += __builtin_amdgcn_exp2f((element<T>(v[n], e) - m) * c);
+    for (int e = 0; e < kPer<T>; ++e) s += __builtin_amdgcn_exp2f(below.of(element<T>(v[n], e)));
     asm volatile("" : "+v"(s));  // one vector's elements after another's
   }
   x.s += s;
@@ -222,10 +223,11 @@ struct Listed {
 
 // ------------------------------------------------------------- a row's results
 
-// A row's gradient, by the word's logit: outside of the list exp2((l - m) c - log2_s) outside, of a place's word
+// A row's gradient, by the word's logit: outside of the list 2^below(l) outside, of a place's word
 // f (p total - t) + b (pa - p R).
 struct Row {
-  float m, c, log2_s, outside;
+  Base2 below;
+  float outside;
   float total, R, f, b;
   bool zero;  // no gradient, whatever the logits
 };
@@ -281,8 +283,8 @@ __device__ __forceinline__ Known know_row(const DistillArgs& g, const Mass& rest
     q.S += s.S[i];
   }
   q.some = q.x.s != 0.f;
-  q.log_s = logf(q.x.s);
-  const float lpr = (rest.m - q.x.m) * g.z.inv_temp + (logf(rest.s) - q.log_s);
+  q.log_s = log_below(q.x.s, q.x.m, c);
+  const float lpr = (rest.m - q.x.m) * g.z.inv_temp + (log_below(rest.s, rest.m, c) - q.log_s);
   q.pr = rest.s != 0.f ? expf(lpr) : 0.f;
   const bool others = g.rest && rest.s != 0.f;
   const double t_rest = others ? fmax(1. - q.S, kLeastRest) : 0.;
@@ -359,21 +361,19 @@ __device__ __forceinline__ Row row_grad(const DistillArgs& g, int t, const Mass&
   const float k = g.z.weight[t] * g.z.grad_scale * g.z.inv_temp, b = g.rev;
   Row r;
   r.zero = k == 0.f || !q.some;
-  r.m = rest.m;
-  r.c = c;
-  r.log2_s = rest.s == 0.f ? 0.f : logf(rest.s) * kLog2e;
+  r.below = base2(rest.m, c);
   r.total = q.total;
   r.R = b == 0.f ? 0.f : g.rest ? o.R : o.R + o.P - 1.f;
   r.f = k * (1.f - b);
   r.b = k * b;
   const float away = g.rest ? (q.pr == 0.f ? 0.f : q.pr * q.ar) - q.pr * r.R : -q.pr * (r.R + 1.f);
-  r.outside = r.f * (q.pr * q.total - q.tr) + (b == 0.f ? 0.f : r.b * away);
+  r.outside = rest.s == 0.f ? 0.f : (r.f * (q.pr * q.total - q.tr) + (b == 0.f ? 0.f : r.b * away)) / rest.s;
   return r;
 }
 
 template <typename T>
 __device__ __forceinline__ float outside_of(const Row& o, float l) {
-  return __builtin_amdgcn_exp2f(fmaf(l - o.m, o.c, -o.log2_s)) * o.outside;
+  return __builtin_amdgcn_exp2f(o.below.of(l)) * o.outside;
 }
 
 // This thread's places' gradients, over what it wrote before.

@@ -178,12 +178,6 @@ __device__ __forceinline__ Soft group_merge(Soft x, float c) {
   return lanes_merge<W>(parts[threadIdx.x % W], c);
 }
 
-// The first lane's sums: a merge's roundings depend on the order of its two sides, so that lanes may differ by one.
-__device__ __forceinline__ Soft first_lane(const Soft& x) {
-  const auto first = [](float y) { return as_f32((uint32_t)__builtin_amdgcn_readfirstlane((int)as_u32(y))); };
-  return Soft{first(x.m), first(x.s), first(x.u)};
-}
-
 // Row t's target, or -1 for a row that takes no part.
 __device__ __forceinline__ int target_of(const LogitsArgs& a, int t) {
   const int64_t y = a.targets64 ? static_cast<const int64_t*>(a.targets)[t] : static_cast<const int32_t*>(a.targets)[t];
@@ -286,5 +280,32 @@ __device__ __forceinline__ void zero_vectors(T* out, const Span& sp, int first, 
   const int odd = odd_of<T>(sp, V);
   if (odds && odd >= 0) store1(out + odd, 0.f);
 }
+
+// ------------------------------------------------------------- sums in base 2
+
+// For exponentials below a logit m, 2^(l c - k) with k = m c rounded, one instruction and one rounding before the
+// exponential: sums of such terms are (exactly) 2^log2_off(m) times those of 2^((l - m) c), so that the rounding of k
+// costs nothing. Where m c is too large for float32, only words equal to m are not 0, which c = 1/2 gives too.
+struct Base2 {
+  float c, k;
+  __device__ __forceinline__ float of(float l) const { return fmaf(l, c, -k); }
+};
+__device__ __forceinline__ Base2 base2(float m, float c) {
+  const float k = m * c;
+  return fabsf(k) < 3e38f ? Base2{c, k} : Base2{0.5f, 0.5f * m};
+}
+__device__ __forceinline__ float log2_off(float m, float c) {
+  const Base2 b = base2(m, c);
+  return b.of(m);
+}
+// What sums below `from` are times, below m >= from.
+__device__ __forceinline__ float rescale(float from, float m, float c) {
+#pragma clang fp contract(off)  // both products rounded, as in base2
+  const Base2 b = base2(m, c);
+  const float k = from * b.c;
+  return __builtin_amdgcn_exp2f(k - b.k);
+}
+// Natural logarithm of a sum below m, had its terms been 2^((l - m) c).
+__device__ __forceinline__ float log_below(float s, float m, float c) { return logf(s) - log2_off(m, c) * (1.f / kLog2e); }
 
 }  // namespace pda

@@ -247,6 +247,59 @@ __device__ __forceinline__ int offer_slowly(Pool& b, int n, int K, const T* row,
   }
 }
 
+// A row's largest logit m, and below it as base2 has them the sums of exponentials and of exponentials times exponents.
+struct Mass {
+  float m, s, u;
+};
+__device__ __forceinline__ Mass rebase(const Mass& x, float m, float c) {
+  const float f = rescale(x.m, m, c), k = base2(x.m, c).k - base2(m, c).k;
+  return Mass{m, x.s * f, f * fmaf(x.s, fmaxf(k, kFar), x.u)};
+}
+__device__ __forceinline__ Mass merge(const Mass& a, const Mass& b, float c) {
+  const float m = fmaxf(a.m, b.m);
+  const Mass x = rebase(a, m, c), y = rebase(b, m, c);
+  return Mass{m, x.s + y.s, x.u + y.u};
+}
+__device__ __forceinline__ void add1(Mass& x, float l, float c) {
+  const float m = fmaxf(x.m, l);
+  x = rebase(x, m, c);
+  const float d = base2(m, c).of(l), p = __builtin_amdgcn_exp2f(d);
+  x.s += p;
+  x.u = fmaf(p, fmaxf(d, kFar), x.u);
+}
+template <int N>
+__device__ __forceinline__ Mass lanes_merge(Mass x, float c) {
+#pragma unroll
+  for (int o = 1; o < N; o *= 2)
+    x = merge(x, Mass{__shfl_xor(x.m, o, 64), __shfl_xor(x.s, o, 64), __shfl_xor(x.u, o, 64)}, c);
+  // the first lane's: a merge's roundings depend on the order of its two sides
+  const auto first = [](float y) { return as_f32((uint32_t)__builtin_amdgcn_readfirstlane((int)as_u32(y))); };
+  return N < 64 ? x : Mass{first(x.m), first(x.s), first(x.u)};
+}
+// Over the workgroup, in every thread (and a barrier for all of them).
+__device__ __forceinline__ Mass group_merge(Mass x, float c) {
+  __shared__ Mass parts[kWaves];
+  x = lanes_merge<64>(x, c);
+  if ((threadIdx.x & 63) == 0) parts[threadIdx.x >> 6] = x;
+  __syncthreads();
+  Mass y = parts[0];
+#pragma unroll
+  for (int w = 1; w < kWaves; ++w) y = merge(y, parts[w], c);
+  return y;
+}
+__device__ __forceinline__ RowStats row_stats(const LogitsArgs& a, const Mass& x, float ly) {
+  RowStats r;
+  if (x.s == 0.f) {  // every logit is -inf: no distribution
+    r.lp = -__builtin_huge_valf();
+    r.ent = r.log_s = 0.f;
+    return r;
+  }
+  r.log_s = log_below(x.s, x.m, a.inv_temp * kLog2e);
+  r.lp = (ly - x.m) * a.inv_temp - r.log_s;
+  r.ent = logf(x.s) - x.u / x.s * (1.f / kLog2e);
+  return r;
+}
+
 // What the words of further batches have to pass.
 struct Bar {
   float least;  // words above it pass; NaN does
@@ -265,11 +318,11 @@ __device__ __forceinline__ Bar bar_at(uint32_t rank) {
 // of a later one loses.
 template <typename T, int U, bool STREAM>
 __device__ __forceinline__ int select_part(const T* row, const Span& sp, int V, int first, int end, bool odds, int K, float c,
-                                           Pool& b, Soft& x) {
+                                           Pool& b, Mass& x) {
   const float low = -__builtin_huge_valf();
   const int odd = odds ? odd_of<T>(sp, V) : -1, wave = wave_id(), lane = (int)(threadIdx.x & 63);
   const float lodd = odd >= 0 ? load1(row + odd) : low;
-  x = none();
+  x = Mass{kLowest, 0.f, 0.f};
   if (odd >= 0) add1(x, lodd, c);
   if (threadIdx.x == 0) b.bar = 0;  // read some barriers later
   uint64_t* keys = b.keys + wave * kRegion;
@@ -325,13 +378,14 @@ __device__ __forceinline__ int select_part(const T* row, const Span& sp, int V, 
       m = fmaxf(m, vm[u]);
     }
     x = rebase(x, m, c);
+    const Base2 below = base2(m, c);
     float s = 0.f, w = 0.f;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       again(v[u]);
 #pragma unroll
       for (int e = 0; e < kPer<T>; ++e) {
-        const float d = element<T>(v[u], e) - m, p = __builtin_amdgcn_exp2f(d * c);
+        const float d = below.of(element<T>(v[u], e)), p = __builtin_amdgcn_exp2f(d);
         s += p;
         w = fmaf(p, fmaxf(d, kFar), w);
       }
@@ -426,7 +480,7 @@ __device__ __forceinline__ int select_part(const T* row, const Span& sp, int V, 
 }
 
 // A row's results from its sums, its target's logit and its words' keys.
-__device__ __forceinline__ void write_top(const TopArgs& g, int t, int k, uint64_t key, const Soft& x, const RowStats& r) {
+__device__ __forceinline__ void write_top(const TopArgs& g, int t, int k, uint64_t key, const Mass& x, const RowStats& r) {
   const int64_t at = (int64_t)t * g.K + k;
   g.ids[at] = key ? (int)~(uint32_t)key : -1;
   g.tops[at] = key ? (logit_of((uint32_t)(key >> 32)) - x.m) * g.z.inv_temp - r.log_s : -__builtin_huge_valf();
@@ -437,7 +491,7 @@ __device__ __forceinline__ void write_stats(const TopArgs& g, int t, const RowSt
 }
 // A row that takes no part.
 __device__ __forceinline__ void write_none(const TopArgs& g, int t) {
-  for (int k = (int)threadIdx.x; k < g.K; k += kPartThreads) write_top(g, t, k, 0, none(), RowStats{});
+  for (int k = (int)threadIdx.x; k < g.K; k += kPartThreads) write_top(g, t, k, 0, Mass{}, RowStats{});
   if (threadIdx.x == 0) write_stats(g, t, RowStats{});
 }
 
@@ -466,7 +520,9 @@ __device__ __forceinline__ void join_parts(const TopArgs& g, int t, Pool& b) {
   const int s = (int)(threadIdx.x & 63);
   if (s < a.splits) bar = load_key(lists + s * g.K + each - 1);
   const float ly = load_part(reinterpret_cast<const float*>(a.part + (int64_t)t * a.splits) + 3);
-  const Soft x = first_lane(merge_parts(a, t, a.inv_temp * kLog2e));
+  const float* part = reinterpret_cast<const float*>(a.part + (int64_t)t * a.splits + min(s, a.splits - 1));
+  const Mass mine = {load_part(part), load_part(part + 1), load_part(part + 2)};
+  const Mass x = lanes_merge<64>(s < a.splits ? mine : Mass{kLowest, 0.f, 0.f}, a.inv_temp * kLog2e);
   const RowStats r = row_stats(a, x, ly);
   if (threadIdx.x == 0) write_stats(g, t, r);
 #pragma unroll
@@ -522,9 +578,9 @@ __global__ __launch_bounds__(kPartThreads) void top_kernel(TopArgs g) {
   const Span sp = row_span(row, a.V);
   const int first = p * a.chunk, end = min(first + a.chunk, sp.vectors);
   const float c = a.inv_temp * kLog2e, ly = load1(row + y);
-  Soft x;
+  Mass x;
   const int n = select_part<T, U, STREAM>(row, sp, a.V, first, end, p == a.splits - 1, g.K, c, b, x);
-  x = first_lane(group_merge<kPartThreads>(x, c));
+  x = group_merge(x, c);
   if (a.splits == 1) {
     const RowStats r = row_stats(a, x, ly);
     if (threadIdx.x == 0) write_stats(g, t, r);
