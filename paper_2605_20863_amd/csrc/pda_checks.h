@@ -74,11 +74,11 @@ inline int vectors_of(const LogitsArgs& a) { return a.bf16 ? a.V / 8 : a.V / 4; 
 // (two for each thread) each. Half or twice as many workgroups, or least vectors, are
 // within 10% on every size tried (1 to 3,000 rows of 8,000 to 150,000 words) but for
 // rows of 8,000 words, which 256 vectors a part cut in two: 5.3 - 9.3 us per call, 4.2 - 7.1 whole.
-inline void split_rows(LogitsArgs* a) {
-  constexpr int64_t kWgs = 1024, kLeast = 512;
+inline void split_rows(LogitsArgs* a, int64_t least = 512) {
+  constexpr int64_t kWgs = 1024;
   const int64_t v = vectors_of(*a);
   int64_t s = (kWgs + a->T - 1) / a->T;
-  if (s > v / kLeast) s = v / kLeast;
+  if (s > v / least) s = v / least;
   if (s > kMaxSplits) s = kMaxSplits;
   if (s < 1) s = 1;
   a->chunk = (int32_t)((v + s - 1) / s);

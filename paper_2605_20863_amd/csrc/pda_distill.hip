@@ -209,12 +209,10 @@ struct Listed {
       if (!mask) continue;
 #pragma unroll
       for (int w = 0; w < 4; ++w) {
-        if constexpr (kPer<T> == 8) {
-          v[n][w] = mask >> (2 * w) & 1 ? (v[n][w] & 0xFFFF0000u) | 0xFF80u : v[n][w];
-          v[n][w] = mask >> (2 * w + 1) & 1 ? (v[n][w] & 0xFFFFu) | 0xFF800000u : v[n][w];
-        } else {
-          v[n][w] = mask >> w & 1 ? 0xFF800000u : v[n][w];
-        }
+        // all ones over a listed word's bits
+        const auto ones = [&](int bit) { return (uint32_t)((int32_t)(mask << (31 - bit)) >> 31); };
+        const uint32_t m = kPer<T> == 8 ? (ones(2 * w) & 0xFFFFu) | (ones(2 * w + 1) & 0xFFFF0000u) : ones(w);
+        v[n][w] = (v[n][w] & ~m) | (m & (kPer<T> == 8 ? 0xFF80FF80u : 0xFF800000u));
       }
     }
   }
@@ -407,8 +405,9 @@ constexpr int kBatch = 4;  // vectors of a thread whose sums are made at a time
 
 // Workgroup per row, whose vectors stay in its threads' registers (N of a thread)
 // and LDS (L of a thread) between the sums and the gradient: one read and one
-// write of the row. Returns thread 0's arrival.
-template <typename T, int NT, int N, int L, bool STREAM>
+// write of the row. Of a longer row up to X more vectors of a thread are read again; few enough rows are on their way for the
+// memory-side cache to hold them. Returns thread 0's arrival.
+template <typename T, int NT, int N, int L, int X, bool STREAM>
 __device__ __forceinline__ uint64_t distill_row(const DistillArgs& g) {
   const LogitsArgs& a = g.z;
   const int t = (int)blockIdx.x;
@@ -421,7 +420,7 @@ __device__ __forceinline__ uint64_t distill_row(const DistillArgs& g) {
     if (a.dlogits) zero_vectors<STREAM>(out, sp, 0, sp.vectors, true, a.V);
     return before;
   }
-  __shared__ Listed<T, NT, N + L> list;
+  __shared__ Listed<T, NT, N + L + X> list;
   __shared__ Parts<NT> parts;
   __shared__ u32x4 more[L ? L : 1][L ? NT : 1];
   static_assert(L % kBatch == 0 && N % kBatch == 0, "whole batches");
@@ -464,12 +463,27 @@ __device__ __forceinline__ uint64_t distill_row(const DistillArgs& g) {
     add<T, kBatch>(x, m, c);
   }
   // a few vectors at a time, as they come
+  const auto load_more = [&](int n, u32x4 (&m)[kBatch]) {
+#pragma unroll
+    for (int j = 0; j < kBatch; ++j) {
+      const int i = (int)threadIdx.x + (n + j) * NT;
+      m[j] = i < sp.vectors ? load_vec<false>(row + sp.head, i) : nothing<T>();
+    }
+  };
   const int live = (sp.vectors - __builtin_amdgcn_readfirstlane((int)threadIdx.x) + NT - 1) / NT;
 #pragma unroll
   for (int n = 0; n < N; n += kBatch) {
     if (n >= live) continue;
     list.template leave_out<kBatch>(v + n, n);
     add<T, kBatch>(x, v + n, c);
+  }
+  if constexpr (X > 0) {
+    for (int n = N + L; n < live; n += kBatch) {
+      u32x4 m[kBatch];
+      load_more(n, m);
+      list.template leave_out<kBatch>(m, n);
+      add<T, kBatch>(x, m, c);
+    }
   }
   add1(x, lodd, c);
   x = wave_merge(x, c);
@@ -507,6 +521,17 @@ __device__ __forceinline__ uint64_t distill_row(const DistillArgs& g) {
         const int i = (int)threadIdx.x + (N + l) * NT;
         if (i < sp.vectors) put(i, more[l][threadIdx.x]);
       }
+      if constexpr (X > 0) {
+        for (int n = N + L; n < live; n += kBatch) {
+          u32x4 m[kBatch];
+          load_more(n, m);
+#pragma unroll
+          for (int j = 0; j < kBatch; ++j) {
+            const int i = (int)threadIdx.x + (n + j) * NT;
+            if (i < sp.vectors) put(i, m[j]);
+          }
+        }
+      }
       if (odd >= 0) store1(out + odd, outside_of<T>(o, lodd));
     }
   }
@@ -521,9 +546,9 @@ __device__ __forceinline__ uint64_t distill_row(const DistillArgs& g) {
 
 // Only workgroups of this size finish a counted call's sums (few longer rows go in parts).
 constexpr int kFinishThreads = 256;
-template <typename T, int NT, int N, int L, bool STREAM>
+template <typename T, int NT, int N, int L, int X, bool STREAM>
 __global__ __launch_bounds__(NT) void distill_row_kernel(DistillArgs g) {
-  const uint64_t before = distill_row<T, NT, N, L, STREAM>(g);
+  const uint64_t before = distill_row<T, NT, N, L, X, STREAM>(g);
   if constexpr (NT == kFinishThreads) {
     if (g.z.counts && last_of(before, g.z.epoch, g.z.T)) sum_terms<NT, 1, kDistillStats>(g.z);
   }
@@ -699,11 +724,11 @@ bool streamed(const LogitsArgs& a) {
 }
 
 // Rows of more than kFinishThreads threads come in numbers that make 7 MB and more, and are always streamed.
-template <typename T, int NT, int N, int L = 0>
+template <typename T, int NT, int N, int L = 0, int X = 0>
 hipError_t rows_for(const DistillArgs& g, hipStream_t s) {
-  const void* k = reinterpret_cast<const void*>(&distill_row_kernel<T, NT, N, L, true>);
+  const void* k = reinterpret_cast<const void*>(&distill_row_kernel<T, NT, N, L, X, true>);
   if constexpr (NT <= kFinishThreads) {
-    if (!streamed<T>(g.z)) k = reinterpret_cast<const void*>(&distill_row_kernel<T, NT, N, L, false>);
+    if (!streamed<T>(g.z)) k = reinterpret_cast<const void*>(&distill_row_kernel<T, NT, N, L, X, false>);
   }
   return launch(k, g.z.T, NT, g, s);
 }
@@ -738,7 +763,7 @@ hipError_t distill_for(DistillArgs g, hipStream_t s) {
         : v <= kFinishThreads * 16 ? rows_for<T, kFinishThreads, 16>(g, s)
         : v <= 512 * 16 ? rows_for<T, 512, 16>(g, s)
         : v <= 1024 * 16 ? rows_for<T, 1024, 16>(g, s)
-        : v <= 1024 * 20 ? rows_for<T, 1024, 20>(g, s) : rows_for<T, 1024, 20, 4>(g, s);
+        : v <= 1024 * 20 ? rows_for<T, 1024, 20>(g, s) : rows_for<T, 1024, 20, 4, kListedMore>(g, s);
   }
   if (e != hipSuccess || a.counts) return e;
   const void* k = a.T <= 8 * kSums ? reinterpret_cast<const void*>(&distill_stats_kernel<8>)

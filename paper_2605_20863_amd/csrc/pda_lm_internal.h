@@ -39,7 +39,9 @@ struct TopArgs {
 
 // Distillation from a teacher's lists (pda_distill.hip).
 constexpr int kDistillStats = 6;
-constexpr int kListedVectors = 1024 * (20 + 4);  // of a row in registers and LDS, beside its words' bits
+// Vectors of a row that one workgroup takes: 20 and 4 of 1,024 threads in registers and LDS, beside the words' bits, and 40 more
+// that are read twice.
+constexpr int kListedMore = 40, kListedVectors = 1024 * (20 + 4 + kListedMore);
 struct DistillArgs {
   LogitsArgs z;     // no targets; weight, terms, stats, dlogits as for the policy loss
   const int32_t* ids;  // [T, K]
