@@ -121,7 +121,10 @@ int top_run(const void* logits, const void* targets, int32_t* top_ids, float* to
                        {top_ids, 4, "top_ids", true}, {top_logprobs, 4, "top_logprobs", true}, {logprobs, 4, "logprobs", false},
                        {entropy, 4, "entropy", false}});
   if (rc != PDA_OK) return rc;
-  split_rows(&a);
+  // a part's own chain (a bar, K keys to hand on) is longer than a sum's: parts of at least 2,048 vectors (us per call of 512 /
+  // 1,024 / 2,048 / 4,096; bf16: 64 x 131,072, 20 alternatives 17.1 / 17.1 / 14.9 / 16.6, 64: 17.4 / 17.5 / 16.4 / 19.7, 256: 40 / 41 / 31 /
+  // 33; 1 x 131,072, 20: 12.5 / 11.9 / 12.5 / 14.2; f32: 2 x 150,001, 5: 16.0 / 13.4 / 12.8 / 16.5)
+  split_rows(&a, 2048);
   if ((int64_t)a.T * a.splits > kMaxWaves / 16) return host_fail(PDA_EINVAL, "num_tokens = %d is too much for one call", a.T);
   const int64_t parts = a.splits > 1 ? (int64_t)a.T * a.splits : 0;
   HeldWorkspace ws;

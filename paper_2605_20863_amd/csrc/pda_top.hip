@@ -608,14 +608,225 @@ __global__ __launch_bounds__(kPartThreads) void top_join_kernel(TopArgs g) {
   if (y >= 0) join_parts(g, t, b);
 }
 
+// ------------------------------------------------------------- short rows
+
+// M keys of each lane, key i = r 64 + lane in v[r], sorted, the largest first.
+template <int M>
+__device__ __forceinline__ void sort_wave(uint64_t (&v)[M]) {
+  const int lane = (int)(threadIdx.x & 63);
+#pragma unroll
+  for (int k = 2; k <= 64 * M; k *= 2)
+#pragma unroll
+    for (int j = k / 2; j > 0; j /= 2) {
+      if (j >= 64) {
+#pragma unroll
+        for (int r = 0; r < M; ++r) {
+          const int q = r ^ (j / 64);
+          if (q < r) continue;
+          const bool down = (r * 64 & k) == 0;  // (k > 64: a lane's bits do not matter)
+          const uint64_t a = v[r], b = v[q];
+          const bool swap = (a < b) == down;
+          v[r] = swap ? b : a;
+          v[q] = swap ? a : b;
+        }
+      } else {
+#pragma unroll
+        for (int r = 0; r < M; ++r) {
+          const uint64_t other = __shfl_xor(v[r], j, 64);
+          const bool down = ((r * 64 + lane) & k) == 0, first = (lane & j) == 0;
+          v[r] = (v[r] < other) == (down == first) ? other : v[r];
+        }
+      }
+    }
+}
+
+// Writes the K largest of a wave's n <= 64 M keys.
+template <int M>
+__device__ __forceinline__ void sort_and_write(const TopArgs& g, int t, const uint64_t* keys, int n, const Mass& x, const RowStats& r) {
+  const int lane = (int)(threadIdx.x & 63);
+  uint64_t v[M];
+#pragma unroll
+  for (int j = 0; j < M; ++j) v[j] = lane + 64 * j < n ? keys[lane + 64 * j] : 0;
+  sort_wave(v);
+#pragma unroll
+  for (int j = 0; j < M; ++j)
+    if (lane + 64 * j < g.K) write_top(g, t, lane + 64 * j, v[j], x, r);
+#pragma unroll 1
+  for (int k = lane + 64 * M; k < g.K; k += 64) write_top(g, t, k, 0, x, r);
+}
+
+// A wave per row, whose N vectors of each lane stay in registers. A lower bound on the K-th largest comes from the lanes' vectors'
+// largest; if too many words are above it, the K-th largest itself is found by halving over the words, and of words
+// equal to it the first ones are taken.
+template <typename T, int N>
+__global__ __launch_bounds__(kPartThreads) void top_rows_kernel(TopArgs g) {
+  constexpr int kHold = 256;  // keys of a wave
+  __shared__ uint64_t pools[kWaves][kHold];
+  const LogitsArgs& a = g.z;
+  const int wave = wave_id(), lane = (int)(threadIdx.x & 63), t = (int)blockIdx.x * kWaves + wave;
+  if (t >= a.T) return;
+  uint64_t* keys = pools[wave];
+  int64_t y = 0;
+  if (a.targets) {
+    y = a.targets64 ? static_cast<const int64_t*>(a.targets)[t] : static_cast<const int32_t*>(a.targets)[t];
+    if (y >= a.V && lane == 0) atomicOr(a.status, kStatusBadTarget);
+  }
+  if (y < 0 || y >= a.V) {
+    for (int k = lane; k < g.K; k += 64) write_top(g, t, k, 0, Mass{}, RowStats{});
+    if (lane == 0) write_stats(g, t, RowStats{});
+    return;
+  }
+  const float low = -__builtin_huge_valf(), c = a.inv_temp * kLog2e;
+  const T* row = static_cast<const T*>(a.logits) + (int64_t)t * a.stride;
+  const Span sp = row_span(row, a.V);
+  u32x4 v[N];
+#pragma unroll
+  for (int n = 0; n < N; ++n) v[n] = lane + 64 * n < sp.vectors ? load_vec<false>(row + sp.head, lane + 64 * n) : nothing<T>();
+  const int in = sp.vectors * kPer<T>, odd = lane >= a.V - in ? -1 : lane < sp.head ? lane : lane + in;
+  const float lodd = odd >= 0 ? load1(row + odd) : low, ly = load1(row + y);
+  // sums
+  float vm[N], m = fmaxf(kLowest, lodd);
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    vm[n] = low;
+#pragma unroll
+    for (int e = 0; e < kPer<T>; ++e) vm[n] = fmaxf(vm[n], element<T>(v[n], e));
+    m = fmaxf(m, vm[n]);
+  }
+  Mass x = {m, 0.f, 0.f};
+  {
+    const Base2 below = base2(m, c);
+    const auto add = [&](float l) {
+      const float d = below.of(l), p = __builtin_amdgcn_exp2f(d);
+      x.s += p;
+      x.u = fmaf(p, fmaxf(d, kFar), x.u);
+    };
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      again(v[n]);
+#pragma unroll
+      for (int e = 0; e < kPer<T>; ++e) add(element<T>(v[n], e));
+      asm volatile("" : "+v"(x.s), "+v"(x.u));
+    }
+    add(lodd);
+  }
+  x = lanes_merge<64>(x, c);
+  const RowStats r = row_stats(a, x, ly);
+  if (lane == 0) write_stats(g, t, r);
+
+  // each(f): f(logit, word) for all words, all lanes together, a vector's e-th words at a time
+  const auto each = [&](auto f) {
+    f(lodd, odd);
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      again(v[n]);
+#pragma unroll
+      for (int e = 0; e < kPer<T>; ++e) f(element<T>(v[n], e), sp.head + (lane + 64 * n) * kPer<T> + e);
+      asm volatile("");
+    }
+  };
+  const auto count = [&](float least) {  // words not below it, NaN among them
+    int n = 0;
+    each([&](float l, int) { n += (int)__popcll(__ballot(!(l < least))); });
+    return n;
+  };
+  int held = 0;
+  const auto take = [&](bool hit, float l, int word) {
+    const uint64_t mask = __ballot(hit);
+    if (!mask) return;
+    const int at = held + lanes_before(mask);
+    if (hit && at < kHold) keys[at] = key_of(l, word);
+    held += (int)__popcll(mask);
+  };
+  uint32_t ranks[N];
+#pragma unroll
+  for (int n = 0; n < N; ++n) ranks[n] = vm[n] == low ? 0 : rank_of(vm[n]);
+  const uint32_t least = kth_of<N>(ranks, g.K, 0);
+  const float from = least ? logit_of(least) : low;
+  each([&](float l, int word) { take(!(l < from) && l != low, l, word); });
+  if (held > kHold) {
+    // exactly: ranks in 16 bits for bf16, whose lower 16 are its sign's
+    constexpr int shift = sizeof(T) == 2 ? 16 : 0;
+    const auto value = [&](uint32_t rank) {
+      const uint32_t k = shift ? rank << 16 | (rank & 0x8000u ? 0u : 0xFFFFu) : rank;
+      return logit_of(k);
+    };
+    uint32_t lo = (least ? least : rank_of(-3.402823466e38f)) >> shift, hi = rank_of(__builtin_huge_valf()) >> shift;
+#pragma unroll 1
+    while (lo < hi) {
+      const uint32_t mid = lo + (hi - lo + 1) / 2;
+      if (count(value(mid)) >= g.K) lo = mid;
+      else hi = mid - 1;
+    }
+    const float kth = value(lo);
+    // NaN passes as larger than the K-th, or if these are enough is what the K-th is
+    int above = 0;
+    each([&](float l, int) { above += (int)__popcll(__ballot(!(l <= kth))); });
+    const bool nan = above >= g.K;
+    const auto larger = [&](float l) { return !nan && !(l <= kth); };
+    const auto equal = [&](float l) { return nan ? l != l : l == kth; };
+    held = 0;
+    each([&](float l, int word) { take(larger(l) && l != low, l, word); });
+    // of the equal ones the first in the order of words: head, vectors by lane and element, tail
+    int room = g.K - held;
+    const bool head = odd >= 0 && odd < sp.head;
+    const auto first_of = [&](bool hit, float l, int word) {
+      const uint64_t mask = __ballot(hit);
+      if (room <= 0 || !mask) return;
+      take(hit && lanes_before(mask) < room, l, word);
+      room -= (int)__popcll(mask);
+    };
+    first_of(head && equal(lodd), lodd, odd);
+#pragma unroll 1
+    for (int n = 0; n < N && room > 0; ++n) {
+      u32x4 w = v[0];
+#pragma unroll
+      for (int i = 1; i < N; ++i) w = i == n ? v[i] : w;
+      int before = 0, all = 0;  // equal words of lower lanes, and of all
+#pragma unroll
+      for (int e = 0; e < kPer<T>; ++e) {
+        const uint64_t mask = __ballot(equal(element<T>(w, e)));
+        before += lanes_before(mask);
+        all += (int)__popcll(mask);
+      }
+      if (!all) continue;
+#pragma unroll
+      for (int e = 0; e < kPer<T>; ++e) {
+        const float l = element<T>(w, e);
+        const bool hit = equal(l);
+        take(hit && before < room, l, sp.head + (lane + 64 * n) * kPer<T> + e);
+        before += hit;
+      }
+      room -= all;
+    }
+    first_of(odd >= 0 && !head && equal(lodd), lodd, odd);
+  }
+  if (held <= 64) sort_and_write<1>(g, t, keys, held, x, r);
+  else if (held <= 128) sort_and_write<2>(g, t, keys, held, x, r);
+  else sort_and_write<4>(g, t, keys, held, x, r);
+}
+
+// ------------------------------------------------------------- launches
+
 hipError_t launch(const void* kernel, int64_t wgs, const TopArgs& a, hipStream_t s) {
   TopArgs args = a;
   void* params[] = {&args};
   return hipLaunchKernel(kernel, dim3((unsigned)wgs), dim3(kPartThreads), params, 0, s);
 }
 
+// Whether a wave takes each row: always where 4 vectors of a lane hold it, with 8 where the rows are many. us per call, a
+// workgroup / a wave per row, bf16: 8,192 x 1,000, 20 alternatives 56 / 18, x 2,000 55 / 20, with 256 372 / 61, x 4,000, 20 54 / 28, 256 119 /
+// 102; 300 x 2,000, 20 9.3 / 8.2; 300 x 4,000, 100 11.2 / 13.3; 8 x 4,000, 256 16 / 38; 1 x 2,000, 20 8.0 / 7.5, x 4,000 8.7 / 10.6; f32
+// 4,000 x 1,000, 20 28 / 11, x 2,000, 100 35 / 18.
+constexpr int kManyRows = 600;
+
 template <typename T>
 hipError_t top_for(const TopArgs& a, hipStream_t s) {
+  const int v = a.z.V / kPer<T>;
+  if (v <= 64 * 4 || (v <= 64 * 8 && a.z.T >= kManyRows)) {
+    const void* k = v <= 64 * 4 ? reinterpret_cast<const void*>(&top_rows_kernel<T, 4>) : reinterpret_cast<const void*>(&top_rows_kernel<T, 8>);
+    return launch(k, (a.z.T + kWaves - 1) / kWaves, a, s);
+  }
   const void* k = a.z.chunk < 8 * kPartThreads ? reinterpret_cast<const void*>(&top_kernel<T, 4, false>)
                                                : reinterpret_cast<const void*>(&top_kernel<T, 8, true>);
   const hipError_t e = launch(k, (int64_t)a.z.T * a.z.splits, a, s);

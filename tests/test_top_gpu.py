@@ -38,7 +38,7 @@ def check(lib, z, K, temp, y=None, pad=0, idt=torch.int64):
 
 
 @pytest.mark.parametrize("t", ["f32", "bf16"])
-@pytest.mark.parametrize("V", VOCABS)
+@pytest.mark.parametrize("V", VOCABS + [1029, 2047, 2056, 4100])
 def test_top(lib, t, V):
     for T, pad, temp, K, masked, targets in ((1, 0, 1.0, 1, 0.0, False), (5, 3, 0.7, 20, 0.1, True), (3, 1, 1.0, 256, 0.0, False),
                                              (67, 2, 1.5, 64, 0.02, True), (2, 0, 1.0, 255, 0.5, False)):
@@ -50,7 +50,7 @@ def test_top(lib, t, V):
     assert lib.read_device_status() == 0
 
 
-@pytest.mark.parametrize("t,V,T", [("bf16", 1003, 1500), ("f32", 8191, 1030), ("bf16", 40_001, 1100), ("f32", 50_001, 300),
+@pytest.mark.parametrize("t,V,T", [("bf16", 1003, 1500), ("bf16", 3001, 700), ("bf16", 4103, 650), ("f32", 2051, 605), ("f32", 8191, 1030), ("bf16", 40_001, 1100), ("f32", 50_001, 300),
                                    ("bf16", 131_072, 140)])
 def test_many_rows(lib, t, V, T):
     g = torch.Generator(DEV).manual_seed(V)
@@ -79,12 +79,12 @@ def orders(V):
 
 
 @pytest.mark.parametrize("t", ["f32", "bf16"])
-@pytest.mark.parametrize("V", [700, 20_003, 131_072])
+@pytest.mark.parametrize("V", [260, 700, 2040, 4003, 20_003, 131_072])
 def test_orders(lib, t, V):
     rows = orders(V)
     z = torch.stack(list(rows.values())).to(TYPES[t])
     for K in (1, 17, 256):
-        for T in (1, 40):  # few rows and many
+        for T in (1, 60):  # few rows and many
             print(f"[orders] {t} V={V} K={K} T={T}", flush=True)
             if T == 1:
                 for r in range(len(rows)):
@@ -94,7 +94,7 @@ def test_orders(lib, t, V):
 
 
 @pytest.mark.parametrize("t", ["f32", "bf16"])
-@pytest.mark.parametrize("V", [50, 9000, 70_001])
+@pytest.mark.parametrize("V", [50, 1500, 9000, 70_001])
 @pytest.mark.parametrize("T", [7, 300])
 def test_masks_and_special_values(lib, t, V, T):
     """Rows of -inf, of NaN, with NaN and infinities; rows that take no part."""
@@ -128,7 +128,7 @@ def test_masks_and_special_values(lib, t, V, T):
         R.near(H[rest], wh[rest], bh[rest], torch.float32, "entropies")
 
 
-@pytest.mark.parametrize("V", [3000, 70_001])
+@pytest.mark.parametrize("V", [3000, 9000, 70_001])
 def test_infinities_and_nan_among_each_other(lib, V):
     """More of +inf than places, and NaN before, among and after them; more NaN than places."""
     z = torch.randn((4, V), generator=torch.Generator().manual_seed(V))
