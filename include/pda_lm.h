@@ -91,8 +91,8 @@ int pdalm_add_rms_norm(const void* x,
  *     grad_weight [H] f32 = sum over tokens of g y'   (NULL: not wanted)
  * grad_h may be grad_out or grad_residual where strides agree. The sums are in a
  * fixed order: repeated calls give identical results. out_dtype and scale_group
- * are not read. Uses the stream's workspace (4 bytes for each weight and each of up to 1,024
- * workgroups). Errors as above.
+ * are not read. Uses the stream's workspace (with grad_weight: 4 bytes for each weight and each of 1,024
+ * workgroups, 512 from a width of 1,025 and 256 from 8,193 on). Errors as above.
  */
 int pdalm_add_rms_norm_backward(const void* h,
                                 const void* weight,

@@ -92,9 +92,11 @@ int norm_backward_run(const void* h, const void* weight, const void* grad_out, c
                        {grad_residual, 16, "grad_residual", false}, {grad_h, 16, "grad_h", any},
                        {grad_weight, 4, "grad_weight", false}});
   if (rc != PDA_OK) return rc;
+  // room for the parts of the weights' gradient; long rows have fewer (backward_for)
   constexpr int64_t kWgsPerCu = 4, kMostWgs = 1024;
+  const int64_t room = a.H <= 1024 ? kMostWgs : a.H <= 8192 ? 512 : 256;
   HeldWorkspace ws;
-  if ((rc = hold_workspace(stream, kHeader + (grad_weight ? kMostWgs * a.H * 4 : 0), &ws)) != PDA_OK) return rc;
+  if ((rc = hold_workspace(stream, kHeader + (grad_weight ? room * a.H * 4 : 0), &ws)) != PDA_OK) return rc;
   a.x = h;
   a.res = grad_residual;
   a.w = weight;
@@ -102,7 +104,7 @@ int norm_backward_run(const void* h, const void* weight, const void* grad_out, c
   a.out = const_cast<void*>(grad_out);
   a.dw = grad_weight;
   a.dw_part = reinterpret_cast<float*>(ws.base + kHeader);
-  a.wgs = (int32_t)(kWgsPerCu * ws.cus < kMostWgs ? kWgsPerCu * ws.cus : kMostWgs);
+  a.wgs = (int32_t)(kWgsPerCu * ws.cus < room ? kWgsPerCu * ws.cus : room);
   const hipError_t e = launch_norm_backward(a, stream);
   return e == hipSuccess ? PDA_OK : host_fail_hip(e, "residual norm gradient kernel launch");
 }

@@ -18,10 +18,9 @@
 namespace pda {
 namespace {
 
-constexpr int kThreads = 256;  // of a workgroup, unless a row has more
-
+// Threads of a workgroup: four rows of a wave each, or one row.
 template <int RT>
-constexpr int kGroup = RT < kThreads ? kThreads : RT;
+constexpr int kGroup = RT == 64 ? 256 : RT;
 
 struct Two {
   float a, b;
@@ -41,25 +40,33 @@ __device__ __forceinline__ Two wave_both(Two x) {
   return x;
 }
 
-// The same over a row's RT threads; `turn` alternates between a workgroup's rows, so that
-// one barrier a row does.
-template <int RT, bool MAX>
-__device__ __forceinline__ Two row_both(Two x, int turn) {
-  x = wave_both<MAX>(x);
+// The same over a row's RT threads, M of each added up one after another's, so that RT threads' M give the bits of RT M threads' one;
+// `turn` alternates between a workgroup's rows, so that one barrier a row does.
+template <int RT, bool MAX, int M>
+__device__ __forceinline__ Two row_both(Two (&x)[M], int turn) {
+#pragma unroll
+  for (int m = 0; m < M; ++m) x[m] = wave_both<MAX>(x[m]);
+  const auto join = [](Two& a, const Two& b) {
+    a.a += b.a;
+    a.b = MAX ? fmaxf(a.b, b.b) : a.b + b.b;
+  };
+  Two all = x[0];
   if constexpr (RT > 64) {
     constexpr int W = RT / 64;
-    __shared__ Two parts[2][W];
-    if ((threadIdx.x & 63) == 0) parts[turn & 1][threadIdx.x / 64] = x;
-    __syncthreads();
-    x = parts[turn & 1][0];
+    __shared__ Two parts[2][M][W];
+    if ((threadIdx.x & 63) == 0) {
 #pragma unroll
-    for (int w = 1; w < W; ++w) {
-      const Two y = parts[turn & 1][w];
-      x.a += y.a;
-      x.b = MAX ? fmaxf(x.b, y.b) : x.b + y.b;
+      for (int m = 0; m < M; ++m) parts[turn & 1][m][threadIdx.x / 64] = x[m];
     }
+    __syncthreads();
+    all = parts[turn & 1][0][0];
+#pragma unroll
+    for (int i = 1; i < M * W; ++i) join(all, parts[turn & 1][i / W][i % W]);
+  } else {
+#pragma unroll
+    for (int m = 1; m < M; ++m) join(all, x[m]);
   }
-  return x;
+  return all;
 }
 
 __device__ __forceinline__ void load_weight(const void* w, bool bf16, int at, float (&y)[8]) {
@@ -124,11 +131,14 @@ __global__ __launch_bounds__(kGroup<RT>) void norm_kernel(NormArgs a) {
     x[n] = load8<STREAM, T>(a.x, t * a.x_stride + 8 * i);
     if (a.res) r[n] = load8<STREAM, T>(a.res, t * a.res_stride + 8 * i);
   }
-  Two s = {0.f, 0.f};
+  // up to 2 sums of a thread, for which the calls of few rows have a thread each: a row's results are the same in both
+  constexpr int M = N <= 2 ? N : 1;
+  Two sums[M] = {};
 #pragma unroll
   for (int n = 0; n < N; ++n) {
     const int i = lane + n * RT;
     if (i >= vecs) continue;
+    Two& s = sums[n % M];
     if (a.res) {
       add_rounded(x[n], r[n]);
       if (a.sum) store_raw<STREAM>(a.sum, t * a.sum_stride + 8 * i, x[n]);
@@ -146,7 +156,7 @@ __global__ __launch_bounds__(kGroup<RT>) void norm_kernel(NormArgs a) {
       for (int e = 0; e < 8; ++e) s.b = fmaxf(s.b, fabsf(h[e] * w[e]));
     }
   }
-  s = row_both<RT, true>(s, 0);
+  Two s = row_both<RT, true>(sums, 0);
   const float rms = inv_rms(s.a, a);
   if (FP8 && !a.group) {
     s.b = scale_of(s.b * rms);
@@ -200,7 +210,7 @@ __global__ __launch_bounds__(kGroup<RT>) void norm_backward_kernel(NormArgs a) {
       g[n] = load8<STREAM, T>(a.out, t * a.out_stride + 8 * i);
       if (a.res) q[n] = load8<STREAM, T>(a.res, t * a.res_stride + 8 * i);
     }
-    Two s = {0.f, 0.f};
+    Two sums[1] = {};
 #pragma unroll
     for (int n = 0; n < N; ++n) {
       const int i = lane + n * RT;
@@ -215,10 +225,10 @@ __global__ __launch_bounds__(kGroup<RT>) void norm_backward_kernel(NormArgs a) {
         b = fmaf(h[e], h[e], b);
         c = fmaf(y[e] * w[e], h[e], c);
       }
-      s.a += b;
-      s.b += c;
+      sums[0].a += b;
+      sums[0].b += c;
     }
-    s = row_both<RT, false>(s, turn);
+    const Two s = row_both<RT, false>(sums, turn);
     const float rms = inv_rms(s.a, a), back = s.b / (float)a.H * rms * rms;
 #pragma unroll
     for (int n = 0; n < N; ++n) {
@@ -297,40 +307,74 @@ hipError_t launch(K kernel, int64_t wgs, int threads, const NormArgs& a, hipStre
   return hipLaunchKernel(reinterpret_cast<const void*>(kernel), dim3((unsigned)wgs), dim3((unsigned)threads), params, 0, s);
 }
 
+// Whether the call loads and stores past the caches: from 2^28 bytes on (4 arrays of the stream's type), bf16 alone (a lane's 8 f32
+// elements are two loads of half a cache line's pieces: 16,384 x 2,048 f32 gradient 102 us through, 113 past them). us through
+// them / past them, alone and between the copy that makes x and a product that reads the result (by 1,024 columns):
+//   tokens x width    16,384 x 4,096         8,192 x 4,096         32,768 x 1,024        4,096 x 8,192         2,048 x 16,384        6,144 x 4,096
+//   norm        95.4 / 89.3, 248 / 241  40.1 / 44.6, 139 / 126 39.5 / 43.8, 131 / 125 40.9 / 44.8, 155 / 137 42.4 / 46.2, 210 / 175 30.1 / 33.4, 101 / 101
+//   gradient   115.6 / 113.1, 270 / 265 54.4 / 62.0, 148 / 147 52.4 / 66.6, 159 / 157 58.5 / 62.7, 165 / 159 76.1 / 77.9, 238 / 213 40.9 / 49.5, 108 / 118
+constexpr int64_t kStreamBytes = 1 << 28;
+
+template <typename T>
+bool streamed(const NormArgs& a) {
+  return sizeof(T) == 2 && (int64_t)a.T * a.H * 2 * 4 >= kStreamBytes;
+}
+
 template <typename T, bool FP8, int RT, int N>
 hipError_t norm_rows(const NormArgs& a, hipStream_t s) {
   constexpr int rows = kGroup<RT> / RT;
-  return launch(&norm_kernel<T, RT, N, FP8, false>, (a.T + rows - 1) / rows, kGroup<RT>, a, s);
+  const int64_t wgs = ((int64_t)a.T + rows - 1) / rows;
+  if constexpr (sizeof(T) == 2)
+    if (streamed<T>(a)) return launch(&norm_kernel<T, RT, N, FP8, true>, wgs, kGroup<RT>, a, s);
+  return launch(&norm_kernel<T, RT, N, FP8, false>, wgs, kGroup<RT>, a, s);
 }
+
+// Few rows take twice as many threads each (us per call, bf16, half / all of them: 3 x 4,096 5.2 / 4.3, 64 x 8,192 5.8 / 5.0, 512 x 8,192
+// 10.6 / 10.0, 512 x 4,096 4.8 / 4.6; 2,048 x 4,096 12.0 / 13.0, 16,384 x 8,192 184 / 188).
+constexpr int kFewRows = 1024;
 
 template <typename T, bool FP8>
 hipError_t norm_for(const NormArgs& a, hipStream_t s) {
   const int v = a.H / 8;
+  const bool few = a.T < kFewRows;
   return v <= 64 ? norm_rows<T, FP8, 64, 1>(a, s)
-         : v <= 256 ? norm_rows<T, FP8, 256, 1>(a, s)
-         : v <= 512 ? norm_rows<T, FP8, 256, 2>(a, s)
-         : v <= 1024 ? norm_rows<T, FP8, 256, 4>(a, s)
-         : v <= 2048 ? norm_rows<T, FP8, 512, 4>(a, s) : norm_rows<T, FP8, 1024, 4>(a, s);
+         : v <= 128 ? norm_rows<T, FP8, 128, 1>(a, s)
+         : v <= 256 ? norm_rows<T, FP8, 128, 2>(a, s)
+         : v <= 512 ? (few ? norm_rows<T, FP8, 512, 1>(a, s) : norm_rows<T, FP8, 256, 2>(a, s))
+         : v <= 1024 ? (few ? norm_rows<T, FP8, 1024, 1>(a, s) : norm_rows<T, FP8, 512, 2>(a, s))
+         : v <= 2048 ? norm_rows<T, FP8, 1024, 2>(a, s) : norm_rows<T, FP8, 1024, 4>(a, s);
 }
 
 template <typename T, int RT, int N>
-hipError_t backward_rows(const NormArgs& a, hipStream_t s) {
-  return launch(&norm_backward_kernel<T, RT, N, false>, a.wgs, kGroup<RT>, a, s);
-}
-
-template <typename T>
-hipError_t backward_for(NormArgs a, hipStream_t s) {
-  const int v = a.H / 8, rows = v <= 64 ? 4 : 1;
+hipError_t backward_rows(NormArgs a, hipStream_t s, int most) {
+  constexpr int rows = kGroup<RT> / RT;
   const int64_t wgs = ((int64_t)a.T + rows - 1) / rows;
+  if (a.wgs > most) a.wgs = most;
   if (wgs < a.wgs) a.wgs = (int32_t)wgs;
   hipError_t e = hipSuccess;
-  if (a.wgs) e = v <= 64 ? backward_rows<T, 64, 1>(a, s)
-                 : v <= 256 ? backward_rows<T, 256, 1>(a, s)
-                 : v <= 512 ? backward_rows<T, 256, 2>(a, s)
-                 : v <= 1024 ? backward_rows<T, 256, 4>(a, s)
-                 : v <= 2048 ? backward_rows<T, 512, 4>(a, s) : backward_rows<T, 1024, 4>(a, s);
+  if constexpr (sizeof(T) == 2) {
+    if (streamed<T>(a)) e = launch(&norm_backward_kernel<T, RT, N, true>, a.wgs, kGroup<RT>, a, s);
+    else if (a.wgs) e = launch(&norm_backward_kernel<T, RT, N, false>, a.wgs, kGroup<RT>, a, s);
+  } else {
+    if (a.wgs) e = launch(&norm_backward_kernel<T, RT, N, false>, a.wgs, kGroup<RT>, a, s);
+  }
   if (e != hipSuccess || !a.dw) return e;
   return launch(&norm_weight_grad_kernel, (a.H + 15) / 16, 16 * kSumRows, a, s);
+}
+
+// A workgroup's part of the weights' gradient is as long as a row, written and read again: of long rows there are fewer workgroups,
+// with more threads. us per call of 256 / 512 / 1,024 of them: 16,384 x 4,096 bf16 152 / 111 / 110 (a row by 256 threads), 8,192 x
+// 8,192 121 / 114 / 120, 2,048 x 4,096 24 / 22 / 23, 2,000 x 16,384 73 / 81 / 95, 32,768 x 1,024 (a wave a row) 86 / 70 / 57; of 512 and
+// a row by 512 threads 16,384 x 4,096 104 where 256 took 113, 2,048 x 4,096 20.4.
+template <typename T>
+hipError_t backward_for(const NormArgs& a, hipStream_t s) {
+  const int v = a.H / 8;
+  return v <= 64 ? backward_rows<T, 64, 1>(a, s, 1024)
+         : v <= 128 ? backward_rows<T, 64, 2>(a, s, 1024)
+         : v <= 256 ? backward_rows<T, 256, 1>(a, s, 512)
+         : v <= 512 ? backward_rows<T, 512, 1>(a, s, 512)
+         : v <= 1024 ? backward_rows<T, 512, 2>(a, s, 512)
+         : v <= 2048 ? backward_rows<T, 1024, 2>(a, s, 256) : backward_rows<T, 1024, 4>(a, s, 256);
 }
 
 }  // namespace

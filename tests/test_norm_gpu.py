@@ -154,7 +154,8 @@ def test_gradient(lib, t, H):
             assert torch.equal(b, dh[:, :H]) and torch.equal(again, dw)
 
 
-@pytest.mark.parametrize("T,H", [(4097, 128), (3000, 2048), (2100, 4096), (1500, 16384), (1029, 8)])
+@pytest.mark.parametrize("T,H", [(4097, 128), (3000, 2048), (2100, 4096), (1500, 16384), (1029, 8), (1023, 4096), (1024, 4096), (1025, 8192),
+                                 (1100, 6000), (4500, 1000), (300, 32768)])
 def test_gradient_of_many_rows(lib, T, H):
     """More rows than workgroups."""
     q, h, w = inputs(T, H, torch.bfloat16, torch.bfloat16, T, loud=False)
@@ -168,6 +169,31 @@ def test_gradient_of_many_rows(lib, T, H):
     lib.add_rms_norm(h.to(DEV), w.to(DEV), o, q.to(DEV), s, eps=EPS)
     y, bound = R.norm(s.cpu(), w, EPS)
     R.near(o, y, bound, torch.bfloat16, "norm")
+
+
+@pytest.mark.parametrize("T,H,out", [(8191, 4096, "bf16"), (8192, 4096, "bf16"), (8192, 4096, "fp8"), (32800, 1024, "bf16"), (4100, 8192, "fp8"),
+                                     (70000, 480, "bf16"), (1100, 32768, "bf16")])
+def test_calls_past_the_caches(lib, T, H, out):
+    """Both sides of the size from which rows are loaded and stored past the caches: as the same rows in smaller calls."""
+    dev = lambda seed, amp=1.0: torch.randn((T, H), generator=torch.Generator(DEV).manual_seed(seed), device=DEV).mul_(amp).to(torch.bfloat16)  # noqa: E731
+    x, res, g = dev(1), dev(2, 3.0), dev(3, 0.1)
+    w = (1 + rand((H,), 4, amp=0.2)).to(DEV)
+    o, s, dh, dw = torch.empty((T, H), dtype=TYPES[out], device=DEV), torch.empty_like(x), torch.empty_like(x), torch.empty(H, device=DEV)
+    scales = torch.empty(T, device=DEV) if out == "fp8" else None
+    lib.add_rms_norm(x, w, o, res, s, scales, eps=EPS)
+    lib.add_rms_norm_backward(s, w, g, dh, dw, res, eps=EPS)
+    assert torch.equal(s, (x.float() + res.float()).to(torch.bfloat16))
+    total = torch.zeros(H, dtype=torch.float64)
+    for i in range(0, T, 2000):
+        at = slice(i, min(T, i + 2000))
+        a, b, c, d = torch.empty_like(o[at]), torch.empty_like(dh[at]), torch.empty(H, device=DEV), scales if scales is None else torch.empty_like(scales[at])
+        lib.add_rms_norm(s[at], w, a, scales=d, eps=EPS)
+        lib.add_rms_norm_backward(s[at], w, g[at], b, c, res[at], eps=EPS)
+        assert torch.equal(a.view(torch.uint8), o[at].view(torch.uint8)) and torch.equal(b, dh[at])
+        total += c.cpu().double()
+    _, _, wdw, dwb = R.norm_grad(s[:2000].cpu(), w.cpu(), g[:2000].cpu(), None, EPS)
+    # more rows of the same kind: terms and bounds grow with their number, sums in a workgroup with its rows
+    assert ((dw.cpu().double() - total).abs() <= 2 * dwb * (T / 2000 + 1) * (1 + T / 512 / 24) + 2 * R.EPS24 * total.abs()).all()
 
 
 def test_gradient_against_differences(lib):
