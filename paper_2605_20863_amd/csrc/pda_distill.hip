@@ -723,11 +723,11 @@ bool streamed(const LogitsArgs& a) {
   return (int64_t)a.T * a.V * (int64_t)sizeof(T) >= kStreamBytes;
 }
 
-// Rows of more than kFinishThreads threads come in numbers that make 7 MB and more, and are always streamed.
+// Rows of 1,024 threads come in numbers that make 5 MB and more, and are always streamed.
 template <typename T, int NT, int N, int L = 0, int X = 0>
 hipError_t rows_for(const DistillArgs& g, hipStream_t s) {
   const void* k = reinterpret_cast<const void*>(&distill_row_kernel<T, NT, N, L, X, true>);
-  if constexpr (NT <= kFinishThreads) {
+  if constexpr (NT <= 512) {
     if (!streamed<T>(g.z)) k = reinterpret_cast<const void*>(&distill_row_kernel<T, NT, N, L, X, false>);
   }
   return launch(k, g.z.T, NT, g, s);

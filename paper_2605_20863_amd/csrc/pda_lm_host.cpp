@@ -170,11 +170,14 @@ int distill_run(const void* logits, const int32_t* teacher_ids, const float* tea
                        {losses, 4, "losses", false}, {dlogits, e, "dlogits", false}});
   if (rc != PDA_OK) return rc;
   if (a.T > kMaxWaves / 64) return host_fail(PDA_EINVAL, "num_tokens = %d is too much for one call", a.T);
-  // Rows in registers (and LDS) where they fit and either there are enough of them for the
-  // compute units or they are short; otherwise in parts, read twice (as the policy loss).
-  constexpr int kManyBf16 = 160, kManyF32 = 112, kShortVectors = 3200;
+  // A workgroup a row where it can take one and rows are short or as many as a 220th of their vectors; otherwise in parts, read twice
+  // (us per call, rows / parts, 64 places; bf16: 16,000 words, 1 row 9.4 / 12.1, 200 12.2 / 16.7; 32,000, 1 11.8 / 12.5, 64 14.0 / 15.5;
+  // 50,000, 8 14.5 / 13.4, 32 15.0 / 14.4, 64 15.2 / 17.2; 131,072, 1 22 / 12, 64 24.0 / 19.4, 96 24.5 / 24.5, 160 26 / 36; 200,000, 64 34 / 23,
+  // 128 35 / 37; f32: 20,000, 1 10.6 / 12.0; 50,001, 32 16.5 / 15.0, 64 16.9 / 16.7, 128 18.4 / 21.7; 110,000, 64 27 / 22, 128 32 / 36).
+  constexpr int kShortVectors = 4096, kShare = 220, kMany = 128;
   const int v = vectors_of(a);
-  if (any && ((a.T < (a.bf16 ? kManyBf16 : kManyF32) && v > kShortVectors) || v > kListedVectors)) split_rows(&a);
+  const bool rows = v <= kListedVectors && (v <= kShortVectors || a.T >= kMany || (int64_t)a.T * kShare >= v);
+  if (any && !rows) split_rows(&a);
   const int64_t terms = ((int64_t)a.T * kTerms * 4 + 255) / 256 * 256, parts = (int64_t)a.T * a.splits * 16;
   HeldWorkspace ws;
   if ((rc = hold_workspace(stream, kHeader + terms + parts + (parts ? (int64_t)a.T * op->num_listed * 8 : 0), &ws)) != PDA_OK) return rc;

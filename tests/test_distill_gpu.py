@@ -98,7 +98,11 @@ def test_distill(lib, t, V):
                                    ("bf16", 2047, 600), ("bf16", 2056, 601),
                                    ("f32", 1023, 777), ("f32", 2050, 650), ("bf16", 4096, 640), ("bf16", 8191, 610), ("bf16", 8200, 602),
                                    ("f32", 4100, 603), ("bf16", 40, 1000), ("f32", 3, 5000),
-                                   ("bf16", 170_001, 161), ("bf16", 204_801, 161), ("f32", 102_401, 161), ("bf16", 300_001, 5)])
+                                   ("bf16", 170_001, 161), ("bf16", 204_801, 161), ("f32", 102_401, 161), ("bf16", 300_001, 5),
+                                   # both sides of the rule between a workgroup a row and parts
+                                   ("bf16", 32_774, 1), ("bf16", 32_784, 1), ("bf16", 50_000, 28), ("bf16", 50_000, 29), ("f32", 50_001, 56),
+                                   ("f32", 50_001, 57), ("bf16", 131_072, 74), ("bf16", 131_072, 75), ("f32", 110_000, 124), ("f32", 110_000, 125),
+                                   ("bf16", 524_296, 3), ("bf16", 530_001, 128), ("f32", 262_150, 129)])
 def test_many_rows(lib, t, V, T):
     n = 4_000_000 // V + 1
     z, ids, tau, w = lists(min(T, n), V, 70, V, dtype=TYPES[t])
