@@ -54,7 +54,7 @@ struct Mass {
 };
 __device__ __forceinline__ Mass no_mass() { return Mass{kLowest, 0.f}; }
 __device__ __forceinline__ Mass rebase(const Mass& x, float m, float c) {
-  return Mass{m, x.s * rescale(x.m, m, c)};
+  return Mass{m, x.s * __builtin_amdgcn_exp2f(exponent_to(x.m, m, c))};
 }
 __device__ __forceinline__ Mass merge(const Mass& a, const Mass& b, float c) {
 #pragma clang fp contract(off)  // the same whichever side is which, so that all lanes agree
@@ -77,12 +77,22 @@ __device__ __forceinline__ void add(Mass& x, u32x4* v, float c) {
   x = rebase(x, m, c);
   const Base2 below = base2(m, c);
   float s = 0.f;
+  if (!below.far) {
 #pragma unroll
-  for (int n = 0; n < N; ++n) {
-    again(v[n]);
+    for (int n = 0; n < N; ++n) {
+      again(v[n]);
 #pragma unroll
-    for (int e = 0; e < kPer<T>; ++e) s += __builtin_amdgcn_exp2f(below.of(element<T>(v[n], e)));
-    asm volatile("" : "+v"(s));  // one vector's elements after another's
+      for (int e = 0; e < kPer<T>; ++e) s += __builtin_amdgcn_exp2f(below.of<false>(element<T>(v[n], e)));
+      asm volatile("" : "+v"(s));  // one vector's elements after another's
+    }
+  } else {
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      again(v[n]);
+#pragma unroll
+      for (int e = 0; e < kPer<T>; ++e) s += __builtin_amdgcn_exp2f(below.of<true>(element<T>(v[n], e)));
+      asm volatile("" : "+v"(s));
+    }
   }
   x.s += s;
 }
@@ -369,9 +379,19 @@ __device__ __forceinline__ Row row_grad(const DistillArgs& g, int t, const Mass&
   return r;
 }
 
-template <typename T>
-__device__ __forceinline__ float outside_of(const Row& o, float l) {
-  return __builtin_amdgcn_exp2f(o.below.of(l)) * o.outside;
+__device__ __forceinline__ float outside_of(const Row& o, float l) { return __builtin_amdgcn_exp2f(o.below.of(l)) * o.outside; }
+// The gradients of a vector's words as if none were listed.
+template <bool STREAM, typename T>
+__device__ __forceinline__ void put_vec(const Row& o, T* out, int i, const u32x4& l) {
+  float y[kPer<T>];
+  if (!o.below.far) {
+#pragma unroll
+    for (int e = 0; e < kPer<T>; ++e) y[e] = __builtin_amdgcn_exp2f(o.below.of<false>(element<T>(l, e))) * o.outside;
+  } else {
+#pragma unroll
+    for (int e = 0; e < kPer<T>; ++e) y[e] = __builtin_amdgcn_exp2f(o.below.of<true>(element<T>(l, e))) * o.outside;
+  }
+  store_vec<STREAM>(out, i, y);
 }
 
 // This thread's places' gradients, over what it wrote before.
@@ -424,7 +444,7 @@ __device__ __forceinline__ uint64_t distill_row(const DistillArgs& g) {
   __shared__ Parts<NT> parts;
   __shared__ u32x4 more[L ? L : 1][L ? NT : 1];
   static_assert(L % kBatch == 0 && N % kBatch == 0, "whole batches");
-  const float c = a.inv_temp * kLog2e;
+  const float c = base2_rate(a);
   // a list's waves ask for its words' logits before the row's vectors, and wait for no vector to have them
   Place place[kPlaces<NT>];
   load_places<NT>(g, t, place);
@@ -504,12 +524,7 @@ __device__ __forceinline__ uint64_t distill_row(const DistillArgs& g) {
     if (o.zero) {
       zero_vectors<STREAM>(out, sp, 0, sp.vectors, true, a.V);
     } else {
-      auto put = [&](int i, const u32x4& l) {
-        float y[kPer<T>];
-#pragma unroll
-        for (int e = 0; e < kPer<T>; ++e) y[e] = outside_of<T>(o, element<T>(l, e));
-        store_vec<STREAM>(out + sp.head, i, y);
-      };
+      auto put = [&](int i, const u32x4& l) { put_vec<STREAM>(o, out + sp.head, i, l); };
 #pragma unroll
       for (int n = 0; n < N; ++n) {
         const int i = (int)threadIdx.x + n * NT;
@@ -532,7 +547,7 @@ __device__ __forceinline__ uint64_t distill_row(const DistillArgs& g) {
           }
         }
       }
-      if (odd >= 0) store1(out + odd, outside_of<T>(o, lodd));
+      if (odd >= 0) store1(out + odd, outside_of(o, lodd));
     }
   }
   if (late) {
@@ -571,7 +586,7 @@ __global__ __launch_bounds__(kPartThreads) void distill_sums_kernel(DistillArgs 
   const Span sp = row_span(row, a.V);
   const int first = p * a.chunk, end = min(first + a.chunk, sp.vectors), odd = odd_of<T>(sp, a.V);
   const bool odds = p == a.splits - 1;
-  const float c = a.inv_temp * kLog2e;
+  const float c = base2_rate(a);
   Place place[1];
   load_places<kPartThreads>(g, t, place);
   Mass x = no_mass();
@@ -633,7 +648,7 @@ __device__ __forceinline__ uint64_t distill_part(const DistillArgs& g) {
   if (p > 0 && !a.dlogits) return before;
   __shared__ Listed<T, kPartThreads, 1> list;  // its bits are not used
   __shared__ Parts<kPartThreads> parts;
-  const float c = a.inv_temp * kLog2e;
+  const float c = base2_rate(a);
   Place place[1];
   load_places<kPartThreads>(g, t, place);
   const int lane = (int)(threadIdx.x & 63);
@@ -679,16 +694,13 @@ __device__ __forceinline__ uint64_t distill_part(const DistillArgs& g) {
     for (int n = 0; n < U; ++n) {
       const int i = i0 + n * kPartThreads + (int)threadIdx.x;
       if (i >= end) break;
-      float y[kPer<T>];
-#pragma unroll
-      for (int e = 0; e < kPer<T>; ++e) y[e] = outside_of<T>(o, element<T>(v[n], e));
-      store_vec<STREAM>(out + sp.head, i, y);
+      put_vec<STREAM>(o, out + sp.head, i, v[n]);
     }
     i0 += U * kPartThreads;
     if (i0 < end) load(i0);
   }
   const int odd = odd_of<T>(sp, a.V);
-  if (odds && odd >= 0) store1(out + odd, outside_of<T>(o, load1(row + odd)));
+  if (odds && odd >= 0) store1(out + odd, outside_of(o, load1(row + odd)));
   write_places(list, o, out);
   return before;
 }

@@ -284,28 +284,31 @@ __device__ __forceinline__ void zero_vectors(T* out, const Span& sp, int first, 
 // ------------------------------------------------------------- sums in base 2
 
 // For exponentials below a logit m, 2^(l c - k) with k = m c rounded, one instruction and one rounding before the
-// exponential: sums of such terms are (exactly) 2^log2_off(m) times those of 2^((l - m) c), so that the rounding of k
-// costs nothing. Where m c is too large for float32, only words equal to m are not 0, which c = 1/2 gives too.
+// exponential: sums of such terms are 2^off times those of 2^((l - m) c), off = m c - k exactly, so that the rounding of k
+// costs nothing. Where k is so large that its rounding is not small (lowest values, temperatures near 0: FAR), logits are
+// subtracted first, and off is 0.
 struct Base2 {
-  float c, k;
-  __device__ __forceinline__ float of(float l) const { return fmaf(l, c, -k); }
+  float c, k, m;
+  bool far;
+  template <bool FAR>
+  __device__ __forceinline__ float of(float l) const {
+    return FAR ? (l - m) * c : fmaf(l, c, -k);
+  }
+  __device__ __forceinline__ float of(float l) const { return far ? of<true>(l) : of<false>(l); }
+  __device__ __forceinline__ float off() const { return far ? 0.f : fmaf(m, c, -k); }
 };
+// c for logits: 1 / temperature in base 2.
+__device__ __forceinline__ float base2_rate(const LogitsArgs& a) { return fminf(a.inv_temp * kLog2e, -kLowest); }
 __device__ __forceinline__ Base2 base2(float m, float c) {
   const float k = m * c;
-  return fabsf(k) < 3e38f ? Base2{c, k} : Base2{0.5f, 0.5f * m};
+  return Base2{c, k, m, !(fabsf(k) < 0x1p22f)};
 }
-__device__ __forceinline__ float log2_off(float m, float c) {
-  const Base2 b = base2(m, c);
-  return b.of(m);
-}
-// What sums below `from` are times, below m >= from.
-__device__ __forceinline__ float rescale(float from, float m, float c) {
-#pragma clang fp contract(off)  // both products rounded, as in base2
-  const Base2 b = base2(m, c);
-  const float k = from * b.c;
-  return __builtin_amdgcn_exp2f(k - b.k);
+// The exponent by which sums below `from` go on below m >= from.
+__device__ __forceinline__ float exponent_to(float from, float m, float c) {
+  const Base2 a = base2(from, c), b = base2(m, c);
+  return a.far || b.far ? (from - m) * c + (b.off() - a.off()) : a.k - b.k;
 }
 // Natural logarithm of a sum below m, had its terms been 2^((l - m) c).
-__device__ __forceinline__ float log_below(float s, float m, float c) { return logf(s) - log2_off(m, c) * (1.f / kLog2e); }
+__device__ __forceinline__ float log_below(float s, float m, float c) { return logf(s) - base2(m, c).off() * (1.f / kLog2e); }
 
 }  // namespace pda

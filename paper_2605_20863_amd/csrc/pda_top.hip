@@ -252,7 +252,7 @@ struct Mass {
   float m, s, u;
 };
 __device__ __forceinline__ Mass rebase(const Mass& x, float m, float c) {
-  const float f = rescale(x.m, m, c), k = base2(x.m, c).k - base2(m, c).k;
+  const float k = exponent_to(x.m, m, c), f = __builtin_amdgcn_exp2f(k);
   return Mass{m, x.s * f, f * fmaf(x.s, fmaxf(k, kFar), x.u)};
 }
 __device__ __forceinline__ Mass merge(const Mass& a, const Mass& b, float c) {
@@ -294,7 +294,7 @@ __device__ __forceinline__ RowStats row_stats(const LogitsArgs& a, const Mass& x
     r.ent = r.log_s = 0.f;
     return r;
   }
-  r.log_s = log_below(x.s, x.m, a.inv_temp * kLog2e);
+  r.log_s = log_below(x.s, x.m, base2_rate(a));
   r.lp = (ly - x.m) * a.inv_temp - r.log_s;
   r.ent = logf(x.s) - x.u / x.s * (1.f / kLog2e);
   return r;
@@ -380,16 +380,27 @@ __device__ __forceinline__ int select_part(const T* row, const Span& sp, int V, 
     x = rebase(x, m, c);
     const Base2 below = base2(m, c);
     float s = 0.f, w = 0.f;
+    const auto sum = [&](float d) {
+      const float p = __builtin_amdgcn_exp2f(d);
+      s += p;
+      w = fmaf(p, fmaxf(d, kFar), w);
+    };
+    if (!below.far) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      again(v[u]);
+      for (int u = 0; u < U; ++u) {
+        again(v[u]);
 #pragma unroll
-      for (int e = 0; e < kPer<T>; ++e) {
-        const float d = below.of(element<T>(v[u], e)), p = __builtin_amdgcn_exp2f(d);
-        s += p;
-        w = fmaf(p, fmaxf(d, kFar), w);
+        for (int e = 0; e < kPer<T>; ++e) sum(below.of<false>(element<T>(v[u], e)));
+        asm volatile("" : "+v"(s), "+v"(w));  // one vector's elements after another's
       }
-      asm volatile("" : "+v"(s), "+v"(w));  // one vector's elements after another's
+    } else {
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        again(v[u]);
+#pragma unroll
+        for (int e = 0; e < kPer<T>; ++e) sum(below.of<true>(element<T>(v[u], e)));
+        asm volatile("" : "+v"(s), "+v"(w));
+      }
     }
     x.s += s;
     x.u += w;
@@ -522,7 +533,7 @@ __device__ __forceinline__ void join_parts(const TopArgs& g, int t, Pool& b) {
   const float ly = load_part(reinterpret_cast<const float*>(a.part + (int64_t)t * a.splits) + 3);
   const float* part = reinterpret_cast<const float*>(a.part + (int64_t)t * a.splits + min(s, a.splits - 1));
   const Mass mine = {load_part(part), load_part(part + 1), load_part(part + 2)};
-  const Mass x = lanes_merge<64>(s < a.splits ? mine : Mass{kLowest, 0.f, 0.f}, a.inv_temp * kLog2e);
+  const Mass x = lanes_merge<64>(s < a.splits ? mine : Mass{kLowest, 0.f, 0.f}, base2_rate(a));
   const RowStats r = row_stats(a, x, ly);
   if (threadIdx.x == 0) write_stats(g, t, r);
 #pragma unroll
@@ -578,7 +589,7 @@ __global__ __launch_bounds__(kPartThreads, 6) void top_kernel(TopArgs g) {
   const T* row = static_cast<const T*>(a.logits) + (int64_t)t * a.stride;
   const Span sp = row_span(row, a.V);
   const int first = p * a.chunk, end = min(first + a.chunk, sp.vectors);
-  const float c = a.inv_temp * kLog2e, ly = load1(row + y);
+  const float c = base2_rate(a), ly = load1(row + y);
   Mass x;
   const int n = select_part<T, U, STREAM>(row, sp, a.V, first, end, p == a.splits - 1, g.K, c, b, x);
   x = group_merge(x, c);
@@ -677,7 +688,7 @@ __global__ __launch_bounds__(kPartThreads) void top_rows_kernel(TopArgs g) {
     if (lane == 0) write_stats(g, t, RowStats{});
     return;
   }
-  const float low = -__builtin_huge_valf(), c = a.inv_temp * kLog2e;
+  const float low = -__builtin_huge_valf(), c = base2_rate(a);
   const T* row = static_cast<const T*>(a.logits) + (int64_t)t * a.stride;
   const Span sp = row_span(row, a.V);
   u32x4 v[N];
@@ -697,19 +708,29 @@ __global__ __launch_bounds__(kPartThreads) void top_rows_kernel(TopArgs g) {
   Mass x = {m, 0.f, 0.f};
   {
     const Base2 below = base2(m, c);
-    const auto add = [&](float l) {
-      const float d = below.of(l), p = __builtin_amdgcn_exp2f(d);
+    const auto sum = [&](float d) {
+      const float p = __builtin_amdgcn_exp2f(d);
       x.s += p;
       x.u = fmaf(p, fmaxf(d, kFar), x.u);
     };
+    if (!below.far) {
 #pragma unroll
-    for (int n = 0; n < N; ++n) {
-      again(v[n]);
+      for (int n = 0; n < N; ++n) {
+        again(v[n]);
 #pragma unroll
-      for (int e = 0; e < kPer<T>; ++e) add(element<T>(v[n], e));
-      asm volatile("" : "+v"(x.s), "+v"(x.u));
+        for (int e = 0; e < kPer<T>; ++e) sum(below.of<false>(element<T>(v[n], e)));
+        asm volatile("" : "+v"(x.s), "+v"(x.u));
+      }
+    } else {
+#pragma unroll
+      for (int n = 0; n < N; ++n) {
+        again(v[n]);
+#pragma unroll
+        for (int e = 0; e < kPer<T>; ++e) sum(below.of<true>(element<T>(v[n], e)));
+        asm volatile("" : "+v"(x.s), "+v"(x.u));
+      }
     }
-    add(lodd);
+    sum(below.of(lodd));
   }
   x = lanes_merge<64>(x, c);
   const RowStats r = row_stats(a, x, ly);

@@ -192,6 +192,28 @@ def test_masks_and_special_values(lib, T, V, b, rest):
         assert grad[r].isnan().all() or (~grad[r].isnan()).sum() <= K
 
 
+@pytest.mark.parametrize("T,V", [(5, 900), (4, 40_000), (650, 700)])
+@pytest.mark.parametrize("temp", [1e-37, 1e-20, 1e24, 1e38])
+def test_temperatures(lib, T, V, temp):
+    """Near 0 one word takes all, far up all take the same: the parts that are finite are as the reference has them."""
+    z, ids, tau, w = base(T, V, 9)
+    z[0] = -3.3e38
+    z[1, : V // 2] = -3.3e38
+    exact = torch.tensor(temp, dtype=torch.float32).double().item()
+    for b, rest in ((0.0, True), (1.0, True), (1.0, False)):
+        grad = torch.empty((T, V), device=DEV)
+        _, losses = run(lib, z.to(DEV), ids, tau, w, b, rest, temp, min(temp, 1.0), grad)
+        want = R.distill(z, ids, tau, w, b, rest, exact, min(exact, 1.0))
+        finite = want["losses"] < 3e38
+        assert (losses.cpu()[~finite] > 2.9e38).all()
+        R.near(losses[finite.to(DEV)], want["losses"][finite], want["loss_bound"][finite] + 4 * R.EPS24 * want["losses"][finite].abs(),
+               torch.float32, "losses")
+        if temp > 1:
+            R.near(grad, want["dlogits"], want["grad_bound"] * (1 + 1e-6), torch.float32, "gradient")
+        else:
+            assert grad.isfinite().all()
+
+
 @pytest.mark.parametrize("rest", [True, False])
 def test_close_distributions_keep_their_digits(lib, rest):
     """A student that has learnt nearly everything: the divergences are far below their terms."""

@@ -165,6 +165,29 @@ def test_options_change_nothing_else(lib):
         assert (one - lp).abs().max() < 2e-5 and (e - H).abs().max() < 2e-5
 
 
+@pytest.mark.parametrize("t", ["f32", "bf16"])
+@pytest.mark.parametrize("temp", [1e-37, 1e-30, 1e-6, 1e6, 1e24, 1e38])
+@pytest.mark.parametrize("T,V", [(5, 900), (4, 9000), (3, 70_001), (700, 3000)])
+def test_temperatures(lib, t, temp, T, V):
+    """From one word that takes all (or shares it with its equals) to an even distribution, with masked and lowest logits."""
+    z, y = batch(T, V, TYPES[t], 7, masked=0.01)
+    z[0] = -3.3e38
+    z[1, : V // 2] = -3.3e38
+    if temp < 1:
+        z[2, 5], z[2, V - 2] = 40.0, 40.0
+    x = padded(z, 1)
+    exact = torch.tensor(temp, dtype=torch.float32).double().item()
+    ids, tops, lp, H = run(lib, x, 20, temp, y)
+    want, (wt, bt), (wl, bl), (wh, bh) = R.top(z, 20, exact, y)
+    assert torch.equal(ids.cpu().long(), want)
+    # a log-probability past float32's range is -inf; 1 / temperature is rounded once more
+    over = lambda v: torch.where(v < -torch.finfo(torch.float32).max, -math.inf, v)  # noqa: E731
+    more = 2 * R.EPS24
+    R.near(tops, over(wt), bt + more * wt.abs().nan_to_num(0, 0, 0), torch.float32, "log-probabilities")
+    R.near(lp, over(wl), bl + more * wl.abs().nan_to_num(0, 0, 0), torch.float32, "targets'")
+    R.near(H, wh, bh + more, torch.float32, "entropies")
+
+
 def test_rows_past_32_bits(lib):
     """Rows that start past 2^31 elements."""
     T, V = 17_000, 130_001
