@@ -23,6 +23,8 @@
 #include "pda_lm_internal.h"
 #include "pda_rows.h"
 
+#include <type_traits>
+
 namespace pda {
 namespace {
 
@@ -54,6 +56,7 @@ struct Mass {
 };
 __device__ __forceinline__ Mass no_mass() { return Mass{kLowest, 0.f}; }
 __device__ __forceinline__ Mass rebase(const Mass& x, float m, float c) {
+#pragma clang fp contract(off)  // a rounded product, whatever adds it: lanes that sum each other's agree
   return Mass{m, x.s * __builtin_amdgcn_exp2f(exponent_to(x.m, m, c))};
 }
 __device__ __forceinline__ Mass merge(const Mass& a, const Mass& b, float c) {
@@ -74,43 +77,35 @@ __device__ __forceinline__ void add(Mass& x, u32x4* v, float c) {
   for (int n = 0; n < N; ++n)
 #pragma unroll
     for (int e = 0; e < kPer<T>; ++e) m = fmaxf(m, element<T>(v[n], e));
-  x = rebase(x, m, c);
-  const Base2 below = base2(m, c);
+  const Base2 below = base2(m, c), before = base2(x.m, c);
   float s = 0.f;
-  if (!below.far) {
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    again(v[n]);
+#pragma unroll
+    for (int e = 0; e < kPer<T>; ++e) s += __builtin_amdgcn_exp2f(below.of<false>(element<T>(v[n], e)));
+    asm volatile("" : "+v"(s));  // one vector's elements after another's
+  }
+#pragma unroll
+  for (int n = 0; n < N; ++n) again(v[n]);
+  // seldom, and apart, so that it costs the others a branch a batch
+  if (__builtin_expect(__ballot(below.far || (before.far && x.s != 0.f)) != 0, 0)) {
+    s = 0.f;
 #pragma unroll
     for (int n = 0; n < N; ++n) {
-      again(v[n]);
 #pragma unroll
-      for (int e = 0; e < kPer<T>; ++e) s += __builtin_amdgcn_exp2f(below.of<false>(element<T>(v[n], e)));
-      asm volatile("" : "+v"(s));  // one vector's elements after another's
-    }
-  } else {
-#pragma unroll
-    for (int n = 0; n < N; ++n) {
-      again(v[n]);
-#pragma unroll
-      for (int e = 0; e < kPer<T>; ++e) s += __builtin_amdgcn_exp2f(below.of<true>(element<T>(v[n], e)));
+      for (int e = 0; e < kPer<T>; ++e) s += __builtin_amdgcn_exp2f(below.of(element<T>(v[n], e)));
       asm volatile("" : "+v"(s));
     }
+    x = rebase(x, m, c);
+  } else {
+#pragma clang fp contract(off)
+    x = Mass{m, x.s * __builtin_amdgcn_exp2f(before.k - below.k)};
   }
   x.s += s;
 }
-// Over the 64 lanes, in each of them (in one order of additions for all).
-__device__ __forceinline__ float wave_total(float x) {
-  x = group_sum<16>(x);
-  x += __shfl_xor(x, 16, 64);
-  return x + __shfl_xor(x, 32, 64);
-}
-__device__ __forceinline__ double wave_total(double x) {
-#pragma unroll
-  for (int o = 1; o < 64; o *= 2) x += __shfl_xor(x, o, 64);
-  return x;
-}
 __device__ __forceinline__ Mass wave_merge(const Mass& x, float c) {
-  float m = group_max<16>(x.m);
-  m = fmaxf(m, __shfl_xor(m, 16, 64));
-  m = fmaxf(m, __shfl_xor(m, 32, 64));
+  const float m = wave_top(x.m);
   return Mass{m, wave_total(rebase(x, m, c).s)};
 }
 // Over W waves' sums, in every thread.
@@ -381,16 +376,11 @@ __device__ __forceinline__ Row row_grad(const DistillArgs& g, int t, const Mass&
 
 __device__ __forceinline__ float outside_of(const Row& o, float l) { return __builtin_amdgcn_exp2f(o.below.of(l)) * o.outside; }
 // The gradients of a vector's words as if none were listed.
-template <bool STREAM, typename T>
+template <bool STREAM, bool FAR, typename T>
 __device__ __forceinline__ void put_vec(const Row& o, T* out, int i, const u32x4& l) {
   float y[kPer<T>];
-  if (!o.below.far) {
 #pragma unroll
-    for (int e = 0; e < kPer<T>; ++e) y[e] = __builtin_amdgcn_exp2f(o.below.of<false>(element<T>(l, e))) * o.outside;
-  } else {
-#pragma unroll
-    for (int e = 0; e < kPer<T>; ++e) y[e] = __builtin_amdgcn_exp2f(o.below.of<true>(element<T>(l, e))) * o.outside;
-  }
+  for (int e = 0; e < kPer<T>; ++e) y[e] = __builtin_amdgcn_exp2f(o.below.of<FAR>(element<T>(l, e))) * o.outside;
   store_vec<STREAM>(out, i, y);
 }
 
@@ -524,26 +514,33 @@ __device__ __forceinline__ uint64_t distill_row(const DistillArgs& g) {
     if (o.zero) {
       zero_vectors<STREAM>(out, sp, 0, sp.vectors, true, a.V);
     } else {
-      auto put = [&](int i, const u32x4& l) { put_vec<STREAM>(o, out + sp.head, i, l); };
+      // seldom: from the row itself again, so that the others have no second copy of what follows (447 us for 442, 4,096 x 131,072 bf16)
+      const bool far = __builtin_amdgcn_readfirstlane(o.below.far);
+#pragma unroll 1
+      for (int i = (int)threadIdx.x; far && i < sp.vectors; i += NT)
+        put_vec<STREAM, true>(o, out + sp.head, i, load_vec<false>(row + sp.head, i));
+      if (!far) {
+        auto put = [&](int i, const u32x4& l) { put_vec<STREAM, false>(o, out + sp.head, i, l); };
 #pragma unroll
-      for (int n = 0; n < N; ++n) {
-        const int i = (int)threadIdx.x + n * NT;
-        if (i >= sp.vectors) break;
-        again(v[n]);
-        put(i, v[n]);
-      }
-      for (int l = 0; l < L; ++l) {
-        const int i = (int)threadIdx.x + (N + l) * NT;
-        if (i < sp.vectors) put(i, more[l][threadIdx.x]);
-      }
-      if constexpr (X > 0) {
-        for (int n = N + L; n < live; n += kBatch) {
-          u32x4 m[kBatch];
-          load_more(n, m);
+        for (int n = 0; n < N; ++n) {
+          const int i = (int)threadIdx.x + n * NT;
+          if (i >= sp.vectors) break;
+          again(v[n]);
+          put(i, v[n]);
+        }
+        for (int l = 0; l < L; ++l) {
+          const int i = (int)threadIdx.x + (N + l) * NT;
+          if (i < sp.vectors) put(i, more[l][threadIdx.x]);
+        }
+        if constexpr (X > 0) {
+          for (int n = N + L; n < live; n += kBatch) {
+            u32x4 m[kBatch];
+            load_more(n, m);
 #pragma unroll
-          for (int j = 0; j < kBatch; ++j) {
-            const int i = (int)threadIdx.x + (n + j) * NT;
-            if (i < sp.vectors) put(i, m[j]);
+            for (int j = 0; j < kBatch; ++j) {
+              const int i = (int)threadIdx.x + (n + j) * NT;
+              if (i < sp.vectors) put(i, m[j]);
+            }
           }
         }
       }
@@ -689,16 +686,20 @@ __device__ __forceinline__ uint64_t distill_part(const DistillArgs& g) {
     zero_vectors<STREAM>(out, sp, first, end, odds, a.V);
     return before;
   }
-  for (int i0 = first; i0 < end;) {
+  const auto write = [&](auto far) {
+    for (int i0 = first; i0 < end;) {
 #pragma unroll
-    for (int n = 0; n < U; ++n) {
-      const int i = i0 + n * kPartThreads + (int)threadIdx.x;
-      if (i >= end) break;
-      put_vec<STREAM>(o, out + sp.head, i, v[n]);
+      for (int n = 0; n < U; ++n) {
+        const int i = i0 + n * kPartThreads + (int)threadIdx.x;
+        if (i >= end) break;
+        put_vec<STREAM, decltype(far)::value>(o, out + sp.head, i, v[n]);
+      }
+      i0 += U * kPartThreads;
+      if (i0 < end) load(i0);
     }
-    i0 += U * kPartThreads;
-    if (i0 < end) load(i0);
-  }
+  };
+  if (o.below.far) write(std::true_type());
+  else write(std::false_type());
   const int odd = odd_of<T>(sp, a.V);
   if (odds && odd >= 0) store1(out + odd, outside_of(o, load1(row + odd)));
   write_places(list, o, out);

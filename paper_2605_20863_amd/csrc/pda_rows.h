@@ -281,6 +281,23 @@ __device__ __forceinline__ void zero_vectors(T* out, const Span& sp, int first, 
   if (odds && odd >= 0) store1(out + odd, 0.f);
 }
 
+// Over the 64 lanes, in each of them (in one order of additions for all).
+__device__ __forceinline__ float wave_total(float x) {
+  x = group_sum<16>(x);
+  x += __shfl_xor(x, 16, 64);
+  return x + __shfl_xor(x, 32, 64);
+}
+__device__ __forceinline__ double wave_total(double x) {
+#pragma unroll
+  for (int o = 1; o < 64; o *= 2) x += __shfl_xor(x, o, 64);
+  return x;
+}
+__device__ __forceinline__ float wave_top(float x) {
+  x = group_max<16>(x);
+  x = fmaxf(x, __shfl_xor(x, 16, 64));
+  return fmaxf(x, __shfl_xor(x, 32, 64));
+}
+
 // ------------------------------------------------------------- sums in base 2
 
 // For exponentials below a logit m, 2^(l c - k) with k = m c rounded, one instruction and one rounding before the
@@ -305,10 +322,11 @@ __device__ __forceinline__ Base2 base2(float m, float c) {
 }
 // The exponent by which sums below `from` go on below m >= from.
 __device__ __forceinline__ float exponent_to(float from, float m, float c) {
+#pragma clang fp contract(off)  // rounded products, as in base2
   const Base2 a = base2(from, c), b = base2(m, c);
   return a.far || b.far ? (from - m) * c + (b.off() - a.off()) : a.k - b.k;
 }
 // Natural logarithm of a sum below m, had its terms been 2^((l - m) c).
-__device__ __forceinline__ float log_below(float s, float m, float c) { return logf(s) - base2(m, c).off() * (1.f / kLog2e); }
+__device__ __forceinline__ float log_below(float s, float m, float c) { return fmaf(base2(m, c).off(), -1.f / kLog2e, logf(s)); }
 
 }  // namespace pda

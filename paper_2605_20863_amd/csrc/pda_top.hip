@@ -252,6 +252,7 @@ struct Mass {
   float m, s, u;
 };
 __device__ __forceinline__ Mass rebase(const Mass& x, float m, float c) {
+#pragma clang fp contract(off)  // rounded products, whatever adds them: lanes that sum each other's agree
   const float k = exponent_to(x.m, m, c), f = __builtin_amdgcn_exp2f(k);
   return Mass{m, x.s * f, f * fmaf(x.s, fmaxf(k, kFar), x.u)};
 }
@@ -267,19 +268,16 @@ __device__ __forceinline__ void add1(Mass& x, float l, float c) {
   x.s += p;
   x.u = fmaf(p, fmaxf(d, kFar), x.u);
 }
-template <int N>
-__device__ __forceinline__ Mass lanes_merge(Mass x, float c) {
-#pragma unroll
-  for (int o = 1; o < N; o *= 2)
-    x = merge(x, Mass{__shfl_xor(x.m, o, 64), __shfl_xor(x.s, o, 64), __shfl_xor(x.u, o, 64)}, c);
-  // the first lane's: a merge's roundings depend on the order of its two sides
-  const auto first = [](float y) { return as_f32((uint32_t)__builtin_amdgcn_readfirstlane((int)as_u32(y))); };
-  return N < 64 ? x : Mass{first(x.m), first(x.s), first(x.u)};
+// Over the 64 lanes, in each of them.
+__device__ __forceinline__ Mass wave_merge(const Mass& x, float c) {
+  const float m = wave_top(x.m);
+  const Mass y = rebase(x, m, c);
+  return Mass{m, wave_total(y.s), wave_total(y.u)};
 }
 // Over the workgroup, in every thread (and a barrier for all of them).
 __device__ __forceinline__ Mass group_merge(Mass x, float c) {
   __shared__ Mass parts[kWaves];
-  x = lanes_merge<64>(x, c);
+  x = wave_merge(x, c);
   if ((threadIdx.x & 63) == 0) parts[threadIdx.x >> 6] = x;
   __syncthreads();
   Mass y = parts[0];
@@ -295,8 +293,8 @@ __device__ __forceinline__ RowStats row_stats(const LogitsArgs& a, const Mass& x
     return r;
   }
   r.log_s = log_below(x.s, x.m, base2_rate(a));
-  r.lp = (ly - x.m) * a.inv_temp - r.log_s;
-  r.ent = logf(x.s) - x.u / x.s * (1.f / kLog2e);
+  r.lp = fmaf(ly - x.m, a.inv_temp, -r.log_s);
+  r.ent = fmaf(-x.u / x.s, 1.f / kLog2e, logf(x.s));
   return r;
 }
 
@@ -533,7 +531,7 @@ __device__ __forceinline__ void join_parts(const TopArgs& g, int t, Pool& b) {
   const float ly = load_part(reinterpret_cast<const float*>(a.part + (int64_t)t * a.splits) + 3);
   const float* part = reinterpret_cast<const float*>(a.part + (int64_t)t * a.splits + min(s, a.splits - 1));
   const Mass mine = {load_part(part), load_part(part + 1), load_part(part + 2)};
-  const Mass x = lanes_merge<64>(s < a.splits ? mine : Mass{kLowest, 0.f, 0.f}, base2_rate(a));
+  const Mass x = wave_merge(s < a.splits ? mine : Mass{kLowest, 0.f, 0.f}, base2_rate(a));
   const RowStats r = row_stats(a, x, ly);
   if (threadIdx.x == 0) write_stats(g, t, r);
 #pragma unroll
@@ -732,7 +730,7 @@ __global__ __launch_bounds__(kPartThreads) void top_rows_kernel(TopArgs g) {
     }
     sum(below.of(lodd));
   }
-  x = lanes_merge<64>(x, c);
+  x = wave_merge(x, c);
   const RowStats r = row_stats(a, x, ly);
   if (lane == 0) write_stats(g, t, r);
 
