@@ -198,7 +198,27 @@ template <typename T, int RT, int N, bool STREAM>
 __global__ __launch_bounds__(kGroup<RT>) void norm_backward_kernel(NormArgs a) {
   constexpr int ROWS = kGroup<RT> / RT;
   const int sub = (int)threadIdx.x / RT, lane = (int)threadIdx.x % RT, vecs = a.H / 8;
-  float acc[N][8] = {};
+  float acc[N][8] = {}, held[N][8] = {};
+  const auto load_weights = [&](int n, float (&w)[8]) {
+    const int i = lane + n * RT;
+    if (i < vecs) load_weight(a.w, a.w_bf16, 8 * i, w);
+  };
+  // Each thread's weights stay in registers where four waves a SIMD still fit, since a row's would be waited for twice (us per call,
+  // bf16, loaded for each row / held: 16,384 x 4,096 110 / 94, 8,192 x 4,096 58.5 / 51.0, 2,000 x 16,384 67.3 / 62.8, 32,768 x 1,024
+  // 54 / 52; at 512 threads of 16 elements three waves, 512 x 8,192 19.3 / 21.1).
+  constexpr bool HOLD = N == 1 || (N == 2 && RT != 512);
+  if constexpr (HOLD) {
+#pragma unroll
+    for (int n = 0; n < N; ++n) load_weights(n, held[n]);
+  }
+  const auto weights = [&](int n, float (&w)[8]) {
+    if constexpr (HOLD) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) w[e] = held[n][e];
+    } else {
+      load_weights(n, w);
+    }
+  };
   int turn = 0;
   for (int t = (int)blockIdx.x * ROWS + sub; t < a.T; t += a.wgs * ROWS, ++turn) {
     Raw<T> x[N] = {}, g[N] = {}, q[N] = {};
@@ -218,7 +238,7 @@ __global__ __launch_bounds__(kGroup<RT>) void norm_backward_kernel(NormArgs a) {
       float h[8], y[8], w[8];
       unpack(x[n], h);
       unpack(g[n], y);
-      load_weight(a.w, a.w_bf16, 8 * i, w);
+      weights(n, w);
       float b = 0.f, c = 0.f;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
@@ -237,7 +257,7 @@ __global__ __launch_bounds__(kGroup<RT>) void norm_backward_kernel(NormArgs a) {
       float h[8], y[8], w[8], o[8];
       unpack(x[n], h);
       unpack(g[n], y);
-      load_weight(a.w, a.w_bf16, 8 * i, w);
+      weights(n, w);
       unpack(q[n], o);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
