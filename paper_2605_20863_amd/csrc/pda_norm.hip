@@ -332,7 +332,7 @@ hipError_t launch(K kernel, int64_t wgs, int threads, const NormArgs& a, hipStre
 // them / past them, alone and between the copy that makes x and a product that reads the result (by 1,024 columns):
 //   tokens x width    16,384 x 4,096         8,192 x 4,096         32,768 x 1,024        4,096 x 8,192         2,048 x 16,384        6,144 x 4,096
 //   norm        95.4 / 89.3, 248 / 241  40.1 / 44.6, 139 / 126 39.5 / 43.8, 131 / 125 40.9 / 44.8, 155 / 137 42.4 / 46.2, 210 / 175 30.1 / 33.4, 101 / 101
-//   gradient   115.6 / 113.1, 270 / 265 54.4 / 62.0, 148 / 147 52.4 / 66.6, 159 / 157 58.5 / 62.7, 165 / 159 76.1 / 77.9, 238 / 213 40.9 / 49.5, 108 / 118
+//   gradient  102.3 / 92.2, 261 / 238  46.3 / 50.8, 135 / 133 46.6 / 49.6, 137 / 137 58.5 / 63.2, 165 / 160 56.2 / 59.6, 216 / 191 35.5 / 40.0, 102 / 107
 constexpr int64_t kStreamBytes = 1 << 28;
 
 template <typename T>

@@ -8,6 +8,8 @@
 #include "pda_lm_internal.h"
 #include "pda_rows.h"
 
+#include <type_traits>
+
 namespace pda {
 namespace {
 
@@ -360,6 +362,10 @@ __device__ __forceinline__ int select_part(const T* row, const Span& sp, int V, 
   const bool few = K <= kPartThreads / 4;
   uint32_t floor = 0;  // the K-th largest rank so far is not below it
   int since = first, mine = n;  // the vectors that came after the last look at all keys; what this wave held then
+  // 0 times -inf of a masked word is NaN: exponents have a least value (kFar), in longer parts from this wave's first batch with one
+  // on (us per call, 20 alternatives of 131,072 words bf16, always / from the first on: 4,096 rows 206 / 199, half of the words
+  // masked 186 / 195). Parts of few batches do not begin one twice (64 rows, half masked 15.6 / 16.9).
+  bool masked = end - first <= 2 * U * kPartThreads;
   for (int i0 = first, batch = 0; i0 < end; i0 += U * kPartThreads, ++batch) {
     u32x4 v[U];
     float vm[U];
@@ -377,28 +383,28 @@ __device__ __forceinline__ int select_part(const T* row, const Span& sp, int V, 
     }
     x = rebase(x, m, c);
     const Base2 below = base2(m, c);
-    float s = 0.f, w = 0.f;
-    const auto sum = [&](float d) {
-      const float p = __builtin_amdgcn_exp2f(d);
-      s += p;
-      w = fmaf(p, fmaxf(d, kFar), w);
-    };
-    if (!below.far) {
+    float s, w;
+    const auto sums = [&](auto far, auto least) {
+      s = w = 0.f;
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         again(v[u]);
 #pragma unroll
-        for (int e = 0; e < kPer<T>; ++e) sum(below.of<false>(element<T>(v[u], e)));
+        for (int e = 0; e < kPer<T>; ++e) {
+          const float d = below.of<decltype(far)::value>(element<T>(v[u], e)), p = __builtin_amdgcn_exp2f(d);
+          s += p;
+          w = fmaf(p, decltype(least)::value ? fmaxf(d, kFar) : d, w);
+        }
         asm volatile("" : "+v"(s), "+v"(w));  // one vector's elements after another's
       }
-    } else {
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        again(v[u]);
-#pragma unroll
-        for (int e = 0; e < kPer<T>; ++e) sum(below.of<true>(element<T>(v[u], e)));
-        asm volatile("" : "+v"(s), "+v"(w));
-      }
+    };
+    if (!masked) {
+      sums(std::false_type(), std::false_type());
+      masked = __ballot(below.far || w != w) != 0;
+    }
+    if (masked) {
+      if (!below.far) sums(std::false_type(), std::true_type());
+      else sums(std::true_type(), std::true_type());
     }
     x.s += s;
     x.u += w;
