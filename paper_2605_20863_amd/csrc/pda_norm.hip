@@ -347,7 +347,7 @@ template <typename T, bool FP8, int RT, int N>
 hipError_t norm_rows(const NormArgs& a, hipStream_t s) {
   constexpr int rows = kGroup<RT> / RT;
   const int64_t wgs = ((int64_t)a.T + rows - 1) / rows;
-  if constexpr (sizeof(T) == 2)
+  if constexpr (sizeof(T) == 2 && !(N == 1 && RT >= 512))  // few rows' threads: below kStreamBytes
     if (streamed<T>(a)) return launch(&norm_kernel<T, RT, N, FP8, true>, wgs, kGroup<RT>, a, s);
   return launch(&norm_kernel<T, RT, N, FP8, false>, wgs, kGroup<RT>, a, s);
 }
@@ -355,6 +355,7 @@ hipError_t norm_rows(const NormArgs& a, hipStream_t s) {
 // Few rows take twice as many threads each (us per call, bf16, half / all of them: 3 x 4,096 5.2 / 4.3, 64 x 8,192 5.8 / 5.0, 512 x 8,192
 // 10.6 / 10.0, 512 x 4,096 4.8 / 4.6; 2,048 x 4,096 12.0 / 13.0, 16,384 x 8,192 184 / 188).
 constexpr int kFewRows = 1024;
+static_assert((int64_t)kFewRows * 8192 * 8 < kStreamBytes, "few rows of one vector a thread are never streamed");
 
 template <typename T, bool FP8>
 hipError_t norm_for(const NormArgs& a, hipStream_t s) {
