@@ -358,7 +358,7 @@ __device__ __forceinline__ int select_part(const T* row, const Span& sp, int V, 
   };
   Bar bar = {low, false};
   // one wave of the workgroup, not always the same, settles the bars: the vector ALUs have no time for four
-  const int judge = (int)blockIdx.x % kWaves;
+  const int settler = (int)blockIdx.x % kWaves;
   const bool few = K <= kPartThreads / 4;
   uint32_t floor = 0;  // the K-th largest rank so far is not below it
   int since = first, mine = n;  // the vectors that came after the last look at all keys; what this wave held then
@@ -419,7 +419,7 @@ __device__ __forceinline__ int select_part(const T* row, const Span& sp, int V, 
       b.tops[threadIdx.x] = rank_of(lo);
       if (!few) b.tops[kPartThreads + threadIdx.x] = rank_of(hi);
       __syncthreads();
-      if (wave == judge) {
+      if (wave == settler) {
         uint32_t t[2 * kWaves], r;
 #pragma unroll
         for (int j = 0; j < kWaves; ++j) t[j] = b.tops[lane + 64 * j];
@@ -465,7 +465,7 @@ __device__ __forceinline__ int select_part(const T* row, const Span& sp, int V, 
       n = wave == 0 ? total : 0;
       __syncthreads();
     } else if (!last && now.all() >= K) {
-      if (wave == judge) {
+      if (wave == settler) {
         floor = kth_held(b, now, K, floor);
         if (lane == 0) b.floor = floor;
       }
@@ -484,7 +484,7 @@ __device__ __forceinline__ int select_part(const T* row, const Span& sp, int V, 
   take(odd >= sp.head && lodd != low, lodd, odd);
   uint32_t least = 0;
   if (held.all() > kPartThreads / 2 && held.all() > K) {
-    if (wave == judge) {
+    if (wave == settler) {
       least = kth_held(b, held, K, floor);
       if (lane == 0) b.floor = least;
     }

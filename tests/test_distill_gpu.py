@@ -192,6 +192,20 @@ def test_masks_and_special_values(lib, T, V, b, rest):
         assert grad[r].isnan().all() or (~grad[r].isnan()).sum() <= K
 
 
+@pytest.mark.parametrize("t,V", [("bf16", 70_001), ("bf16", 140_000), ("bf16", 200_003), ("f32", 110_001)])
+def test_lowest_words_of_long_rows(lib, t, V):
+    """Rows in registers, LDS and read again, whose words are the type's lowest in whole or in part."""
+    T = 130
+    z, ids, tau, w = base(T, V, 40)
+    z = z.to(TYPES[t])
+    z[0] = -3.3e38
+    z[1, : V // 2] = -3.3e38
+    z[2, V // 2:] = -3.3e38
+    z[3, V - 20_000: V - 9] = -math.inf
+    z[4, 5:30] = -3.3e38
+    check(lib, z, ids, tau, w, 0.5, True, 1.0, 64.0)
+
+
 @pytest.mark.parametrize("T,V", [(5, 900), (4, 40_000), (650, 700)])
 @pytest.mark.parametrize("temp", [1e-37, 1e-20, 1e24, 1e38])
 def test_temperatures(lib, T, V, temp):

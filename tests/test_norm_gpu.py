@@ -217,6 +217,41 @@ def test_gradient_against_differences(lib):
         assert abs(slope - dot) <= 64 * R.EPS24 * size + 1e-8 * (1 + size)
 
 
+@pytest.mark.parametrize("out", ["bf16", "f32", "fp8"])
+@pytest.mark.parametrize("H", [64, 512, 2048, 4096, 8192, 16384, 32768])
+def test_a_row_is_the_same_in_every_call(lib, H, out):
+    """Whatever the other rows, and however many: bit for bit, in calls around every limit on their number."""
+    T = 1030 if H < 16384 else 40
+    x, res, w = inputs(T, H, torch.bfloat16, torch.bfloat16, H)
+    x, res, w = x.to(DEV), res.to(DEV), w.to(DEV)
+
+    def run(n):
+        o, s = torch.empty((n, H), dtype=TYPES[out], device=DEV), torch.empty((n, H), dtype=torch.bfloat16, device=DEV)
+        scales = torch.empty(n, device=DEV) if out == "fp8" else None
+        lib.add_rms_norm(x[:n], w, o, res[:n], s, scales, eps=EPS)
+        return o.view(torch.uint8), s, scales
+
+    want = run(T)
+    for n in (1, 3, 4, 37, 1023, 1024):
+        if n < T:
+            for a, b in zip(run(n), want):
+                assert a is None or torch.equal(a, b[:n]), n
+
+
+@pytest.mark.parametrize("out", ["bf16", "fp8"])
+def test_zeros_without_eps(lib, out):
+    """A row of zeros has no norm with eps 0: NaN in its own row alone; its gradient likewise."""
+    x, _, w = inputs(5, 256, torch.bfloat16, torch.float32, 3)
+    x[2] = 0
+    x, w = x.to(DEV), w.to(DEV)
+    o, dx = torch.empty((5, 256), dtype=TYPES[out], device=DEV), torch.empty((5, 256), dtype=torch.bfloat16, device=DEV)
+    lib.add_rms_norm(x, w, o, scales=torch.empty(5, device=DEV) if out == "fp8" else None, eps=0.0)
+    lib.add_rms_norm_backward(x, w, x, dx, eps=0.0)
+    for r in range(5):
+        assert bool(o[r].float().isnan().all()) == (r == 2) and bool(dx[r].float().isnan().any()) == (r == 2)
+        assert r == 2 or not o[r].float().isnan().any()
+
+
 def test_no_rows(lib):
     H = 64
     e = torch.empty((0, H), dtype=torch.bfloat16, device=DEV)

@@ -188,6 +188,27 @@ def test_temperatures(lib, t, temp, T, V):
     R.near(H, wh, bh + more, torch.float32, "entropies")
 
 
+@pytest.mark.parametrize("t", ["f32", "bf16"])
+@pytest.mark.parametrize("T,V", [(300, 70_001), (3, 131_072)])
+def test_masks_that_begin_late(lib, t, T, V):
+    """Masked and lowest words in the first, a later or the last of a row's batches alone, and in one thread's vector."""
+    z, y = batch(T, V, TYPES[t], 11)
+    third = V // 3
+    for r in range(T):
+        low = -math.inf if r % 2 else -3.3e38
+        part = (slice(0, third), slice(third, 2 * third), slice(2 * third, V), slice(V - 5, V - 4), slice(V // 2, V // 2 + 8))[r % 5]
+        z[r, part] = low
+    exact = torch.tensor(0.9, dtype=torch.float32).double().item()
+    ids, tops, lp, H = run(lib, padded(z, 0), 20, 0.9, y)
+    want, (wt, bt), (wl, bl), (wh, bh) = R.top(z, 20, exact, y)
+    assert torch.equal(ids.cpu().long(), want)
+    # -3.3e38 / 0.9 = -3.67e38 rounds to -inf: it is more than half a step past -3.4028e38
+    wl = torch.where(wl < -torch.finfo(torch.float32).max, -math.inf, wl)
+    R.near(tops, wt, bt, torch.float32, "log-probabilities")
+    R.near(lp, wl, bl, torch.float32, "targets'")
+    R.near(H, wh, bh, torch.float32, "entropies")
+
+
 def test_rows_past_32_bits(lib):
     """Rows that start past 2^31 elements."""
     T, V = 17_000, 130_001
