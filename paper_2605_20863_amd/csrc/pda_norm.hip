@@ -132,7 +132,7 @@ __device__ __forceinline__ float scale_of(float amax) { return fmaxf(__fdiv_rn(a
 __device__ __forceinline__ float inv_rms(float squares, const NormArgs& a) { return 1.f / sqrtf(squares / (float)a.H + a.eps); }
 
 // Bound by its bytes where rows are many: 16,384 x 4,096 bf16 with residual 88 us, 6.1 TB/s (a copy of 256 MiB 5.3); 512 x 8,192 into fp8
-// 9.2 us and 3 x 4,096 4.2, of which a launch with one load and one store takes most.
+// 8.8 us and 3 x 4,096 4, of which a launch with one load and one store takes most.
 template <typename T, int RT, int N, bool FP8, bool STREAM>
 __global__ __launch_bounds__(kGroup<RT>) void norm_kernel(NormArgs a) {
   constexpr int ROWS = kGroup<RT> / RT;
