@@ -67,8 +67,9 @@ typedef struct pdalm_norm_problem {
  *
  * A row's results are the same in every call of its width, whatever the other rows.
  * A row that holds NaN gives NaN in its whole out (code 0x7f; its scales are those of
- * its other values) and in no other row's. Squares are summed in float32: a row whose mean square
- * passes 3e38 gives 0, and with eps 0 a row of zeros NaN.
+ * its other values) and in no other row's. Squares are summed in float32, where their
+ * sum passes it those of the row times 2^-72: a row gives 0 where the mean square itself passes
+ * float32 (3.4e38). With eps 0 a row of zeros gives NaN, and values below 1e-19 lose digits.
  *
  * Errors: PDA_EINVAL for bad sizes, types, strides, NULL or misaligned pointers, or more
  * than 2^22 rows; PDA_EUNSUPPORTED for a width that is no multiple of 8 or above 32768, and a

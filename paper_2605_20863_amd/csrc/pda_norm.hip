@@ -41,8 +41,9 @@ __device__ __forceinline__ Two wave_both(Two x) {
 }
 
 // The same over a row's RT threads, M of each added up one after another's, so that RT threads' M give the bits of RT M threads' one;
-// `turn` alternates between a workgroup's rows, so that one barrier a row does.
-template <int RT, bool MAX, int M>
+// `turn` alternates between a workgroup's rows, so that one barrier a row does. SELDOM: in few registers rather than quickly, with an array
+// of its own.
+template <int RT, bool MAX, bool SELDOM = false, int M>
 __device__ __forceinline__ Two row_both(Two (&x)[M], int turn) {
 #pragma unroll
   for (int m = 0; m < M; ++m) x[m] = wave_both<MAX>(x[m]);
@@ -60,8 +61,15 @@ __device__ __forceinline__ Two row_both(Two (&x)[M], int turn) {
     }
     __syncthreads();
     all = parts[turn & 1][0][0];
+    // up to 16 in registers at once; of the 32 of 1,024 threads' two sums 8, so that two such rows' waves fit beside each other
+    constexpr int S = SELDOM ? 1 : M * W > 16 ? 8 : M * W;
+    const Two* p = &parts[turn & 1][0][0];
 #pragma unroll
-    for (int i = 1; i < M * W; ++i) join(all, parts[turn & 1][i / W][i % W]);
+    for (int i = 1; i < S; ++i) join(all, p[i]);
+#pragma unroll 1
+    for (int j = S; j < M * W; j += S)
+#pragma unroll
+      for (int i = 0; i < S; ++i) join(all, p[j + i]);
   } else {
 #pragma unroll
     for (int m = 1; m < M; ++m) join(all, x[m]);
@@ -105,6 +113,22 @@ __device__ __forceinline__ void add_rounded(Raw<float>& x, const Raw<float>& r) 
     x.b[i] = as_u32(a[4 + i] + b[4 + i]);
   }
 }
+// x times s, a power of two: exact but for what falls below the type's smallest numbers.
+__device__ __forceinline__ void scale_raw(Raw<uint16_t>& x, float s) {
+  float a[8];
+  unpack(x, a);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) x.a[i] = pack_bf16(a[2 * i] * s, a[2 * i + 1] * s);
+}
+__device__ __forceinline__ void scale_raw(Raw<float>& x, float s) {
+  float a[8];
+  unpack(x, a);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    x.a[i] = as_u32(a[i] * s);
+    x.b[i] = as_u32(a[4 + i] * s);
+  }
+}
 template <bool STREAM>
 __device__ __forceinline__ void store_raw(void* base, int64_t at, const Raw<uint16_t>& x) {
   put16<STREAM>(static_cast<uint16_t*>(base) + at, x.a);
@@ -130,6 +154,14 @@ __device__ __forceinline__ uint32_t encode4(const float* y, const Div& d) {
 __device__ __forceinline__ float scale_of(float amax) { return fmaxf(__fdiv_rn(amax, kE4M3Max), kMinScale); }
 
 __device__ __forceinline__ float inv_rms(float squares, const NormArgs& a) { return 1.f / sqrtf(squares / (float)a.H + a.eps); }
+
+// A row whose squares sum past float32, where their mean need not: its sums are made again of the row times kDown, all of whose squares'
+// sums float32 holds, and whose 1 / rms follows from them; 0 where the mean itself passes float32.
+constexpr float kDown = 0x1p-72f;
+__device__ __forceinline__ float inv_rms_down(float squares, const NormArgs& a) {
+  const float mean = squares / (float)a.H + a.eps * kDown * kDown;
+  return mean < 0x1p-16f ? 1.f / sqrtf(mean) : 0.f;  // 2^128 kDown^2
+}
 
 // Bound by its bytes where rows are many: 16,384 x 4,096 bf16 with residual 88 us, 6.1 TB/s (a copy of 256 MiB 5.3); 512 x 8,192 into fp8
 // 8.8 us and 3 x 4,096 4, of which a launch with one load and one store takes most.
@@ -163,15 +195,7 @@ __global__ __launch_bounds__(kGroup<RT>) void norm_kernel(NormArgs a) {
   // up to 2 sums of a thread, for which the calls of few rows have a thread each: a row's results are the same in both
   constexpr int M = N <= 2 ? N : 1;
   Two sums[M] = {};
-#pragma unroll
-  for (int n = 0; n < N; ++n) {
-    const int i = lane + n * RT;
-    if (i >= vecs) continue;
-    Two& s = sums[n % M];
-    if (a.res) {
-      add_rounded(x[n], r[n]);
-      if (a.sum) store_raw<STREAM>(a.sum, t * a.sum_stride + 8 * i, x[n]);
-    }
+  const auto add_squares = [&](int n, Two& s) {
     float h[8];
     unpack(x[n], h);
     float q = 0.f;
@@ -184,9 +208,31 @@ __global__ __launch_bounds__(kGroup<RT>) void norm_kernel(NormArgs a) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) s.b = fmaxf(s.b, fabsf(h[e] * w[e]));
     }
+  };
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    const int i = lane + n * RT;
+    if (i >= vecs) continue;
+    Two& s = sums[n % M];
+    if (a.res) {
+      add_rounded(x[n], r[n]);
+      if (a.sum) store_raw<STREAM>(a.sum, t * a.sum_stride + 8 * i, x[n]);
+    }
+    add_squares(n, s);
   }
   Two s = row_both<RT, true>(sums, 0);
-  const float rms = inv_rms(s.a, a);
+  float rms = inv_rms(s.a, a);
+  if (__builtin_expect(s.a == __builtin_huge_valf(), 0)) {  // all of a row's threads
+    Two anew[M] = {};
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      if (lane + n * RT >= vecs) continue;
+      scale_raw(x[n], kDown);
+      add_squares(n, anew[n % M]);
+    }
+    s = row_both<RT, true, true>(anew, 0);
+    rms = inv_rms_down(s.a, a);
+  }
   if (FP8 && !a.group) {
     s.b = scale_of(s.b * rms);
     if (lane == 0) a.scales[t] = s.b;

@@ -1,0 +1,49 @@
+"""The residual stream's norm and its gradient at the ends of their ranges (64-bit references and bounds of
+tests/_lm_ref.py)."""
+
+import pytest
+import torch
+
+from tests import _lm_ref as R
+from tests.test_norm_gpu import DEV, EPS, TYPES, lib, rand  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+# rows' sizes: below the sum's limit (3.4e38 / H), past it, close to the mean's limit, past that (a norm of 0)
+SIZES = [1.0, 1e16, 1e17, 5e17, 1e18, 9e18, 1.5e19, 4e19, 1e25, 1e37]
+
+
+def large(T, H, dt, seed):
+    x = rand((T, H), seed)
+    x = x / (x * x).mean(dim=1, keepdim=True).sqrt()
+    size = torch.tensor([SIZES[(i * 7 + 3) % len(SIZES)] for i in range(T)])
+    x = (x * size[:, None]).clamp(-3e38, 3e38).to(dt)
+    return x, size > 2e19
+
+
+@pytest.mark.parametrize("out", ["bf16", "f32", "fp8"])
+@pytest.mark.parametrize("t", ["bf16", "f32"])
+@pytest.mark.parametrize("T,H", [(13, 64), (21, 512), (30, 1000), (11, 2048), (15, 4096), (1030, 4096), (12, 8192), (11, 16384), (10, 32768)])
+def test_rows_whose_squares_sum_past_float32(lib, T, H, t, out):
+    """The norm of every row whose mean square float32 holds, and 0 for larger ones, with weights that take |h w| past it."""
+    x, zero = large(T, H, TYPES[t], H)
+    w = 50 * (1 + rand((H,), 2, amp=0.2))
+    o = torch.empty((T, H), dtype=TYPES[out], device=DEV)
+    y, bound = R.norm(x, w, EPS)
+    y[zero], bound[zero] = 0, 0
+    if out == "fp8":
+        for group in (g for g in (0, 64, 128) if g == 0 or H % g == 0):
+            s = torch.empty((T, H // group if group else 1), device=DEV)
+            lib.add_rms_norm(x.to(DEV), w.to(DEV), o, scales=s, eps=EPS)
+            scales, ds, z, dz = R.fp8(y, bound, group)
+            R.near(s, scales, ds, torch.float32, "scales")
+            assert ((o.float().cpu().double() - z).abs() <= dz).all()
+    else:
+        lib.add_rms_norm(x.to(DEV), w.to(DEV), o, eps=EPS)
+        R.near(o, y, bound, TYPES[out], "norm")
+    if t == "bf16" and out == "bf16":  # the sum as it is kept, with its residual
+        half, kept = x / 2, torch.empty_like(x, device=DEV)
+        lib.add_rms_norm(half.to(DEV), w.to(DEV), o, half.to(DEV), kept, eps=EPS)
+        assert torch.equal(kept.cpu(), (half.float() * 2).to(torch.bfloat16))
+        R.near(o, *[torch.where(zero[:, None], 0.0, v) for v in R.norm(kept.cpu(), w, EPS)], torch.bfloat16, "norm of the sum")
