@@ -91,6 +91,7 @@ int pdalm_add_rms_norm(const void* x,
  *     grad_h = grad_residual + r (g w - y' mean(g w y')),  y' = h r,  g = grad_out
  * which is the gradient of x and of residual alike, and
  *     grad_weight [H] f32 = sum over tokens of g y'   (NULL: not wanted)
+ * r is the forward's (0 for a row whose mean square passes float32).
  * grad_h may be grad_out or grad_residual where strides agree. The sums are in a
  * fixed order: repeated calls give identical results. out_dtype and scale_group
  * are not read. Uses the stream's workspace (with grad_weight: 4 bytes for each weight and each of 1,024

@@ -95,6 +95,10 @@ __device__ __forceinline__ void have_weight(const RawWeight& w, bool bf16, float
   else unpack(w.full, y);
 }
 
+// Makes the compiler unpack the elements again after this point, rather than keep them in registers of their own.
+__device__ __forceinline__ void again(Raw<uint16_t>& x) { asm volatile("" : "+v"(x.a)); }
+__device__ __forceinline__ void again(Raw<float>& x) { asm volatile("" : "+v"(x.a), "+v"(x.b)); }
+
 // h = x + residual in the stream's type, as kept.
 __device__ __forceinline__ void add_rounded(Raw<uint16_t>& x, const Raw<uint16_t>& r) {
   float a[8], b[8];
@@ -295,37 +299,57 @@ __global__ __launch_bounds__(kGroup<RT>) void norm_backward_kernel(NormArgs a) {
       load_weights(n, w);
     }
   };
+  // of the longest rows grad_residual is loaded as it is used: beside the rest of the row it has no registers, and spills cost more (1,000 x
+  // 32,768 f32 184 us, so 163 with 112 bytes of scratch left, bf16 none; 2,000 x 16,384 f32 117 / 114)
+  constexpr bool LATE = N == 4 || (RT == 1024 && sizeof(T) == 4);
   int turn = 0;
   for (int t = (int)blockIdx.x * ROWS + sub; t < a.T; t += a.wgs * ROWS, ++turn) {
-    Raw<T> x[N] = {}, g[N] = {}, q[N] = {};
+    Raw<T> x[N] = {}, g[N] = {}, q[LATE ? 1 : N] = {};
 #pragma unroll
     for (int n = 0; n < N; ++n) {
       const int i = lane + n * RT;
       if (i >= vecs) continue;
       x[n] = load8<STREAM, T>(a.x, t * a.x_stride + 8 * i);
       g[n] = load8<STREAM, T>(a.out, t * a.out_stride + 8 * i);
-      if (a.res) q[n] = load8<STREAM, T>(a.res, t * a.res_stride + 8 * i);
+      if (!LATE && a.res) q[LATE ? 0 : n] = load8<STREAM, T>(a.res, t * a.res_stride + 8 * i);
     }
-    Two sums[1] = {};
+    const auto sum_row = [&](float scale, Two (&sums)[1]) {
 #pragma unroll
-    for (int n = 0; n < N; ++n) {
-      const int i = lane + n * RT;
-      if (i >= vecs) continue;
-      float h[8], y[8], w[8];
-      unpack(x[n], h);
-      unpack(g[n], y);
-      weights(n, w);
-      float b = 0.f, c = 0.f;
+      for (int n = 0; n < N; ++n) {
+        const int i = lane + n * RT;
+        if (i >= vecs) continue;
+        float h[8], y[8], w[8];
+        unpack(x[n], h);
+        unpack(g[n], y);
+        weights(n, w);
+        float b = 0.f, c = 0.f;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        b = fmaf(h[e], h[e], b);
-        c = fmaf(y[e] * w[e], h[e], c);
+        for (int e = 0; e < 8; ++e) {
+          h[e] *= scale;
+          b = fmaf(h[e], h[e], b);
+          c = fmaf(y[e] * w[e], h[e], c);
+        }
+        sums[0].a += b;
+        sums[0].b += c;
       }
-      sums[0].a += b;
-      sums[0].b += c;
+    };
+    Two sums[1] = {};
+    sum_row(1.f, sums);
+    Two s = row_both<RT, false>(sums, turn);
+    float rms = inv_rms(s.a, a), back = s.b / (float)a.H * rms * rms;
+    if (__builtin_expect(s.a == __builtin_huge_valf(), 0)) {  // all of a row's threads
+#pragma unroll
+      for (int n = 0; n < N && N > 1; ++n) {
+        again(x[n]);
+        again(g[n]);
+      }
+      sums[0] = {};
+      sum_row(kDown, sums);
+      s = row_both<RT, false, true>(sums, 0);  // (a barrier lies between two rows' of these)
+      rms = inv_rms_down(s.a, a);
+      back = s.b / (float)a.H * rms * rms * kDown;
+      rms *= kDown;
     }
-    const Two s = row_both<RT, false>(sums, turn);
-    const float rms = inv_rms(s.a, a), back = s.b / (float)a.H * rms * rms;
 #pragma unroll
     for (int n = 0; n < N; ++n) {
       const int i = lane + n * RT;
@@ -334,7 +358,8 @@ __global__ __launch_bounds__(kGroup<RT>) void norm_backward_kernel(NormArgs a) {
       unpack(x[n], h);
       unpack(g[n], y);
       weights(n, w);
-      unpack(q[n], o);
+      if (LATE && a.res) q[0] = load8<STREAM, T>(a.res, t * a.res_stride + 8 * i);
+      unpack(q[LATE ? 0 : n], o);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         acc[n][e] = fmaf(y[e], h[e] * rms, acc[n][e]);

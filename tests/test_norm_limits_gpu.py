@@ -47,3 +47,22 @@ def test_rows_whose_squares_sum_past_float32(lib, T, H, t, out):
         lib.add_rms_norm(half.to(DEV), w.to(DEV), o, half.to(DEV), kept, eps=EPS)
         assert torch.equal(kept.cpu(), (half.float() * 2).to(torch.bfloat16))
         R.near(o, *[torch.where(zero[:, None], 0.0, v) for v in R.norm(kept.cpu(), w, EPS)], torch.bfloat16, "norm of the sum")
+
+
+@pytest.mark.parametrize("add", [False, True])
+@pytest.mark.parametrize("t", ["bf16", "f32"])
+@pytest.mark.parametrize("T,H", [(13, 64), (21, 512), (30, 1000), (11, 2048), (15, 4096), (1030, 4096), (12, 8192), (11, 16384), (10, 32768),
+                                 (600, 16384)])
+def test_gradient_of_rows_whose_squares_sum_past_float32(lib, T, H, t, add):
+    """As the forward's: r is that of every row whose mean square float32 holds, and 0 for larger ones."""
+    dt = TYPES[t]
+    h, zero = large(T, H, dt, H)
+    w, g = 1 + rand((H,), 2, amp=0.2), rand((T, H), 3, dt, 0.1)
+    q = rand((T, H), 4, dt, 1e-3) if add else None
+    dh, dw = torch.empty((T, H), dtype=dt, device=DEV), torch.empty(H, device=DEV)
+    lib.add_rms_norm_backward(h.to(DEV), w.to(DEV), g.to(DEV), dh, dw, None if q is None else q.to(DEV), eps=EPS)
+    want, bound, _, _ = R.norm_grad(h, w, g, q, EPS)
+    want[zero] = q[zero].double() if add else 0.0
+    R.near(dh, want, bound, dt, "gradient of the stream")
+    _, _, wdw, dwb = R.norm_grad(h[~zero], w, g[~zero], None, EPS)
+    R.near(dw, wdw, dwb, torch.float32, "gradient of the weights")
