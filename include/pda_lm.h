@@ -66,10 +66,11 @@ typedef struct pdalm_norm_problem {
  *             nearest even, so that out * scale stands for y
  *
  * A row's results are the same in every call of its width, whatever the other rows.
- * A row that holds NaN gives NaN in its whole out (code 0x7f; its scales are those of
- * its other values) and in no other row's. Squares are summed in float32, where their
- * sum passes it those of the row times 2^-72: a row gives 0 where the mean square itself passes
- * float32 (3.4e38). With eps 0 a row of zeros gives NaN, and values below 1e-19 lose digits.
+ * A row whose stream holds NaN gives NaN in its whole out (in fp8 code 0x7f, and every
+ * scale of the row 2^-126) and in no other row's; a weight's NaN stays in its column.
+ * Squares are summed in float32, where their sum passes it those of the row times 2^-72:
+ * a row gives 0 (NaN where it is infinite) where the mean square itself passes float32
+ * (3.4e38). With eps 0 a row of zeros gives NaN, and values below 1e-19 lose digits.
  *
  * Errors: PDA_EINVAL for bad sizes, types, strides, NULL or misaligned pointers, or more
  * than 2^22 rows; PDA_EUNSUPPORTED for a width that is no multiple of 8 or above 32768, and a

@@ -144,7 +144,7 @@ __device__ __forceinline__ void store_raw(void* base, int64_t at, const Raw<floa
   put16<STREAM>(p + 4, x.b);
 }
 
-// Codes of y / s; NaN stays NaN (a clamp by min and max would make a number of it).
+// Codes of y / s; NaN stays NaN (a clamp by min and max would make a number of it), of either sign 0x7f.
 __device__ __forceinline__ uint32_t encode4(const float* y, const Div& d) {
   float z[4];
 #pragma unroll
@@ -153,7 +153,8 @@ __device__ __forceinline__ uint32_t encode4(const float* y, const Div& d) {
     z[i] = z[i] > kE4M3Max ? kE4M3Max : z[i] < -kE4M3Max ? -kE4M3Max : z[i];
   }
   const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(z[0], z[1], 0, false);
-  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(z[2], z[3], lo, true);
+  const uint32_t codes = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(z[2], z[3], lo, true);
+  return codes & ~(((codes & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u);  // the sign of a byte whose other bits are all ones
 }
 __device__ __forceinline__ float scale_of(float amax) { return fmaxf(__fdiv_rn(amax, kE4M3Max), kMinScale); }
 

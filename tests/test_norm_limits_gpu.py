@@ -66,3 +66,34 @@ def test_gradient_of_rows_whose_squares_sum_past_float32(lib, T, H, t, add):
     R.near(dh, want, bound, dt, "gradient of the stream")
     _, _, wdw, dwb = R.norm_grad(h[~zero], w, g[~zero], None, EPS)
     R.near(dw, wdw, dwb, torch.float32, "gradient of the weights")
+
+
+@pytest.mark.parametrize("group", [0, 64, 128])
+@pytest.mark.parametrize("t", ["bf16", "f32"])
+@pytest.mark.parametrize("T,H", [(4, 256), (4, 4096), (1100, 4096), (3, 16384)])
+def test_nan_rows_in_fp8(lib, T, H, t, group):
+    """One NaN, of either sign, in the stream, the residual or the weights: every code of the row is 0x7f, every scale 2^-126."""
+    x, res, w = rand((T, H), 1, TYPES[t]), rand((T, H), 2, TYPES[t]), rand((H,), 3)
+    nan = torch.tensor([0x7FC0, 0xFFC0 - 0x10000], dtype=torch.int16).view(torch.bfloat16).to(TYPES[t])
+    assert not nan[0].signbit() and nan[1].signbit()
+    x[0, 9], x[1, H - 1], res[2, 77] = nan[0], nan[1], nan[1]
+
+    def run(w):
+        o = torch.empty((T, H), dtype=torch.uint8, device=DEV)
+        s = torch.full((T, H // group) if group else (T, 1), 9.0, device=DEV)
+        lib.add_rms_norm(x.to(DEV), w.to(DEV), o, res.to(DEV), scales=s, eps=EPS)
+        return o.cpu(), s.cpu()
+
+    codes, scales = run(w)
+    assert (codes[:3] == 0x7F).all(), codes[:3].unique()
+    assert (scales[:3] == 2.0 ** -126).all()
+    assert (codes[3:] & 0x7F != 0x7F).all() and (scales[3:] > 2.0 ** -126).all()
+    # a weight's NaN is its column's alone, and its group's scale that of the others
+    x[:3], res[2] = rand((3, H), 4, TYPES[t]), rand((1, H), 5, TYPES[t])
+    plain, plain_scales = run(w.clone().index_fill_(0, torch.tensor([70]), 0.0))
+    for v in nan:
+        codes, scales = run(w.clone().index_fill_(0, torch.tensor([70]), float(v)) if not v.signbit()
+                            else torch.where(torch.arange(H) == 70, v.float(), w))
+        assert (codes[:, 70] == 0x7F).all(), codes[:, 70].unique()
+        rest = torch.arange(H) != 70
+        assert torch.equal(codes[:, rest], plain[:, rest]) and torch.equal(scales, plain_scales)
