@@ -72,8 +72,9 @@ typedef struct pdalm_norm_problem {
  * a row gives 0 (NaN where it is infinite) where the mean square itself passes float32
  * (3.4e38). With eps 0 a row of zeros gives NaN, and values below 1e-19 lose digits.
  *
- * Errors: PDA_EINVAL for bad sizes, types, strides, NULL or misaligned pointers, or more
- * than 2^22 rows; PDA_EUNSUPPORTED for a width that is no multiple of 8 or above 32768, and a
+ * Errors: PDA_EINVAL for bad sizes, types, strides, NULL or misaligned pointers, more
+ * than 2^22 rows, or as many of a width above 8192 (which the gradient takes);
+ * PDA_EUNSUPPORTED for a width that is no multiple of 8 or above 32768, and a
  * scale_group other than 0, 64 and 128 or that does not divide the width.
  */
 int pdalm_add_rms_norm(const void* x,

@@ -27,6 +27,9 @@ int check_norm(const pdalm_norm_problem* pr, bool gradient, NormArgs* a) {
   if (pr->width < 1) return host_fail(PDA_EINVAL, "width = %d < 1", pr->width);
   if (pr->width % 8 || pr->width > kMaxWidth)
     return host_fail(PDA_EUNSUPPORTED, "width = %d (supported: multiples of 8 up to %d)", pr->width, kMaxWidth);
+  // the norm's launch: 1,024 threads for each of the longest rows (the gradient's workgroups take rows in turn)
+  if (!gradient && pr->width > kLongWidth && pr->num_tokens == kMaxWaves / 16)
+    return host_fail(PDA_EINVAL, "num_tokens = %d (below 2^22 for widths above %d)", pr->num_tokens, kLongWidth);
   if (!float_type(pr->dtype)) return host_fail(PDA_EINVAL, "dtype = %d (supported: F32, BF16)", pr->dtype);
   if (!float_type(pr->weight_dtype)) return host_fail(PDA_EINVAL, "weight_dtype = %d (supported: F32, BF16)", pr->weight_dtype);
   if (!(pr->eps >= 0.f) || !std::isfinite(pr->eps)) return host_fail(PDA_EINVAL, "eps is negative or not finite");

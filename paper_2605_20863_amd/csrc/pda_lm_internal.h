@@ -10,6 +10,7 @@ constexpr int kStatusTwice = 128;  // a teacher's token that its list holds twic
 
 constexpr int kMaxTop = 256;       // alternatives of a row, entries of a list
 constexpr int kMaxWidth = 32768;   // of the residual stream
+constexpr int kLongWidth = 8192;   // above it the norm has 1,024 threads a row, however many rows there are
 
 enum class OutType : int { F32 = 0, BF16 = 1, FP8 = 2 };
 

@@ -454,7 +454,7 @@ hipError_t norm_rows(const NormArgs& a, hipStream_t s) {
 // Few rows take twice as many threads each (us per call, bf16, half / all of them: 3 x 4,096 5.2 / 4.3, 64 x 8,192 5.8 / 5.0, 512 x 8,192
 // 10.6 / 10.0, 512 x 4,096 4.8 / 4.6; 2,048 x 4,096 12.0 / 13.0, 16,384 x 8,192 184 / 188).
 constexpr int kFewRows = 1024;
-static_assert((int64_t)kFewRows * 8192 * 8 < kStreamBytes, "few rows of one vector a thread are never streamed");
+static_assert((int64_t)kFewRows * kLongWidth * 8 < kStreamBytes, "few rows of one vector a thread are never streamed");
 
 template <typename T, bool FP8>
 hipError_t norm_for(const NormArgs& a, hipStream_t s) {
@@ -464,7 +464,7 @@ hipError_t norm_for(const NormArgs& a, hipStream_t s) {
          : v <= 128 ? norm_rows<T, FP8, 128, 1>(a, s)
          : v <= 256 ? norm_rows<T, FP8, 128, 2>(a, s)
          : v <= 512 ? (few ? norm_rows<T, FP8, 512, 1>(a, s) : norm_rows<T, FP8, 256, 2>(a, s))
-         : v <= 1024 ? (few ? norm_rows<T, FP8, 1024, 1>(a, s) : norm_rows<T, FP8, 512, 2>(a, s))
+         : v <= kLongWidth / 8 ? (few ? norm_rows<T, FP8, 1024, 1>(a, s) : norm_rows<T, FP8, 512, 2>(a, s))
          : v <= 2048 ? norm_rows<T, FP8, 1024, 2>(a, s) : norm_rows<T, FP8, 1024, 4>(a, s);
 }
 
