@@ -50,6 +50,14 @@ __device__ __forceinline__ int lanes_before(uint64_t mask) {
   return (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
 }
 
+// Between a wave's writes to LDS and its other lanes' reads of them, or reads and the writes over them: its lanes go on together, and the
+// compiler moves neither across (no instruction of its own).
+__device__ __forceinline__ void wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 // This thread's number, for code that is seldom reached: the compiler works out what follows from it there, rather than
 // once for all at the kernel's start and in registers of its own.
 __device__ __forceinline__ int thread_here() {
@@ -152,6 +160,7 @@ __device__ __forceinline__ int thin(Pool& b, int n, uint32_t least) {
     const uint64_t key = i + lane < n ? keys[i + lane] : 0;
     const bool stays = key && (uint32_t)(key >> 32) >= least;
     const uint64_t mask = __ballot(stays);
+    wave_sync();
     if (stays) keys[kept + lanes_before(mask)] = key;
     kept += (int)__popcll(mask);
   }
@@ -164,6 +173,7 @@ __device__ __forceinline__ int gather(Pool& b, int n, uint32_t least) {
   const int wave = wave_id(), lane = thread_here() & 63;
   uint64_t v[N];
   int kept = 0;
+  wave_sync();  // this wave's last keys
 #pragma unroll
   for (int j = 0; j < N; ++j) {
     v[j] = lane + 64 * j < n ? b.keys[wave * kRegion + lane + 64 * j] : 0;
@@ -337,8 +347,10 @@ __device__ __forceinline__ int select_part(const T* row, const Span& sp, int V, 
   };
   int queued = 0;
   const auto look_through = [&](const float least) {
+    wave_sync();
     const u32x4 w = b.queue[wave][lane];
     const int word = b.first[wave][lane];
+    wave_sync();
 #pragma unroll
     for (int e = 0; e < kPer<T>; ++e) {
       const float l = element<T>(w, e);
@@ -796,6 +808,7 @@ __global__ __launch_bounds__(kPartThreads) void top_rows_kernel(TopArgs g) {
     const auto larger = [&](float l) { return !nan && !(l <= kth); };
     const auto equal = [&](float l) { return nan ? l != l : l == kth; };
     held = 0;
+    wave_sync();
     each([&](float l, int word) { take(larger(l) && l != low, l, word); });
     // of the equal ones the first in the order of words: head, vectors by lane and element, tail
     int room = g.K - held;
@@ -831,6 +844,7 @@ __global__ __launch_bounds__(kPartThreads) void top_rows_kernel(TopArgs g) {
     }
     first_of(odd >= 0 && !head && equal(lodd), lodd, odd);
   }
+  wave_sync();
   if (held <= 64) sort_and_write<1>(g, t, keys, held, x, r);
   else if (held <= 128) sort_and_write<2>(g, t, keys, held, x, r);
   else sort_and_write<4>(g, t, keys, held, x, r);
