@@ -97,3 +97,31 @@ def test_nan_rows_in_fp8(lib, T, H, t, group):
         assert (codes[:, 70] == 0x7F).all(), codes[:, 70].unique()
         rest = torch.arange(H) != 70
         assert torch.equal(codes[:, rest], plain[:, rest]) and torch.equal(scales, plain_scales)
+
+
+def far_apart(x, stride):
+    """x on the device as rows `stride` elements apart, 9 between them where anything is read back."""
+    full = torch.empty((x.shape[0] - 1) * stride + x.shape[1], dtype=x.dtype, device=DEV)
+    rows = full.as_strided(x.shape, (stride, 1))
+    rows.copy_(x)
+    return rows
+
+
+@pytest.mark.parametrize("out", ["bf16", "fp8"])
+@pytest.mark.parametrize("T,H,stride", [(700, 1024, 3_100_008), (5, 8192, (1 << 29) + 8)])
+def test_rows_past_2_to_the_31_elements(lib, T, H, stride, out):
+    """Offsets of rows that 32 bits do not hold: the bits of the same rows side by side."""
+    assert (T - 1) * stride > 1 << 31
+    x, res, g, w = (rand((T, H), i, torch.bfloat16) for i in (1, 2, 3, 4))
+    w = w[0].float().to(DEV)
+
+    def run(place):
+        o, s = place(torch.zeros((T, H), dtype=TYPES[out])), place(torch.zeros_like(x))
+        scales = torch.empty(T, device=DEV) if out == "fp8" else None
+        lib.add_rms_norm(place(x), w, o, place(res), s, scales, eps=EPS)
+        o, dh, dw = o.contiguous(), place(torch.zeros_like(x)), torch.empty(H, device=DEV)
+        lib.add_rms_norm_backward(s, w, place(g), dh, dw, place(res), eps=EPS)
+        return o.view(torch.uint8), s.contiguous(), scales, dh.contiguous(), dw
+
+    for a, b in zip(run(lambda v: far_apart(v, stride)), run(lambda v: v.to(DEV))):
+        assert a is None or torch.equal(a, b)
