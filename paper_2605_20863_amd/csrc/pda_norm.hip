@@ -286,8 +286,8 @@ __global__ __launch_bounds__(kGroup<RT>) void norm_backward_kernel(NormArgs a) {
   };
   // Each thread's weights stay in registers where four waves a SIMD still fit, since a row's would be waited for twice (us per call,
   // bf16, loaded for each row / held: 16,384 x 4,096 110 / 94, 8,192 x 4,096 58.5 / 51.0, 2,000 x 16,384 67.3 / 62.8, 32,768 x 1,024
-  // 54 / 52; at 512 threads of 16 elements three waves, 512 x 8,192 19.3 / 21.1).
-  constexpr bool HOLD = N == 1 || (N == 2 && RT != 512);
+  // 54 / 52, 16,384 x 8,192 202 / 182, 4,096 x 8,192 63.5 / 57.0, 512 x 8,192 19.6 / 18.7).
+  constexpr bool HOLD = N <= 2;
   if constexpr (HOLD) {
 #pragma unroll
     for (int n = 0; n < N; ++n) load_weights(n, held[n]);
