@@ -61,7 +61,8 @@ __device__ __forceinline__ Two row_both(Two (&x)[M], int turn) {
     }
     __syncthreads();
     all = parts[turn & 1][0][0];
-    // up to 16 in registers at once; of the 32 of 1,024 threads' two sums 8, so that two such rows' waves fit beside each other
+    // up to 16 in registers at once; of the 32 of 1,024 threads' two sums 8, so that two such rows' waves fit beside each other (2,048 x 16,384
+    // bf16 into fp8 63 us with all of them, 48 so)
     constexpr int S = SELDOM ? 1 : M * W > 16 ? 8 : M * W;
     const Two* p = &parts[turn & 1][0][0];
 #pragma unroll
@@ -169,7 +170,7 @@ __device__ __forceinline__ float inv_rms_down(float squares, const NormArgs& a) 
 }
 
 // Bound by its bytes where rows are many: 16,384 x 4,096 bf16 with residual 88 us, 6.1 TB/s (a copy of 256 MiB 5.3); 512 x 8,192 into fp8
-// 8.8 us and 3 x 4,096 4, of which a launch with one load and one store takes most.
+// 8.8 us and 3 x 4,096 4, of which a launch with one load and one store takes most; 2,048 x 16,384 into fp8 47, 5.0 TB/s.
 template <typename T, int RT, int N, bool FP8, bool STREAM>
 __global__ __launch_bounds__(kGroup<RT>) void norm_kernel(NormArgs a) {
   constexpr int ROWS = kGroup<RT> / RT;
@@ -301,7 +302,7 @@ __global__ __launch_bounds__(kGroup<RT>) void norm_backward_kernel(NormArgs a) {
     }
   };
   // of the longest rows grad_residual is loaded as it is used: beside the rest of the row it has no registers, and spills cost more (1,000 x
-  // 32,768 f32 184 us, so 163 with 112 bytes of scratch left, bf16 none; 2,000 x 16,384 f32 117 / 114)
+  // 32,768 f32 184 us, so 160 with 112 bytes of scratch left, bf16 none; 2,000 x 16,384 f32 117 / 114)
   constexpr bool LATE = N == 4 || (RT == 1024 && sizeof(T) == 4);
   int turn = 0;
   for (int t = (int)blockIdx.x * ROWS + sub; t < a.T; t += a.wgs * ROWS, ++turn) {

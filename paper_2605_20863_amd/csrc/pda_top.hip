@@ -591,9 +591,9 @@ __device__ __forceinline__ void join_parts(const TopArgs& g, int t, Pool& b) {
 
 // Workgroup (row, part): a whole row's results, or a part's sums and sorted keys, which the last part's workgroup joins
 // where arrivals are counted.
-// Where rows are many the vector ALUs bound it (an element is converted twice and takes half a maximum, two multiply-adds, an addition
-// and an exponential, 6.6 instructions with one of four times the length; looking for its words adds about a third): 4,096 x 131,072 bf16,
-// 64 alternatives 180-199 us, 8,192 rows 328 (6.5 TB/s). Where they are few, the chain of loads, bar, keys, arrival and
+// Where rows are many the vector ALUs bound it (a word's sums take 8.5 instructions by their counters, with two conversions, a maximum, two
+// multiply-adds, an addition and an exponential of four times the length; looking for words adds 2.3): 4,096 x 131,072 bf16,
+// 64 alternatives 180-200 us, 8,192 rows 328 (6.5 TB/s). Where they are few, the chain of loads, bar, keys, arrival and
 // join does: 64 rows, 20 alternatives 14 us.
 // Six workgroups to a compute unit, as many as LDS holds: 4,096 x 131,072 bf16, 256 alternatives, 228 us, with the registers of five 243.
 template <typename T, int U, bool STREAM>
